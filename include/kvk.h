@@ -65,7 +65,9 @@ typedef enum {
 enum { KVK_KIND_GQA = 0, KVK_KIND_MLA = 1 };
 enum { KVK_AXIS_TOKEN = 0, KVK_AXIS_CHANNEL = 1 };
 enum { KVK_QUANT_GROUPED = 0, KVK_QUANT_SYMMETRIC = 1 };
-enum { KVK_DTYPE_F32 = 0, KVK_DTYPE_BF16 = 1 };
+/* F16: the serving entry points only (kvk_rotary_apply, kvk_paged_*,
+ * kvk_prompt_attention). */
+enum { KVK_DTYPE_F32 = 0, KVK_DTYPE_BF16 = 1, KVK_DTYPE_F16 = 2 };
 
 /* Device error word values (kvk_get_device_error). */
 enum {
@@ -74,8 +76,9 @@ enum {
   KVK_DEVERR_CAPACITY = 2,     /* append position >= capacity                */
   KVK_DEVERR_COUNT = 4,        /* per-sequence append count out of range     */
   KVK_DEVERR_TIMEOUT = 8,      /* a bounded wait on an async copy gave up    */
-  KVK_DEVERR_ALIGN = 16        /* shared memory not aligned for a copy; the  */
+  KVK_DEVERR_ALIGN = 16,       /* shared memory not aligned for a copy; the  */
                                /* call computed nothing                      */
+  KVK_DEVERR_PAGE = 32         /* page index outside the pool                */
 };
 
 /* Model geometry.  GQA: n_q_heads query heads, n_kv_heads KV heads of
@@ -489,6 +492,130 @@ kvk_status kvk_set_decode_schedule(kvk_cache *cache, int32_t schedule, int32_t r
  * Returns KVK_ERR_DEVICE if the word was non-zero.  After a
  * KVK_DEVERR_TIMEOUT the outputs of the affected calls are unspecified. */
 kvk_status kvk_get_device_error(kvk_cache *cache, kvk_stream stream, int32_t *code);
+
+/* ---- serving: rotary positions, a paged cache, whole prompts --------------
+ * The steps around the compressed cache that a serving program needs: queries
+ * and keys are rotated to their positions, new tokens enter a cache kept in
+ * pages, chunks of new tokens (single ones included) attend over the pages,
+ * and whole prompts attend to themselves before anything is cached.  The new
+ * tokens of a batch are packed one behind another in one flat dimension;
+ * sequence b's are tokens cu[b] .. cu[b + 1] - 1.  Tokens that belong to no
+ * sequence are left alone: nothing is written for them.
+ * Values are BF16 or F16 (rotary: F32 too); arithmetic, softmax statistics
+ * and sums are binary32, the stored result is rounded once.  The softmax
+ * weights enter the product with the values rounded to the stored type
+ * (once, or in two halves), so an output carries two such roundings. */
+
+/* Rows [n_tokens, heads, head_dim] of device memory, channels contiguous;
+ * strides in elements, at least head_dim (a dimension of size one: any). */
+typedef struct {
+  void *data;
+  int64_t token_stride;
+  int64_t head_stride;
+} kvk_rows;
+
+/* Rotary positions with several axes.  Frequency i < rotary_dim / 2 turns with
+ * the position on axis[i]: the pair (x, y) of channels (i, i + rotary_dim / 2),
+ * or (2 i, 2 i + 1) where `adjacent` is 1, becomes
+ *   (x c - y s, y c + x s),  (c, s) = factor (cos, sin)(pos[axis[i]] inv_freq[i]);
+ * the channels from rotary_dim on stay.  Text has one axis; images and video
+ * have a time, a height and a width.  Angles are exact to 2^-32 of a turn plus
+ * the position times inv_freq's own rounding, at any position.
+ * inv_freq (rotary_dim / 2 doubles) and axis (as many) are host arrays, copied.
+ * head_dim: even, at most 256; rotary_dim: even, at most head_dim; n_axes: 1..8.
+ * Errors: INVALID_ARG. */
+typedef struct kvk_rotary kvk_rotary;
+kvk_status kvk_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t n_axes, const double *inv_freq,
+                             const int32_t *axis, int32_t adjacent, float factor, kvk_rotary **out);
+kvk_status kvk_rotary_destroy(kvk_rotary *rotary);
+
+/* Rotates queries and keys of n_tokens tokens (either may be NULL with 0
+ * heads).  positions: device int32 [n_axes, n_tokens], any sign.  The outputs
+ * may be the inputs themselves; they may not overlap them otherwise. */
+kvk_status kvk_rotary_apply(const kvk_rotary *rotary, const kvk_rows *q, const kvk_rows *q_out, int32_t q_heads,
+                            const kvk_rows *k, const kvk_rows *k_out, int32_t k_heads, int32_t dtype,
+                            int32_t n_tokens, const int32_t *positions, kvk_stream stream);
+
+/* A paged cache: per layer a pool of keys and one of values, each
+ * [n_pages, n_kv_heads, page_size, head_dim] of BF16 or F16, owned by the
+ * caller.  head_dim 64 or 128; page_size 16, 32, 64 or 128; at most 64 query
+ * heads per KV head.  Which pages hold a sequence is the caller's table; a page
+ * may stand in several sequences (a shared prefix). */
+typedef struct {
+  int32_t n_layers, n_q_heads, n_kv_heads, head_dim;
+  int32_t page_size, n_pages;
+  int32_t dtype;       /* KVK_DTYPE_BF16 or KVK_DTYPE_F16 */
+} kvk_paged_desc;
+typedef struct kvk_paged kvk_paged;
+
+/* The batch of a call; device pointers.  lengths count the positions held with
+ * the new tokens: token j of sequence b's n_b new ones sits at position
+ * lengths[b] - n_b + j.  table [batch, max_pages]: sequence b's position t is
+ * slot t % page_size of page table[b][t / page_size]; entries from its last
+ * page on are not read. */
+typedef struct {
+  const int32_t *cu_new;   /* [batch + 1], not decreasing, within [0, n_tokens] */
+  const int32_t *lengths;  /* [batch] */
+  const int32_t *table;
+  int32_t batch, max_pages, n_tokens;
+} kvk_paged_batch;
+
+/* Bytes of one layer's pool of keys (values: as many) and of the workspace. */
+kvk_status kvk_paged_plan(const kvk_paged_desc *desc, size_t *pool_bytes, size_t *ws_bytes);
+/* k_pages, v_pages: n_layers device pointers, 128-byte aligned; workspace:
+ * device, 256-byte aligned.  The current device becomes the cache's; calls
+ * with another current device are refused.  kvk_paged_reset clears the
+ * workspace, and has to have run before the first attention. */
+kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, void *workspace,
+                            size_t ws_bytes, kvk_paged **out);
+kvk_status kvk_paged_destroy(kvk_paged *cache);
+kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
+
+/* Writes the new tokens' keys and values into `layer`'s pages.  With a rotary
+ * the keys are rotated on the way, and with q its queries are rotated to q_out
+ * (which may be q) in the same pass; positions (device int32
+ * [n_axes, n_tokens]) may be NULL for one axis: the tokens' own positions.
+ * Tokens before position 0 are not stored.  A position past max_pages sets
+ * KVK_DEVERR_CAPACITY, a page outside the pool KVK_DEVERR_PAGE; the token is not
+ * stored.  No two tokens of a call may go to the same slot.
+ * Errors: INVALID_ARG. */
+kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *k,
+                            const kvk_rows *v, const kvk_rotary *rotary, const int32_t *positions, const kvk_rows *q,
+                            const kvk_rows *q_out, kvk_stream stream);
+
+/* Attention of the new tokens (appended first) over `layer`'s pages: query j
+ * of sequence b, at position p = lengths[b] - n_b + j, attends to positions
+ * max(0, p - window + 1) .. p (window 0: from 0), query head h reading KV head
+ * h / (n_q_heads / n_kv_heads).  A query before position 0 sees nothing and
+ * gives zeros.  q: post-RoPE, rows on 16 bytes; out: device
+ * [n_tokens, n_q_heads, head_dim] of the cache's dtype, 16-byte aligned.
+ * max_new: no sequence has more new tokens (n_tokens always serves; single
+ * tokens run a form of their own).  A sequence that has more, or more positions
+ * than its table holds, sets KVK_DEVERR_COUNT, and its outputs are unspecified;
+ * a page outside the pool sets KVK_DEVERR_PAGE and reads as zeros.
+ * What the slots behind a sequence's last position hold does not matter, and a
+ * key or value that a query does not see does not change its result, not even
+ * one that is not finite.
+ * Calls that use the same cache object share its workspace and have to be
+ * ordered (one stream, or graphs that do not overlap). */
+kvk_status kvk_paged_attention(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *q,
+                               float softmax_scale, int32_t max_new, int32_t window, void *out, kvk_stream stream);
+/* As kvk_get_device_error, for the paged cache's own error word. */
+kvk_status kvk_paged_get_device_error(kvk_paged *cache, kvk_stream stream, int32_t *code);
+
+/* Attention over whole prompts: causal, grouped heads, packed sequences.
+ * Query i of sequence b (tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1) attends
+ * to its sequence's tokens max(0, i - window + 1) .. i (window 0: from 0).  q:
+ * n_q_heads, k and v: n_kv_heads rows per token (post-RoPE, rows on 16 bytes);
+ * out: device [n_tokens, n_q_heads, head_dim] of `dtype` (BF16 or F16),
+ * 16-byte aligned.  Offsets out of order or range are clamped.  head_dim 64 or
+ * 128, at most 64 query heads per KV head.  error: device int32 that gets
+ * KVK_DEVERR bits, or NULL.  Non-finite keys and values as above.
+ * Errors: INVALID_ARG, UNSUPPORTED. */
+kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_rows *v, int32_t n_tokens,
+                                int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                const int32_t *cu_seqlens, int32_t batch, float softmax_scale, int32_t window, void *out,
+                                int32_t *error, kvk_stream stream);
 
 const char *kvk_status_string(kvk_status s);
 const char *kvk_last_error(void);

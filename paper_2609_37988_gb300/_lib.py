@@ -21,7 +21,7 @@ STATUS_NAMES = {
 KIND_GQA, KIND_MLA = 0, 1
 AXIS_TOKEN, AXIS_CHANNEL = 0, 1
 QUANT_GROUPED, QUANT_SYMMETRIC = 0, 1
-DTYPE_F32, DTYPE_BF16 = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16 = 0, 1, 2
 
 
 class ModelDesc(ctypes.Structure):
@@ -36,6 +36,21 @@ class LayerCfg(ctypes.Structure):
         "scheme")]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64)]
+
+
+class PagedDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in (
+        "n_layers", "n_q_heads", "n_kv_heads", "head_dim", "page_size", "n_pages", "dtype")]
+
+
+class PagedBatch(ctypes.Structure):
+    _fields_ = [("cu_new", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_tokens", ctypes.c_int32)]
+
+
 class KVKError(RuntimeError):
     def __init__(self, status: int, message: str):
         self.status = status
@@ -47,6 +62,8 @@ _P = ctypes.c_void_p
 _I = ctypes.c_int32
 _F = ctypes.c_float
 _SZ = ctypes.c_size_t
+_R = ctypes.POINTER(Rows)
+_PB = ctypes.POINTER(PagedBatch)
 
 # name -> argument types (all return kvk_status unless listed in _RET)
 _SIGS = {
@@ -82,6 +99,19 @@ _SIGS = {
                       ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_double)],
     "kvk_export_layer": [_P, _I, _P, _P, _P, _P, _P, _P, _P, _P],
     "kvk_get_device_error": [_P, _P, ctypes.POINTER(_I)],
+    "kvk_rotary_create": [_I, _I, _I, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_I), _I, _F,
+                          ctypes.POINTER(_P)],
+    "kvk_rotary_destroy": [_P],
+    "kvk_rotary_apply": [_P, _R, _R, _I, _R, _R, _I, _I, _I, _P, _P],
+    "kvk_paged_plan": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)],
+    "kvk_paged_create": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_P), ctypes.POINTER(_P), _P, _SZ,
+                         ctypes.POINTER(_P)],
+    "kvk_paged_destroy": [_P],
+    "kvk_paged_reset": [_P, _P],
+    "kvk_paged_append": [_P, _I, _PB, _R, _R, _P, _P, _R, _R, _P],
+    "kvk_paged_attention": [_P, _I, _PB, _R, _F, _I, _I, _P, _P],
+    "kvk_paged_get_device_error": [_P, _P, ctypes.POINTER(_I)],
+    "kvk_prompt_attention": [_R, _R, _R, _I, _I, _I, _I, _I, _P, _I, _F, _I, _P, _P, _P],
     "kvk_status_string": [_I],
     "kvk_last_error": [],
     "kvk_version": [],

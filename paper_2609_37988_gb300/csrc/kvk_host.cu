@@ -1137,7 +1137,11 @@ static kvk_status gqa_decode_common(kvk_cache *c, int32_t layer, const void *q, 
 
 }  // extern "C"
 
-// Records a failed CUDA call as the thread's last error (for noalloc.cu).
+// Records a failure as the thread's last error (for serve_host.cu).
+kvk_status kvk_internal_fail(kvk_status s, const char *message) { return fail(s, "%s", message); }
+
+// Records a failed CUDA call as the thread's last error (for noalloc.cu and
+// serve_host.cu).
 kvk_status kvk_internal_cuda_error(cudaError_t e, const char *what) { return cuda_fail(e, what); }
 
 // INVALID_ARG unless the calling thread's current device is the one the cache

@@ -1,0 +1,65 @@
+// serve.h -- arguments of the serving kernels (rotary positions, paged cache,
+// attention over packed prompts) and their launchers.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+namespace kvk {
+
+constexpr int kSrvF32 = 0, kSrvBf16 = 1, kSrvF16 = 2;  // KVK_DTYPE_*
+constexpr int kRotMaxFreq = 128;
+
+// Rotation frequencies: step[i] = inv_freq[i] / (2 pi) of a turn as a 64-bit
+// binary fraction, axis[i] the axis whose position it turns with.
+struct RotTable {
+  uint64_t step[kRotMaxFreq];
+  uint8_t axis[kRotMaxFreq];
+  float factor;
+  int n_freq, n_axes, adjacent;
+};
+
+// [tokens, heads, head_dim] rows; strides in elements, channels contiguous
+struct Rows {
+  uint8_t *p;
+  int64_t ts, hs;
+};
+
+// The pages of one layer and the batch that a call works on.
+struct PagedView {
+  uint8_t *k, *v;         // [n_pages, Hkv, page, D]
+  const int32_t *cu;      // [B + 1] offsets of the new tokens
+  const int32_t *lens;    // [B] positions held, the new tokens' included
+  const int32_t *table;   // [B, max_pages]
+  int B, max_pages, n_pages, page_shift, Hkv, D, n_tokens;
+  int32_t *err;
+};
+
+struct RotArgs {
+  RotTable t;
+  Rows q, k, v, qo, ko;   // k and v go to the pages where pv.k is set
+  int Hq, Hk, Hv, D, n_tokens;
+  const int32_t *pos;     // [n_axes, n_tokens]; null: positions in the sequence
+  PagedView pv;
+};
+cudaError_t launch_rotary(const RotArgs &a, int dtype, cudaStream_t st);
+
+// Attention of packed queries over pages (pv.k set) or over packed keys and
+// values (k, v), causal, each query seeing at most `window` positions.
+struct AttnArgs {
+  PagedView pv;
+  Rows q, k, v;
+  void *out;              // [n_tokens, Hq, D]
+  int Hq, G, window, max_new;
+  float sig_log2;
+  float *part;            // partial results, kPartSlots of rows_part() floats
+  int32_t *counter;       // zero between calls
+  int sms;
+};
+cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
+// CTAs that a split launch may use at most, and the partial slots of each
+constexpr int kRowsMaxCtas = 512;
+constexpr int kRowsPerUnit = 16;
+// floats of one partial: rows of D sums, then maxima, then totals
+__host__ __device__ constexpr int rows_part(int D) { return kRowsPerUnit * (D + 2); }
+
+}  // namespace kvk

@@ -1,0 +1,582 @@
+"""Serving operators on the GPU against the float64 oracle: rotary positions,
+the paged cache's append and attention, attention over whole prompts, and a run
+of them together.  Every tolerance is oracle.serving.attend_bound's (or, for
+the rotary, the bound beside it), derived from the roundings each path makes."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving as osv
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+U = {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}
+# half the last step below the type's normal range, relative to a row's largest weight
+SMALL = {BF16: 0.0, F16: 2.0 ** -25}
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def offsets(news):
+    return ints(np.concatenate([[0], np.cumsum(news)]).tolist())
+
+
+def randn(g, shape, dtype=F32):
+    return torch.randn(shape, generator=g).to(dtype).cuda()
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def close(got, ref, tol, what=""):
+    got = f64(got) if isinstance(got, torch.Tensor) else got
+    assert got.shape == ref.shape
+    assert np.isfinite(got).all(), f"{what}: non-finite output"
+    over = np.abs(got - ref) - tol
+    assert (over <= 0).all(), f"{what}: {np.abs(got - ref).max():.3e} off, {over.max():.3e} over at {np.unravel_index(over.argmax(), over.shape)}"
+
+
+# -- rotary ------------------------------------------------------------------------
+def rotary_bound(x, ref, inv_freq, pos, dtype, factor, adjacent, n):
+    """Rounded once (u); before it each product and sum in binary32 on cos and
+    sin within 2^-22 (their own 2 ulp, the turn's 2^-25 as a float, 2^-32 of a
+    turn cut off), and the angle's own share of the position times half a step of
+    the double that holds the frequency."""
+    mag = np.abs(np.asarray(x)).copy()
+    a = np.arange(n) * (2 if adjacent else 1)
+    b = a + (1 if adjacent else n)
+    both = mag[..., a] + mag[..., b]
+    far = np.abs(np.asarray(pos, np.float64)).max(0)[:, None, None] * np.max(np.abs(inv_freq)) * 2.0 ** -51
+    e = (2.0 ** -21 + far) * both * abs(factor)
+    extra = np.zeros_like(mag)
+    extra[..., a], extra[..., b] = e, e
+    return U[dtype] * np.abs(ref) + extra * (1 + U[dtype]) + (2.0 ** -25 if dtype == F16 else 0.0)
+
+
+def rotary_case(dtype, head_dim, rotary_dim, axes, adjacent, n_tokens, hq, hk, pos_hi, seed=0, factor=1.0, stride="fused",
+                inplace=False):
+    from paper_2609_37988_gb300.serving import Rotary
+    g = gen(seed)
+    n = rotary_dim // 2
+    axis = [int(a) for a in torch.randint(0, axes, (n,), generator=g)]
+    axis[-1] = axes - 1
+    rot = Rotary(head_dim=head_dim, rotary_dim=rotary_dim, base=10000.0, axes=axis, adjacent=adjacent, factor=factor)
+    inv_freq = [10000.0 ** (-2.0 * i / rotary_dim) for i in range(n)]
+    pos = torch.randint(-pos_hi // 8, pos_hi, (axes, n_tokens), generator=g, dtype=torch.int32)
+    extra = {"fused": 1, "odd": 0}[stride]
+    if stride == "odd":  # rows that start on no 16-byte boundary
+        flat = randn(g, (n_tokens * (hq + hk) * (head_dim + 1) + 1,), dtype)[1:]
+        qkv = flat.view(n_tokens, hq + hk, head_dim + 1)[..., :head_dim]
+    else:
+        qkv = randn(g, (n_tokens, hq + hk + extra, head_dim), dtype)
+    q, k = qkv[:, :hq], qkv[:, hq:hq + hk]
+    x = f64(qkv)
+    out = (q, k) if inplace else None
+    oq, ok = rot.apply(q if hq else None, k if hk else None, pos.cuda(), out=out if hq and hk else None)
+    for got, lo, h in ((oq, 0, hq), (ok, hq, hk)):
+        if not h:
+            assert got is None
+            continue
+        xs = x[:, lo:lo + h]
+        ref = osv.rotary(xs, pos.numpy(), inv_freq, axis, adjacent, factor)
+        close(got, ref, rotary_bound(xs, ref, inv_freq, pos.numpy(), dtype, factor, adjacent, n))
+    if inplace and extra:  # the value head beside them is as it was
+        np.testing.assert_array_equal(f64(qkv)[:, hq + hk:], x[:, hq + hk:])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F32])
+@pytest.mark.parametrize("adjacent", [False, True])
+@pytest.mark.parametrize("head_dim,rotary_dim,axes", [(128, 128, 1), (128, 128, 3), (64, 64, 2), (128, 64, 3), (256, 256, 1),
+                                                      (80, 80, 3), (96, 24, 2), (2, 2, 1), (64, 6, 8)])
+def test_rotary(dtype, adjacent, head_dim, rotary_dim, axes):
+    rotary_case(dtype, head_dim, rotary_dim, min(axes, rotary_dim // 2), adjacent, 7, 5, 2, 4096)
+
+
+@pytest.mark.parametrize("stride,inplace", [("fused", True), ("odd", False), ("odd", True)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rotary_strides_and_in_place(dtype, stride, inplace):
+    rotary_case(dtype, 128, 128, 3, False, 9, 4, 2, 100000, stride=stride, inplace=inplace, factor=1.1)
+    rotary_case(dtype, 64, 32, 1, True, 9, 4, 2, 100000, stride=stride, inplace=inplace)
+
+
+@pytest.mark.parametrize("tokens,hq,hk", [(1, 28, 4), (1, 1, 0), (3, 0, 2), (4099, 2, 1), (5, 64, 8)])
+def test_rotary_sizes_and_far_positions(tokens, hq, hk):
+    rotary_case(F32, 64, 64, 2, False, tokens, hq, hk, 2 ** 30, seed=3)
+    rotary_case(BF16, 128, 128, 1, False, tokens, hq, hk, 2 ** 24, seed=4)
+
+
+def test_rotary_empty():
+    from paper_2609_37988_gb300.serving import Rotary
+    rot = Rotary(head_dim=64)
+    q, k = rot.apply(torch.empty((0, 4, 64), device="cuda"), None, ints([]).view(1, 0))
+    assert q.shape == (0, 4, 64) and k is None
+
+
+# -- batches over pages --------------------------------------------------------------
+class Batch:
+    """A batch over pages: pools full of NaN, sequences' pages in random order,
+    the table's unused entries far outside the pool."""
+
+    def __init__(self, news, lens, hq, hkv, d, dtype, page, seed=0, spare=3, slack=1, rows_behind=0):
+        from paper_2609_37988_gb300.serving import PagedCache
+        g = gen(seed)
+        self.news, self.lens, self.page, self.dtype = news, lens, page, dtype
+        self.hq, self.hkv, self.d = hq, hkv, d
+        per = [(max(l, 0) + page - 1) // page for l in lens]
+        n_pages = sum(per) + spare
+        order = torch.randperm(n_pages, generator=g).tolist()
+        width = max(per + [0]) + slack
+        self.table = np.full((len(lens), width), 2 ** 30, np.int64)
+        for b, m in enumerate(per):
+            self.table[b, :m] = [order.pop() for _ in range(m)]
+        pools = [torch.full((n_pages, hkv, page, d), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
+        self.cache = PagedCache(n_q_heads=hq, k_pages=pools[:1], v_pages=pools[1:])
+        self.cu, self.lengths, self.table_d = offsets(news), ints(lens), ints(self.table.tolist())
+        # every position's keys and values, the new tokens' too
+        self.k = [torch.randn((max(l, 0), hkv, d), generator=g).to(dtype) for l in lens]
+        self.v = [torch.randn((max(l, 0), hkv, d), generator=g).to(dtype) for l in lens]
+        self.n = sum(news) + rows_behind
+        self.q = torch.randn((self.n, hq, d), generator=g).to(dtype)
+
+    def fill(self):
+        """All positions through the append, as if all were new."""
+        ls = [max(l, 0) for l in self.lens]
+        if sum(ls):
+            k, v = torch.cat(self.k).cuda(), torch.cat(self.v).cuda()
+            self.cache.append(0, k, v, offsets(ls), ints(ls), self.table_d)
+        return self
+
+    def expected(self, scale, window, t_max=None):
+        out, tol, at = [], [], 0
+        for b, (n, l) in enumerate(zip(self.news, self.lens)):
+            k, v = (np.transpose(f64(x[b]), (1, 0, 2)) for x in (self.k, self.v))
+            if l < n:  # queries before position 0
+                k, v = (np.zeros((self.hkv, max(l, 0), self.d)) if not l > 0 else x for x in (k, v))
+            r = osv.attend(f64(self.q[at:at + n]), k, v, scale, window)
+            if l < 0:
+                r = tuple(np.zeros_like(x) for x in r)
+            out.append(r[0])
+            tol.append(osv.attend_bound(*r, self.d, max(l, 1), U[self.dtype], SMALL[self.dtype]))
+            at += n
+        return np.concatenate(out), np.concatenate(tol)
+
+    def attend(self, scale, window=0, max_new=None, q=None, **kw):
+        return self.cache.attend(0, self.q.cuda() if q is None else q, self.cu, self.lengths, self.table_d, scale,
+                                 window=window, max_new=max(self.news + [1]) if max_new is None else max_new, **kw)
+
+    def check(self, window=0, max_new=None):
+        scale = 1.0 / math.sqrt(self.d)
+        got = self.attend(scale, window, max_new)
+        ref, tol = self.expected(scale, window)
+        close(got[: sum(self.news)], ref, tol, f"window {window}, max_new {max_new}")
+        assert self.cache.device_error() == 0
+        return got
+
+
+HEADS = [(40, 8, 128), (28, 4, 128), (8, 2, 64), (4, 4, 64), (16, 1, 128), (6, 2, 128), (48, 1, 64)]
+
+
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("dtype,page", [(BF16, 16), (F16, 32), (BF16, 64), (F16, 128)])
+def test_single_tokens(hq, hkv, d, dtype, page):
+    b = Batch([1] * 7, [1, 2, 63, 64, 65, 300, 17], hq, hkv, d, dtype, page).fill()
+    for window in (0, 1, 50):
+        b.check(window)
+
+
+@pytest.mark.parametrize("news,lens", [([5, 1, 3, 0, 2], [5, 1, 130, 77, 66]), ([9, 4], [700, 4]), ([1], [2100]), ([3, 1], [1, 0]),
+                                       ([2, 0, 0, 6], [513, 0, 9, 64])])
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(40, 8, 128, BF16, 16), (28, 4, 128, F16, 64), (8, 2, 64, BF16, 128)])
+def test_few_tokens(news, lens, hq, hkv, d, dtype, page):
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=5).fill()
+    for window in (0, 1, 7, 100):
+        b.check(window)
+    b.check(0, max_new=sum(news))
+
+
+CHUNKS = [([70, 33], [70, 500]), ([129, 1, 64, 0, 127], [129, 1, 200, 5, 383]), ([260], [260]), ([31, 300], [1000, 301]),
+          ([50, 50], [20, 50])]
+
+
+@pytest.mark.parametrize("news,lens", CHUNKS)
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 128, BF16, 16), (7, 1, 128, F16, 32), (8, 2, 64, BF16, 64), (3, 3, 64, F16, 16),
+                                                 (8, 1, 128, BF16, 128)])
+def test_chunks(news, lens, hq, hkv, d, dtype, page):
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=6).fill()
+    for window in (0, 40, 129):
+        b.check(window)
+
+
+def test_rows_in_no_sequence_stay():
+    b = Batch([3, 2], [70, 9], 8, 2, 64, BF16, 16, rows_behind=4).fill()
+    out = torch.full((b.n, 8, 64), 7.0, dtype=BF16, device="cuda")
+    b.attend(0.125, out=out)
+    assert (out[5:] == 7.0).all() and not (out[:5] == 7.0).all()
+    out2 = torch.full((b.n, 8, 64), 7.0, dtype=BF16, device="cuda")
+    b.attend(0.125, out=out2, max_new=b.n)
+    assert (out2[5:] == 7.0).all() and not (out2[:5] == 7.0).all()
+
+
+@pytest.mark.parametrize("news", [[1, 1], [3, 2], [80, 150]])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_are_not_finite_reach_only_rows_that_see_them(news, bad):
+    """In keys and values, at a position of the last tile and of an earlier one."""
+    lens = [200, 190]
+    b = Batch(news, lens, 10, 2, 128, BF16, 16, seed=8)
+    places = [(0, lens[0] - 1, 3), (1, lens[1] - 2, 77), (1, lens[1] - news[1] // 2 - 1, 5)]
+    for s, t, ch in places:
+        b.v[s][t, 1, ch] = bad
+    b.k[1][lens[1] - 1, 0, 9] = float("nan")
+    b.fill()
+    for window in (0, 60):
+        scale = 1.0 / math.sqrt(128)
+        got = f64(b.attend(scale, window)[: sum(news)])
+        ref, tol = b.expected(scale, window)
+        fine = np.isfinite(ref)
+        assert (np.isfinite(got) == fine).all()
+        assert (np.abs(got - ref)[fine] <= tol[fine]).all()
+
+
+def test_an_infinite_score_is_not_a_number():
+    b = Batch([1], [70], 4, 2, 64, BF16, 16, seed=9)
+    b.k[0][33, 0, :] = 3e38
+    b.q[0, 0, :] = 3e38
+    b.fill()
+    got = f64(b.attend(0.125))
+    assert np.isnan(got[0, 0]).all() and np.isfinite(got[0, 2:]).all()
+
+
+def test_large_scores_and_equal_rows():
+    """Scores far apart (one key takes all), far below zero, and all equal."""
+    b = Batch([2, 90], [150, 300], 10, 2, 128, F16, 16, seed=10)
+    for s in range(2):
+        b.k[s] *= 8
+    b.q *= 4
+    b.k[1][:] = b.k[1][:1]
+    b.fill().check()
+    b.check(33)
+
+
+def test_pages_shared_between_sequences():
+    b = Batch([1, 1, 1], [100, 100, 40], 8, 2, 64, BF16, 16, seed=11)
+    b.table[1, :5] = b.table[0, :5]
+    b.table_d = ints(b.table.tolist())
+    b.k[1][:80], b.v[1][:80] = b.k[0][:80], b.v[0][:80]
+    b.fill().check()
+
+
+def test_strided_queries_and_repeated_calls_agree_to_the_bit():
+    b = Batch([4, 1, 100], [3000, 1000, 700], 28, 4, 128, BF16, 32, seed=12).fill()
+    wide = torch.zeros((b.n, 40, 128), dtype=BF16, device="cuda")
+    wide[:, 5:33] = b.q.cuda()
+    a = b.attend(0.088, q=wide[:, 5:33])
+    for max_new in (None, b.n):
+        first = b.attend(0.088, max_new=max_new)
+        for _ in range(5):
+            assert torch.equal(first, b.attend(0.088, max_new=max_new))
+    assert torch.equal(a, b.attend(0.088))
+    perm = b.q.cuda().permute(1, 0, 2).contiguous().permute(1, 0, 2)  # heads outermost
+    assert torch.equal(a, b.attend(0.088, q=perm))
+
+
+def test_device_errors_and_recovery():
+    b = Batch([1, 2], [80, 90], 8, 2, 64, BF16, 16, seed=13, slack=0).fill()
+    keep = b.attend(0.125)
+    bad = b.table_d.clone()
+    bad[0, 2] = 10 ** 6
+    b.cache.attend(0, b.q.cuda(), b.cu, b.lengths, bad, 0.125, max_new=2)
+    assert b.cache.device_error() == 32
+    bad[0, 2] = -5
+    b.cache.attend(0, b.q.cuda(), b.cu, b.lengths, bad, 0.125)
+    assert b.cache.device_error() == 32
+    # more new tokens than said; more positions than the table holds
+    b.attend(0.125, max_new=1)
+    assert b.cache.device_error() == 4
+    b.cache.attend(0, b.q.cuda(), b.cu, ints([80, 10 ** 6]), b.table_d, 0.125, max_new=2)
+    assert b.cache.device_error() == 4
+    k = torch.zeros((3, 2, 64), dtype=BF16, device="cuda")
+    b.cache.append(0, k, k, b.cu, ints([80, 10 ** 6]), b.table_d)
+    assert b.cache.device_error() == 2
+    b.cache.append(0, k, k, b.cu, ints([49, 90]), torch.full_like(b.table_d, 10 ** 6))
+    assert b.cache.device_error() == 32
+    b.fill()
+    assert torch.equal(keep, b.attend(0.125)) and b.cache.device_error() == 0
+
+
+def test_empty_batches():
+    b = Batch([0, 0], [0, 40], 8, 2, 64, BF16, 16).fill()
+    assert b.attend(0.125).shape == (0, 8, 64)
+    q = torch.full((3, 8, 64), 5.0, dtype=BF16, device="cuda")
+    out = b.attend(0.125, q=q, out=q.clone(), max_new=3)
+    assert (out == 5.0).all()
+    none = torch.zeros((0,), dtype=torch.int32, device="cuda")
+    b.cache.attend(0, q, ints([0]), none, torch.zeros((0, 3), dtype=torch.int32, device="cuda"), 0.125)
+    assert b.cache.device_error() == 0
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1, 1], [500, 2, 77]), ([64, 200], [64, 900])])
+def test_captured_and_replayed_on_another_stream(news, lens):
+    b = Batch(news, lens, 10, 2, 128, BF16, 16, seed=14).fill()
+    scale = 1.0 / math.sqrt(128)
+    keep = b.attend(scale)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    q, out = b.q.cuda(), torch.empty_like(keep)
+    b.attend(scale, q=q, out=out, stream=side)
+    side.synchronize()
+    assert torch.equal(keep, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        b.attend(scale, q=q, out=out)
+        b.attend(scale, q=q, out=out)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(keep, out)
+    # the lengths are read when the graph runs
+    b.lengths.copy_(ints([max(n, l - 1) for n, l in zip(news, lens)]))
+    graph.replay()
+    torch.cuda.synchronize()
+    b.lens = [max(n, l - 1) for n, l in zip(news, lens)]
+    b.k = [x[:l] for x, l in zip(b.k, b.lens)]
+    b.v = [x[:l] for x, l in zip(b.v, b.lens)]
+    ref, tol = b.expected(scale, 0)
+    close(out, ref, tol)
+
+
+# -- append ----------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,page,hq,hkv,d", [(BF16, 16, 10, 2, 128), (F16, 64, 8, 2, 64), (BF16, 128, 3, 3, 64), (F16, 32, 28, 4, 128)])
+@pytest.mark.parametrize("mode", ["plain", "rotary", "own positions", "odd strides"])
+def test_append(dtype, page, hq, hkv, d, mode):
+    from paper_2609_37988_gb300.serving import Rotary
+    news, lens = [3, 0, 1, 40, 6], [3, 5, 129, 200, 4]
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=15, rows_behind=2)
+    n = b.n
+    g = gen(16)
+    if mode == "odd strides":
+        flat = randn(g, (n * (hq + 2 * hkv) * (d + 1) + 1,), dtype)[1:]
+        qkv = flat.view(n, hq + 2 * hkv, d + 1)[..., :d]
+    else:
+        qkv = randn(g, (n, hq + 2 * hkv, d), dtype)
+    q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+    sections = [d // 2] if mode == "own positions" else [d // 8, d // 8, d // 4]
+    axis = [a for a, m in enumerate(sections) for _ in range(m)]
+    rot = Rotary(head_dim=d, base=1e6, sections=sections)
+    inv_freq = [1e6 ** (-2.0 * i / d) for i in range(d // 2)]
+    pos = torch.randint(0, 50000, (3, n), generator=g, dtype=torch.int32)
+    own = np.concatenate([np.arange(l - m, l) for m, l in zip(news, lens)] + [np.zeros(2)])[None]
+    before = [f64(t) for t in (b.cache.k_pages[0], b.cache.v_pages[0])]
+    kw = {} if mode == "plain" else dict(rotary=rot, positions=None if mode == "own positions" else pos.cuda(), q=q)
+    q_out = torch.full((n, hq, d), 7.0, dtype=dtype, device="cuda")
+    got = b.cache.append(0, k, v, b.cu, b.lengths, b.table_d, q_out=q_out if kw else None, **kw)
+    assert b.cache.device_error() == 0
+    rk, tol_k = f64(k), np.zeros((n, hkv, d))
+    if kw:
+        p = own if mode == "own positions" else pos.numpy()
+        rk = osv.rotary(f64(k), p, inv_freq, axis)
+        tol_k = rotary_bound(f64(k), rk, inv_freq, p, dtype, 1.0, False, d // 2)
+        ref = osv.rotary(f64(q), p, inv_freq, axis)
+        m = sum(news)
+        close(got[:m], ref[:m], rotary_bound(f64(q), ref, inv_freq, p, dtype, 1.0, False, d // 2)[:m])
+        assert (got[m:] == 7.0).all()
+    else:
+        assert got is None
+    after = [f64(t) for t in (b.cache.k_pages[0], b.cache.v_pages[0])]
+    at = 0
+    for s, (m, l) in enumerate(zip(news, lens)):
+        for j in range(m):
+            t = l - m + j
+            if t >= 0:
+                pg, sl = osv.place(t, b.table[s], page)
+                close(after[0][pg, :, sl], rk[at + j], tol_k[at + j])
+                np.testing.assert_array_equal(after[1][pg, :, sl], f64(v)[at + j])
+                for x in (0, 1):
+                    before[x][pg, :, sl] = after[x][pg, :, sl]
+        at += m
+    for x in (0, 1):  # nothing else was written
+        np.testing.assert_array_equal(before[x], after[x])
+
+
+def test_append_rotates_queries_in_place():
+    from paper_2609_37988_gb300.serving import Rotary
+    b = Batch([5, 4000], [5, 4000], 4, 2, 64, BF16, 16, seed=17)
+    rot = Rotary(head_dim=64)
+    k, v, q = (randn(gen(18), (4005, h, 64), BF16) for h in (2, 2, 4))
+    a = b.cache.append(0, k, v, b.cu, b.lengths, b.table_d, rotary=rot, q=q)
+    pos = torch.cat([torch.arange(5), torch.arange(4000)]).to(torch.int32).cuda()
+    c, d = rot.apply(q, k, pos)
+    assert torch.equal(a, c)
+    same = b.cache.append(0, k, v, b.cu, b.lengths, b.table_d, rotary=rot, q=q, q_out=q)
+    assert same is q and torch.equal(a, q)
+    b2 = Batch([5, 4000], [5, 4000], 4, 2, 64, BF16, 16, seed=17)
+    b2.cache.append(0, d, v, b2.cu, b2.lengths, b2.table_d)
+    for x, y in ((b.cache.k_pages[0], b2.cache.k_pages[0]), (b.cache.v_pages[0], b2.cache.v_pages[0])):
+        assert torch.equal(x.nan_to_num(3.0), y.nan_to_num(3.0))
+
+
+# -- prompts -----------------------------------------------------------------------------
+def prompt_case(lens, hq, hkv, d, dtype, windows=(0,), seed=0, behind=0, first=0, mul=1.0, strided=False):
+    from paper_2609_37988_gb300.serving import prompt_attention
+    g = gen(seed)
+    n = first + sum(lens) + behind
+    if strided:
+        qkv = randn(g, (n, hq + 2 * hkv + 1, d), dtype)
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:hq + 2 * hkv]
+    else:
+        q, k, v = (randn(g, (n, h, d), F32) for h in (hq, hkv, hkv))
+        q, k, v = (q * mul).to(dtype), (k * mul).to(dtype), v.to(dtype)
+    cu = ints((first + np.concatenate([[0], np.cumsum(lens)])).tolist())
+    error = ints([0])
+    scale = 1.0 / math.sqrt(d)
+    for window in windows:
+        out = torch.full((n, hq, d), 7.0, dtype=dtype, device="cuda")
+        got = prompt_attention(q, k, v, cu, scale, window=window, out=out, error=error)
+        at = first
+        for m in lens:
+            r = osv.attend(f64(q[at:at + m]), *(np.transpose(f64(x[at:at + m]), (1, 0, 2)) for x in (k, v)), scale, window)
+            close(got[at:at + m], r[0], osv.attend_bound(*r, d, max(m, 1), U[dtype], SMALL[dtype]), f"length {m}, window {window}")
+            at += m
+        assert (got[:first] == 7.0).all() and (got[at:] == 7.0).all()
+        assert int(error) == 0
+
+
+@pytest.mark.parametrize("hq,hkv,d", HEADS)
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_prompts_of_every_head_layout(hq, hkv, d, dtype):
+    prompt_case([1, 0, 37, 2, 140], hq, hkv, d, dtype, windows=(0, 19), behind=3)
+
+
+@pytest.mark.parametrize("lens", [[1], [2], [25, 26], [51, 52, 53], [127, 128, 129], [255, 256, 257], [385], [0, 0, 64, 0]])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(5, 1, 128, BF16), (2, 1, 64, F16), (1, 1, 128, F16)])
+def test_prompt_lengths(lens, hq, hkv, d, dtype):
+    prompt_case(lens, hq, hkv, d, dtype, windows=(0, 1, 64, 100, 1000), seed=21, first=2)
+
+
+@pytest.mark.parametrize("mul", [0.05, 4.0])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_prompt_score_ranges(mul, dtype):
+    prompt_case([300, 90], 4, 2, 128, dtype, seed=22, mul=mul)
+
+
+def test_prompt_strides():
+    prompt_case([130, 5, 260], 10, 2, 128, BF16, windows=(0, 70), seed=23, strided=True)
+    prompt_case([130, 5, 260], 8, 2, 64, F16, seed=24, strided=True)
+
+
+def test_prompts_many_sequences():
+    rng = np.random.default_rng(25)
+    prompt_case([int(x) for x in rng.integers(0, 40, 90)], 4, 2, 64, BF16, seed=25)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("-inf")])
+def test_prompt_values_that_are_not_finite(bad):
+    from paper_2609_37988_gb300.serving import prompt_attention
+    g = gen(26)
+    lens, hq, hkv, d = [300, 170], 5, 1, 128
+    q, k, v = (randn(g, (470, h, d), BF16) for h in (hq, hkv, hkv))
+    for t, ch in ((120, 0), (299, 64), (303, 127), (469, 3)):
+        v[t, 0, ch] = bad
+    k[140, 0, 3] = float("nan")
+    for window in (0, 90):
+        got = f64(prompt_attention(q, k, v, offsets(lens), 0.088, window=window))
+        at = 0
+        for m in lens:
+            r = osv.attend(f64(q[at:at + m]), *(np.transpose(f64(x[at:at + m]), (1, 0, 2)) for x in (k, v)), 0.088, window)
+            fine = np.isfinite(r[0])
+            x = got[at:at + m]
+            assert (np.isfinite(x) == fine).all(), (m, window)
+            tol = osv.attend_bound(*r, d, m, U[BF16], 0.0)
+            assert (np.abs(x - r[0])[fine] <= tol[fine]).all()
+            at += m
+
+
+def test_prompt_captured_and_repeated():
+    from paper_2609_37988_gb300.serving import prompt_attention
+    g = gen(27)
+    lens = [700, 33, 260]
+    q, k, v = (randn(g, (993, h, 128), BF16) for h in (10, 2, 2))
+    cu = offsets(lens)
+    keep = prompt_attention(q, k, v, cu, 0.088)
+    for _ in range(5):
+        assert torch.equal(keep, prompt_attention(q, k, v, cu, 0.088))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out = prompt_attention(q, k, v, cu, 0.088, stream=side)
+    side.synchronize()
+    assert torch.equal(keep, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        a = prompt_attention(q, k, v, cu, 0.088)
+        c = prompt_attention(q, k, v, cu, 0.088)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(keep, a) and torch.equal(keep, c)
+
+
+def test_prompt_offsets_out_of_order_are_clamped():
+    from paper_2609_37988_gb300.serving import prompt_attention
+    q, k, v = (randn(gen(28), (50, h, 64), BF16) for h in (2, 1, 1))
+    out = torch.full((50, 2, 64), 7.0, dtype=BF16, device="cuda")
+    prompt_attention(q, k, v, ints([0, 20, 10, 10 ** 6, -3]), 0.125, out=out)
+    torch.cuda.synchronize()
+    assert torch.isfinite(out).all()
+
+
+# -- together ------------------------------------------------------------------------------
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 128, BF16, 16), (8, 2, 64, F16, 64)])
+def test_prompts_then_chunks_then_steps(hq, hkv, d, dtype, page):
+    """Prompts attend to themselves and enter the pages, a chunk follows, then
+    single tokens: every output against the oracle over all positions so far,
+    and the prompt's own attention against the pages' attention of the same."""
+    from paper_2609_37988_gb300.serving import PagedCache, Rotary, prompt_attention
+    g = gen(30)
+    B, stages = 3, [[140, 7, 65], [30, 61, 1], [1, 1, 1], [1, 1, 1]]
+    total = [sum(s[b] for s in stages) for b in range(B)]
+    rot = Rotary(head_dim=d, base=1e6)
+    inv_freq = [1e6 ** (-2.0 * i / d) for i in range(d // 2)]
+    per = [(t + page - 1) // page for t in total]
+    order = torch.randperm(sum(per), generator=g).tolist()
+    table = np.zeros((B, max(per)), np.int64)
+    for b in range(B):
+        table[b, :per[b]] = [order.pop() for _ in range(per[b])]
+    cache = PagedCache(n_layers=2, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, n_pages=sum(per), page_size=page, dtype=dtype)
+    scale, held = 1.0 / math.sqrt(d), [0] * B
+    seen = [[np.zeros((0, hkv, d))] * 2 for _ in range(B)]
+    for i, news in enumerate(stages):
+        n = sum(news)
+        qkv = randn(g, (n, hq + 2 * hkv, d), dtype)
+        q, k, v = qkv[:, :hq], qkv[:, hq:hq + hkv], qkv[:, hq + hkv:]
+        held = [h + m for h, m in zip(held, news)]
+        cu, lengths, tab = offsets(news), ints(held), ints(table.tolist())
+        qr = cache.append(1, k, v, cu, lengths, tab, rotary=rot, q=q)
+        pos = ints(np.concatenate([np.arange(h - m, h) for m, h in zip(news, held)]).tolist())
+        q2, k2 = rot.apply(q, k, pos)
+        assert torch.equal(qr, q2)
+        out = cache.attend(1, qr, cu, lengths, tab, scale, max_new=max(news))
+        if i == 0:
+            own = prompt_attention(q2, k2, v, cu, scale)
+        at = 0
+        for b, m in enumerate(news):
+            rows = slice(at, at + m)
+            seen[b] = [np.concatenate([a, f64(x[rows])]) for a, x in zip(seen[b], (k2, v))]
+            # the keys as the pages hold them
+            pool = f64(cache.k_pages[1])
+            np.testing.assert_array_equal(np.transpose(osv.from_pages(pool, table[b], held[b], page), (1, 0, 2)), seen[b][0])
+            r = osv.attend(f64(qr[rows]), *(np.transpose(a, (1, 0, 2)) for a in seen[b]), scale)
+            tol = osv.attend_bound(*r, d, held[b], U[dtype], SMALL[dtype])
+            close(out[rows], r[0], tol, f"stage {i}")
+            if i == 0:
+                close(own[rows], r[0], tol, "prompt")
+            at += m
+    assert cache.device_error() == 0
