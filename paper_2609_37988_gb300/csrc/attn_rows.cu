@@ -60,17 +60,12 @@ __device__ __forceinline__ void join(float &M, float &L, float4 &x, float m, flo
 struct Seq {
   int q0, n, len;  // first token, tokens, positions held
 };
-template <bool PAGED>
 __device__ __forceinline__ Seq load_seq(const PagedView &v, int b, int max_new) {
   Seq s;
   const int c0 = min(max(v.cu[b], 0), v.n_tokens);
   s.n = min(max(v.cu[b + 1], c0), v.n_tokens) - c0;
   s.q0 = c0;
-  if (!PAGED) {
-    s.len = s.n;
-    return s;
-  }
-  s.len = v.lens[b];
+  s.len = max(v.lens[b], 0);
   const int64_t cap = (int64_t)v.max_pages << v.page_shift;
   if (s.n > max_new || s.len > cap) {
     set_err(v.err, kErrCount);
@@ -88,11 +83,7 @@ __device__ __forceinline__ void block_range(const Seq &s, int G, int window, int
   nt = max(1, (last + kT - lo) / kT);
 }
 __device__ __forceinline__ int row_blocks(const Seq &s, int G) { return (s.n * G + kRowsPerUnit - 1) / kRowsPerUnit; }
-// What a sequence adds per KV head to the list that is cut into runs: its
-// tiles, or (without pages: no workspace to join pieces in) its units.
-template <bool PAGED>
 __device__ __forceinline__ int seq_tiles(const Seq &s, int G, int window) {
-  if (!PAGED) return row_blocks(s, G);
   int sum = 0;
   for (int rb = 0; rb < row_blocks(s, G); ++rb) {
     int lo, nt;
@@ -109,7 +100,7 @@ struct At {
   Seq s;
 };
 
-template <int D, bool BF16, bool PAGED>
+template <int D, bool BF16>
 __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   constexpr int RB = D * 2;            // bytes of a row
   constexpr int CH = RB / 16;          // 16-byte pieces of a row
@@ -128,7 +119,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   // the run of this CTA: tiles [w0, w1) of all
   if (warp == 0) {
     int64_t total = 0;
-    for (int b = lane; b < pv.B; b += 32) total += (int64_t)pv.Hkv * seq_tiles<PAGED>(load_seq<PAGED>(pv, b, a.max_new), a.G, a.window);
+    for (int b = lane; b < pv.B; b += 32) total += (int64_t)pv.Hkv * seq_tiles(load_seq(pv, b, a.max_new), a.G, a.window);
     for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
     const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
     const int64_t w0 = share * blockIdx.x;
@@ -137,7 +128,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
     if (w0 < total) {
       for (int b0 = 0; b0 < pv.B && found < 0; b0 += 32) {
         int64_t x = 0;
-        if (b0 + lane < pv.B) x = (int64_t)pv.Hkv * seq_tiles<PAGED>(load_seq<PAGED>(pv, b0 + lane, a.max_new), a.G, a.window);
+        if (b0 + lane < pv.B) x = (int64_t)pv.Hkv * seq_tiles(load_seq(pv, b0 + lane, a.max_new), a.G, a.window);
         int64_t sum = x;
         for (int o = 1; o < 32; o <<= 1) {
           const int64_t y = __shfl_up_sync(kAll, sum, o);
@@ -162,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   __syncthreads();
   const int64_t total = s_total;
   const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
-  int64_t w0 = share * blockIdx.x, w1 = min(total, w0 + share);
+  const int64_t w0 = share * blockIdx.x, w1 = min(total, w0 + share);
   if (w0 >= w1) {
     pdl_trigger();
     return;
@@ -177,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
         x.h = 0;
         do {
           if (++x.b >= pv.B) return;  // behind the last unit: not used again
-          x.s = load_seq<PAGED>(pv, x.b, a.max_new);
+          x.s = load_seq(pv, x.b, a.max_new);
         } while (x.s.n == 0);
       }
     }
@@ -186,29 +177,19 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   At at;
   {
     at.b = s_b;
-    at.s = load_seq<PAGED>(pv, at.b, a.max_new);
+    at.s = load_seq(pv, at.b, a.max_new);
     int64_t off = w0 - s_start;
-    const int per = seq_tiles<PAGED>(at.s, a.G, a.window);
+    const int per = seq_tiles(at.s, a.G, a.window);
     at.h = (int)(off / per);
     int r = (int)(off - (int64_t)at.h * per);
-    at.rb = PAGED ? 0 : r;
+    at.rb = 0;
     settle(at);
-    while (PAGED && r >= at.nt) {
+    while (r >= at.nt) {
       r -= at.nt;
       ++at.rb;
       settle(at);
     }
-    at.t = PAGED ? r : 0;
-    if (!PAGED) {  // from units to tiles
-      At x = at;
-      int64_t tiles = x.nt;
-      for (int64_t u = w0 + 1; u < w1; ++u) {
-        next_unit(x);
-        tiles += x.nt;
-      }
-      w0 = 0;
-      w1 = tiles;
-    }
+    at.t = r;
   }
 
   // copies: a thread moves piece cc of rows r0 + RS i
@@ -226,12 +207,6 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
       const int r = r0 + RS * i, t = t0 + r, pg = t >> pv.page_shift;
       bool ok = t < x.s.len;
       const int dst = r * RB + ((cc ^ (r & 7)) << 4);
-      if constexpr (!PAGED) {
-        const int64_t row = x.s.q0 + (ok ? t : 0);
-        cp_async16(ks + dst, a.k.p + 2 * (row * a.k.ts + x.h * a.k.hs) + 16 * cc, ok);
-        cp_async16(vs + dst, a.v.p + 2 * (row * a.v.ts + x.h * a.v.hs) + 16 * cc, ok);
-        continue;
-      }
       if (ok && pg != last) {
         const int page = tab[pg];
         last = pg;
@@ -512,36 +487,31 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   pdl_trigger();
 }
 
-template <int D, bool BF16, bool PAGED>
+template <int D, bool BF16>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   constexpr int smem = kStages * 2 * kT * D * 2 + 128;
   static std::atomic<bool> ready{false};
   if (!ready.load(std::memory_order_relaxed)) {
     const cudaError_t e =
-        cudaFuncSetAttribute(attn_rows_kernel<D, BF16, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        cudaFuncSetAttribute(attn_rows_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     ready.store(true, std::memory_order_relaxed);
   }
   // two CTAs per SM, no more of them than tiles that there can be
-  const int64_t cap = (PAGED ? (int64_t)a.pv.max_pages << a.pv.page_shift : a.pv.n_tokens) / kT + 2;
+  const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / kT + 2;
   const int64_t tiles = (int64_t)a.pv.B * a.pv.Hkv * ((a.max_new * a.G + kRowsPerUnit - 1) / kRowsPerUnit) * cap;
   const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), tiles);
-  return launch_pdl(attn_rows_kernel<D, BF16, PAGED>, dim3(grid), dim3(kThreads), smem, st, a);
+  return launch_pdl(attn_rows_kernel<D, BF16>, dim3(grid), dim3(kThreads), smem, st, a);
 }
 
 }  // namespace
-
-template <int D, bool BF16>
-static cudaError_t launch_src(const AttnArgs &a, cudaStream_t st) {
-  return a.pv.k ? launch_t<D, BF16, true>(a, st) : launch_t<D, BF16, false>(a, st);
-}
 
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st) {
   if (a.pv.B == 0 || a.pv.n_tokens == 0) return cudaSuccess;
   const bool bf = dtype == kSrvBf16;
   switch (a.pv.D) {
-    case 128: return bf ? launch_src<128, true>(a, st) : launch_src<128, false>(a, st);
-    case 64: return bf ? launch_src<64, true>(a, st) : launch_src<64, false>(a, st);
+    case 128: return bf ? launch_t<128, true>(a, st) : launch_t<128, false>(a, st);
+    case 64: return bf ? launch_t<64, true>(a, st) : launch_t<64, false>(a, st);
     default: return cudaErrorInvalidValue;
   }
 }

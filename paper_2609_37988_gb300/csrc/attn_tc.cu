@@ -1,0 +1,718 @@
+// attn_tc.cu -- causal attention of many packed queries on the 5th-generation
+// tensor cores: whole prompts over their own keys and values, and chunks of new
+// tokens over a paged cache.  Bound: the tensor pipe.
+//
+// Rows: token i of a sequence and head h of a KV head's group G are row
+// i G + h; a query tile is the rows of P = 128 / G whole tokens (at most 128
+// rows, TMEM lane = row), a job two such tiles of one (sequence, KV head).  Per
+// 128 positions of keys and values, for either tile: S = Q K^T (fp32 in TMEM),
+// then x = sigma log2(e) s; each row keeps a reference m that moves only when
+// a score rises more than 8 above it (then O and the row's sum are rescaled in
+// place; 6 for f16, whose weights are kept 2^8 larger so that small ones stay
+// normal); P = 2^(x - m) in the stored type overwrites S, and O += P V with P
+// the A operand from TMEM.  The two tiles take turns: while one's products run,
+// the other's softmax does.
+//
+// One persistent CTA per SM, 12 warps: two softmax warpgroups (a thread: a
+// row; they also write the tile's result), one thread that issues all products,
+// one warp that schedules jobs and issues the TMA copies (query tiles; a ring
+// of key and value tiles), two that look through the values of tiles which some
+// row does not see in full: weight 0 times a value that is not finite would be
+// NaN, so those enter as zeros, and a row that sees one gets NaN in that
+// channel when it is written.
+//
+// Jobs in order of their distance from their sequence's end, all sequences
+// side by side: the longest first where lengths are equal, the short ones last
+// in any case; dealt to the CTAs back and forth.
+#include <cuda.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "serve.h"
+#include "umma.cuh"
+
+namespace kvk {
+namespace {
+
+constexpr int kTcT = 128;                 // positions per tile, rows per query tile
+constexpr int kTcThreads = 384;
+constexpr int kBox = 128 * 128;           // 64 channels x 128 rows
+constexpr int kErrTimeout = 8, kErrCount = 4, kErrPage = 32;  // KVK_DEVERR_*
+constexpr uint32_t kAll = 0xffffffffu;
+constexpr uint32_t kWaits = 1u << 20;     // polls of up to 2 us each
+
+struct TcArgs {
+  CUtensorMap mq, mk, mv;
+  AttnArgs a;
+  int P;                                  // tokens of a query tile
+};
+
+struct Job {
+  int b, h, q0, n;      // sequence, KV head, its first token in the batch, its tokens
+  int p0, tok0;         // position of its token 0, the job's first token
+  int lo, nt;           // position of tile 0, tiles
+  int js[2], je[2];     // tiles that either query tile sees: [js, je)
+  int first, low;       // tiles in [low, first] positions are seen by every row
+  int two, bad;         // second query tile; values that are not finite
+};
+
+template <int D>
+struct Smem {
+  static constexpr int kTile = D / 64 * kBox;          // a query, key or value tile
+  static constexpr int kStages = D == 128 ? 5 : 8;
+  static constexpr int kQ = 0, kRing = 2 * kTile, kBar = kRing + kStages * kTile;
+  static constexpr int kBars = 3 * kStages + 17;
+  static constexpr int kJob = kBar + 8 * kBars;        // two jobs
+  static constexpr int kWords = kJob + 2 * (int)sizeof(Job);
+  static constexpr int kTotal = kWords + 16;
+  static constexpr int kBytes = kTotal + 1024;         // + alignment of the base
+};
+static_assert(Smem<128>::kBytes <= 232448 && Smem<64>::kBytes <= 232448, "shared memory");
+static_assert(Smem<64>::kBytes > 116 * 1024, "one CTA (holding all TMEM columns) per SM");
+
+__device__ __forceinline__ void tma3(void *dst, const CUtensorMap *m, int x, int y, int z, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ void tma4(void *dst, const CUtensorMap *m, int x, int y, int z, int w, uint64_t *bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+          smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
+      : "memory");
+}
+// 32 columns of this warp's lanes, not waited for
+__device__ __forceinline__ void tmem_ld32_nw(uint32_t taddr, float *v) {
+  uint32_t r[32];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+        "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+        "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(r[j]);
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+
+template <bool BF16>
+__device__ __forceinline__ bool pair_fine(uint32_t w) {
+  constexpr uint32_t m = BF16 ? 0x7F80u : 0x7C00u;
+  return (w & m) != m && (w >> 16 & m) != m;
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t pair_scrubbed(uint32_t w) {
+  constexpr uint32_t m = BF16 ? 0x7F80u : 0x7C00u;
+  if ((w & m) == m) w &= 0xFFFF0000u;
+  if ((w >> 16 & m) == m) w &= 0xFFFFu;
+  return w;
+}
+
+// Tokens of sequence b, its first one in the batch.
+__device__ __forceinline__ int seq_tokens(const PagedView &v, int b, int &q0) {
+  q0 = min(max(v.cu[b], 0), v.n_tokens);
+  return min(max(v.cu[b + 1], q0), v.n_tokens) - q0;
+}
+
+template <int D, bool BF16, bool PAGED>
+__global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_constant__ TcArgs t) {
+  using SM = Smem<D>;
+  constexpr int NS = SM::kStages;
+  extern __shared__ uint8_t tc_raw[];
+  uint8_t *sm = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
+  uint64_t *bar = reinterpret_cast<uint64_t *>(sm + SM::kBar);
+  // ring: full[NS] a tile landed, free[NS] its products done and the looking
+  // warps past it, vclean[NS] a partly seen value tile looked through (the
+  // looking warps pass every tile, so that no wait falls two phases behind, and
+  // a stage is not used again before its vclean was awaited).  qfull / qfree
+  // the job's query tiles; jfull[2] / jfree[2] the job's description (11
+  // readers); per query tile: sfull scores done, pfull[2] either half of the
+  // weights written (a warp each), odone value products done, ofree the result
+  // read.
+  uint64_t *full = bar, *free_ = bar + NS, *qfull = bar + 2 * NS, *qfree = qfull + 1, *jfull = qfree + 1, *jfree = jfull + 2,
+           *sfull = jfree + 2, *pfull = sfull + 2, *odone = pfull + 4, *ofree = odone + 2, *vclean = ofree + 2,
+           *drain = vclean + NS;
+  Job *jobs = reinterpret_cast<Job *>(sm + SM::kJob);
+  uint32_t *tbase = reinterpret_cast<uint32_t *>(sm + SM::kWords);
+  volatile int *abort_flag = reinterpret_cast<volatile int *>(sm + SM::kWords + 4);
+  const AttnArgs &a = t.a;
+  const PagedView &pv = a.pv;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int P = t.P, G = a.G;
+
+  if (tid == 0) {
+    for (int i = 0; i < SM::kBars; ++i) {
+      uint64_t *b = bar + i;
+      const int n = b >= jfree && b < jfree + 2 ? 11
+                    : (b >= pfull && b < pfull + 4) || (b >= ofree && b < ofree + 2) ? 4
+                    : b >= vclean && b < vclean + NS ? 2
+                    : b >= free_ && b < free_ + NS   ? 3
+                                                     : 1;
+      mbar_init(b, n);
+    }
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tbase)), "n"(512)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tbase;
+  const uint32_t tS = tmem, tO = tmem + 256;  // scores 2 x 128 columns, results 2 x D
+  pdl_wait();
+
+  auto wait = [&](uint64_t *b, uint32_t parity) {
+    if (mbar_wait_or_abort(b, parity, kWaits, abort_flag)) return true;
+    *abort_flag = 1;
+    return false;
+  };
+
+  if (warp == 9) {
+    // -- schedule and copies ---------------------------------------------------
+    auto blocks = [&](int b) {
+      int q0;
+      return (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P);
+    };
+    int total = 0, most = 0;
+    for (int b = lane; b < pv.B; b += 32) {
+      const int x = blocks(b);
+      total += x;
+      most = max(most, x);
+    }
+    total = (int)__reduce_add_sync(kAll, (unsigned)total);
+    most = (int)__reduce_max_sync(kAll, (unsigned)most);
+    // jobs at most `d` blocks from their sequence's end
+    auto upto = [&](int d) {
+      unsigned s = 0;
+      for (int b = lane; b < pv.B; b += 32) s += min(blocks(b), d);
+      return (int)__reduce_add_sync(kAll, s);
+    };
+    const int n_jobs = total * pv.Hkv, step = gridDim.x;
+    int s = 0;          // ring place and its round's parity
+    uint32_t ph = 0;
+    int loads = 0;      // query loads so far
+    // lane 0 waits, the warp goes on together
+    auto wait0 = [&](uint64_t *b, uint32_t parity) {
+      int ok = 1;
+      if (lane == 0) ok = wait(b, parity);
+      return __shfl_sync(kAll, ok, 0) != 0;
+    };
+    constexpr int NB = D / 64;
+    for (int k = 0;; ++k) {
+      const int idx = k * step + (k & 1 ? step - 1 - (int)blockIdx.x : (int)blockIdx.x);
+      Job j = {};
+      const bool go = idx < n_jobs;
+      if (go) {
+        const int r = idx / pv.Hkv;
+        j.h = idx - r * pv.Hkv;
+        int d0 = 0, d1 = most, f0 = 0;  // upto(d0) <= r < upto(d1)
+        while (d1 - d0 > 1) {
+          const int mid = (d0 + d1) / 2, f = upto(mid);
+          if (f <= r)
+            d0 = mid, f0 = f;
+          else
+            d1 = mid;
+        }
+        int rem = r - f0;
+        for (int b0 = 0;; b0 += 32) {
+          const uint32_t in = __ballot_sync(kAll, b0 + lane < pv.B && blocks(min(b0 + lane, pv.B - 1)) > d0);
+          const int c = __popc(in);
+          if (rem < c) {
+            j.b = b0 + (int)__fns(in, 0, rem + 1);
+            break;
+          }
+          rem -= c;
+        }
+        j.n = seq_tokens(pv, j.b, j.q0);
+        int len = j.n;
+        if (PAGED) {
+          len = max(pv.lens[j.b], 0);
+          const int64_t cap = (int64_t)pv.max_pages << pv.page_shift;
+          if (len > cap || j.n > a.max_new) {
+            if (lane == 0) set_err(pv.err, kErrCount);
+            len = (int)min((int64_t)len, cap);
+          }
+        }
+        j.p0 = len - j.n;
+        j.tok0 = ((j.n + 2 * P - 1) / (2 * P) - 1 - d0) * 2 * P;
+        j.two = j.tok0 + P < j.n;
+        const int lo0 = max(0, j.p0 + j.tok0 - a.window + 1);
+        j.lo = lo0 / kTcT * kTcT;
+        int last = 0;
+        for (int i = 0; i < 1 + j.two; ++i) {
+          const int f = j.p0 + j.tok0 + i * P, l = j.p0 + min(j.n, j.tok0 + (i + 1) * P) - 1;
+          if (l >= 0) {
+            j.js[i] = (max(0, f - a.window + 1) - j.lo) / kTcT;
+            j.je[i] = (l - j.lo) / kTcT + 1;
+          }
+          last = l;
+        }
+        j.nt = max(j.je[0], j.je[1]);
+        j.first = j.p0 + j.tok0;
+        j.low = last - a.window + 1;
+      } else {
+        j.b = -1;
+      }
+      const int slot = k & 1;
+      if (k >= 2 && !wait0(&jfree[slot], (k / 2 - 1) & 1)) break;
+      if (lane == 0) {
+        jobs[slot] = j;
+        mbar_arrive(&jfull[slot]);
+      }
+      __syncwarp();
+      if (!go) break;
+      if (j.nt == 0) continue;
+      if (loads > 0 && !wait0(qfree, (loads - 1) & 1)) break;
+      ++loads;
+      if (lane == 0) mbar_expect_tx(qfull, (1 + j.two) * NB * G * P * 128);
+      __syncwarp();
+      if (lane < (1 + j.two) * NB) {
+        const int i = lane / NB, half = lane % NB;
+        tma3(sm + SM::kQ + i * SM::kTile + half * kBox, &t.mq, 64 * half, j.h * G, j.q0 + j.tok0 + i * P, qfull);
+      }
+      // page of this lane's part of a tile, one tile ahead
+      const int pages = PAGED ? kTcT >> pv.page_shift : 1;
+      const int part = lane / NB, half = lane % NB;
+      auto page_of = [&](int jt) {
+        const int pos = j.lo + jt * kTcT + (part << pv.page_shift);
+        if (part >= pages || pos >= j.p0 + j.n) return pv.n_pages;  // outside: reads as zeros
+        const int page = pv.table[(int64_t)j.b * pv.max_pages + (pos >> pv.page_shift)];
+        if ((unsigned)page < (unsigned)pv.n_pages) return page;
+        set_err(pv.err, kErrPage);
+        return pv.n_pages;
+      };
+      int page = PAGED ? page_of(0) : 0;
+      bool ok = true;
+      for (int jt = 0; jt < j.nt && ok; ++jt) {
+        const int page_next = PAGED && jt + 1 < j.nt ? page_of(jt + 1) : 0;
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv) {
+          ok = wait0(&free_[s], ph ^ 1);
+          if (!ok) break;
+          if (lane == 0) mbar_expect_tx(&full[s], SM::kTile);
+          __syncwarp();
+          uint8_t *dst = sm + SM::kRing + s * SM::kTile + half * kBox;
+          const CUtensorMap *m = kv ? &t.mv : &t.mk;
+          if (lane < pages * NB) {
+            if (PAGED)
+              tma4(dst + (part << pv.page_shift) * 128, m, 64 * half, 0, j.h, page, &full[s]);
+            else
+              tma3(dst, m, 64 * half, j.q0 + j.lo + jt * kTcT, j.h, &full[s]);
+          }
+          if (++s == NS) s = 0, ph ^= 1;
+        }
+        page = page_next;
+      }
+      if (!ok) break;
+    }
+    // after a wait that gave up: the copies in flight land before the CTA ends
+    if (*abort_flag && lane == 0) {
+      if (loads > 0) mbar_wait(qfull, (loads - 1) & 1, kWaits);
+      for (int i = 0; i < NS; ++i) {
+        if (ph == 0 && i >= s) break;  // never used
+        mbar_wait(&full[i], i < s ? ph : ph ^ 1, kWaits);
+      }
+    }
+  } else if (warp == 8) {
+    // -- products ---------------------------------------------------------------
+    if (lane == 0) {
+      constexpr uint32_t id_s = BF16 ? umma_idesc(128, kTcT, false, false) : umma_idesc_f16(128, kTcT, false, false);
+      constexpr uint32_t id_v = BF16 ? umma_idesc(128, D, false, true) : umma_idesc_f16(128, D, false, true);
+      constexpr uint32_t hi = umma_desc_hi_sw128(1024);
+      int s = 0;
+      uint32_t ph = 0;
+      int loads = 0;
+      uint32_t cleans = 0;  // parity of either stage's vclean
+      int tiles[2] = {0, 0}, done[2] = {0, 0};  // tiles, and jobs with any, of either query tile
+      auto scores = [&](int i, int at) {
+        const uint32_t q = umma_desc_lo(smem_u32(sm + SM::kQ + i * SM::kTile), 16);
+        const uint32_t kk = umma_desc_lo(smem_u32(sm + SM::kRing + at * SM::kTile), 16);
+#pragma unroll
+        for (int b = 0; b < D / 64; ++b)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            umma_f16_ss_w(tS + 128 * i, q + b * (kBox >> 4) + 2 * x, kk + b * (kBox >> 4) + 2 * x, hi, id_s, b + x > 0);
+        umma_commit(&sfull[i]);
+      };
+      auto values = [&](int i, int at, bool acc) {
+        const uint32_t vv = umma_desc_lo(smem_u32(sm + SM::kRing + at * SM::kTile), kBox);
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          if (!wait(&pfull[2 * i + hf], tiles[i] & 1)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int x = 4 * hf; x < 4 * hf + 4; ++x)
+            umma_f16_ts_w(tO + D * i, tS + 128 * i + 8 * x, vv + 128 * x, hi, id_v, acc || x > 0);
+        }
+        umma_commit(&odone[i]);
+        ++tiles[i];
+        return true;
+      };
+      bool ok = true;
+      for (int k = 0; ok; ++k) {
+        const int slot = k & 1;
+        if (!wait(&jfull[slot], (k / 2) & 1)) break;
+        const Job j = jobs[slot];
+        mbar_arrive(&jfree[slot]);
+        if (j.b < 0) break;
+        if (j.nt == 0) continue;
+        if (!wait(qfull, loads & 1)) break;
+        ++loads;
+        // K of tile 0
+        if (!wait(&full[s], ph)) break;
+        tc_fence_after();
+        for (int i = 0; i < 2; ++i)
+          if (j.js[i] == 0 && j.je[i] > 0) scores(i, s);
+        umma_commit(&free_[s]);
+        if (j.nt == 1) umma_commit(qfree);
+        int sv = s + 1, phv = ph;
+        if (sv == NS) sv = 0, phv ^= 1;
+        for (int jt = 0; jt < j.nt && ok; ++jt) {
+          const int t0 = j.lo + jt * kTcT;
+          int sk = sv + 1, phk = phv;
+          if (sk == NS) sk = 0, phk ^= 1;
+          bool have_v = false, have_k = false;
+          for (int i = 0; i < 2 && ok; ++i) {
+            if (jt >= j.js[i] && jt < j.je[i]) {
+              if (!have_v) {
+                ok = wait(&full[sv], phv);
+                if (ok && (t0 + kTcT - 1 > j.first || t0 < j.low)) {
+                  ok = wait(&vclean[sv], cleans >> sv & 1);
+                  cleans ^= 1u << sv;
+                }
+                tc_fence_after();
+                have_v = true;
+              }
+              if (ok && jt == j.js[i]) {
+                // the tile's last result has been read
+                if (done[i] > 0) ok = wait(&ofree[i], (done[i] - 1) & 1);
+                ++done[i];
+              }
+              if (ok) ok = values(i, sv, jt > j.js[i]);
+            }
+            if (ok && jt + 1 >= j.js[i] && jt + 1 < j.je[i]) {
+              if (!have_k) {
+                ok = wait(&full[sk], phk);
+                tc_fence_after();
+                have_k = true;
+              }
+              if (ok) scores(i, sk);
+            }
+          }
+          if (!ok) break;
+          umma_commit(&free_[sv]);
+          if (jt + 1 < j.nt) {
+            umma_commit(&free_[sk]);
+            if (jt + 2 == j.nt) umma_commit(qfree);
+          }
+          s = sk, ph = phk;
+          sv = sk + 1, phv = phk;
+          if (sv == NS) sv = 0, phv ^= 1;
+        }
+      }
+      // after a wait that gave up: the products in flight end before TMEM is freed
+      if (*abort_flag) {
+        umma_commit(drain);
+        mbar_wait(drain, 0, kWaits);
+      }
+    }
+    __syncwarp();
+  } else if (warp >= 10) {
+    // -- values of partly seen tiles ----------------------------------------------
+    int s = 0;
+    uint32_t ph = 0;
+    for (int k = 0;; ++k) {
+      const int slot = k & 1;
+      if (!wait(&jfull[slot], (k / 2) & 1)) break;
+      Job &js = jobs[slot];
+      const int nt = js.b < 0 ? -1 : js.nt, lo = js.lo, first = js.first, low = js.low;
+      bool ok = true;
+      auto pass = [&]() {
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&free_[s]);
+        if (++s == NS) s = 0, ph ^= 1;
+      };
+      for (int jt = 0; jt < nt; ++jt) {
+        if (!(ok = wait(&full[s], ph))) break;  // keys
+        pass();
+        if (!(ok = wait(&full[s], ph))) break;
+        const int t0 = lo + jt * kTcT;
+        if (t0 + kTcT - 1 > first || t0 < low) {
+          uint4 *x = reinterpret_cast<uint4 *>(sm + SM::kRing + s * SM::kTile) + (warp - 10) * (SM::kTile / 32);
+          bool fine = true;
+          for (int e = lane; e < SM::kTile / 32; e += 32 * 8) {
+            uint4 u[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) u[y] = x[e + 32 * y];
+#pragma unroll
+            for (int y = 0; y < 8; ++y)
+              if (!(pair_fine<BF16>(u[y].x) && pair_fine<BF16>(u[y].y) && pair_fine<BF16>(u[y].z) && pair_fine<BF16>(u[y].w))) {
+                x[e + 32 * y] = make_uint4(pair_scrubbed<BF16>(u[y].x), pair_scrubbed<BF16>(u[y].y),
+                                           pair_scrubbed<BF16>(u[y].z), pair_scrubbed<BF16>(u[y].w));
+                fine = false;
+              }
+          }
+          if (!fine) {
+            js.bad = 1;
+            fence_proxy_async();
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&vclean[s]);
+        }
+        pass();
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&jfree[slot]);
+      if (nt < 0 || !ok) break;
+    }
+  } else {
+    // -- softmax and results: a thread per row of query tile i -----------------------
+    const int i = warp >> 2;
+    const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t ts = tS + 128 * i + lane_off, to = tO + D * i + lane_off;
+    const int row = (warp & 3) * 32 + lane, my_tok = row / G;
+    const float sg = a.sig_log2;
+    // f16 weights are 2^8 larger, and the reference moves sooner: at most 2^14
+    constexpr float kShift = BF16 ? 0.f : 8.f, kLag = BF16 ? 8.f : 6.f;
+    int tiles = 0;  // of this query tile so far
+    auto arrive = [&](uint64_t *b) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(b);
+    };
+    for (int k = 0;; ++k) {
+      const int slot = k & 1;
+      if (!wait(&jfull[slot], (k / 2) & 1)) break;
+      const Job &j = jobs[slot];
+      const int jb = j.b;
+      bool ok = true;
+      if (jb >= 0 && (i == 0 || j.two)) {
+        const int tok = j.tok0 + i * P + my_tok;
+        const bool real = my_tok < P && tok < j.n;
+        const int pos = j.p0 + tok;
+        // rows that are nobody's are never masked: their own affair
+        const int lim = real ? pos : 1 << 30, low = real ? pos - a.window + 1 : -(1 << 30);
+        const int js = j.js[i], je = j.je[i], lo = j.lo;
+        float m = -INFINITY, l = 0.f;
+        for (int jt = js; jt < je; ++jt) {
+          if (!(ok = wait(&sfull[i], tiles & 1))) break;
+          tc_fence_after();
+          float x[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32_nw(ts + 32 * c, x + 32 * c);
+          tmem_wait_ld();
+          const int t0 = lo + jt * kTcT;
+          const int past = lim - t0, before = low - t0;  // columns [before, past] are seen
+          if (__any_sync(kAll, past < kTcT - 1 || before > 0)) {
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c > past || c < before) x[c] = -INFINITY;
+          }
+          float mx[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+          for (int c = 4; c < 128; c += 8)
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              mx[y] = c + 4 + y < 128 ? fmaxf(fmaxf(mx[y], x[c + y]), x[c + 4 + y]) : fmaxf(mx[y], x[c + y]);
+          const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * sg;
+          const bool move = real && top > m + kLag;
+          if (__any_sync(kAll, move)) {
+            const float mn = move ? top : m;
+            const float f = m == -INFINITY ? 0.f : fast_exp2(m - mn);
+            m = mn;
+            l *= f;
+            if (jt > js) {  // the products before this tile's have to be in
+              if (!(ok = wait(&odone[i], (tiles - 1) & 1))) break;
+              tc_fence_after();
+#pragma unroll 1
+              for (int c = 0; c < D; c += 16) {
+                float o[16];
+                tmem_ld16(to + c, o);
+#pragma unroll
+                for (int y = 0; y < 16; ++y) o[y] *= f;
+                tmem_st16(to + c, o);
+              }
+            }
+          }
+          const float ref = (m == -INFINITY ? 0.f : m) - kShift;
+          const uint64_t sg2 = pair_f32(sg, sg), ref2 = pair_f32(-ref, -ref);
+          uint64_t sum[2] = {0, 0};
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            uint32_t w[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              float u, v;
+              unpair_f32(fma_f32x2(pair_f32(x[16 * c + 2 * y], x[16 * c + 2 * y + 1]), sg2, ref2), u, v);
+              u = fast_exp2(u);
+              v = fast_exp2(v);
+              sum[y & 1] = add_f32x2(sum[y & 1], pair_f32(u, v));
+              w[y] = pack2<BF16>(u, v);
+            }
+            tmem_st8_nw(ts + 8 * c, w);
+            if (c == 3 || c == 7) {
+              tmem_wait_st();
+              tc_fence_before();
+              arrive(&pfull[2 * i + (c >> 2)]);
+            }
+          }
+          float u, v;
+          unpair_f32(add_f32x2(sum[0], sum[1]), u, v);
+          l += u + v;
+          ++tiles;
+        }
+        if (!ok) break;
+        const bool sees = real && pos >= 0;
+        const float inv = sees ? 1.f / l : 0.f;
+        uint32_t nan[D / 32] = {};  // channels of which the row sees a value that is not finite
+        if (je > js) {
+          if (!wait(&odone[i], (tiles - 1) & 1)) break;
+          tc_fence_after();
+          if (j.bad && real) {
+            const int first = j.first, lowest = j.low;
+            for (int jt = js; jt < je; ++jt) {
+              const int t0 = lo + jt * kTcT;
+              if (t0 + kTcT - 1 <= first && t0 >= lowest) continue;
+              for (int p = max(t0, low); p <= min(t0 + kTcT - 1, lim); ++p) {
+                const uint8_t *src;
+                if (PAGED) {
+                  const int page = pv.table[(int64_t)jb * pv.max_pages + (p >> pv.page_shift)];
+                  if ((unsigned)page >= (unsigned)pv.n_pages) continue;
+                  src = pv.v + (((((int64_t)page * pv.Hkv + j.h) << pv.page_shift) + (p & ((1 << pv.page_shift) - 1))) * D) * 2;
+                } else {
+                  src = a.v.p + 2 * ((int64_t)(j.q0 + p) * a.v.ts + j.h * a.v.hs);
+                }
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                  const uint4 u = reinterpret_cast<const uint4 *>(src)[c];
+                  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                  for (int y = 0; y < 4; ++y) {
+                    constexpr uint32_t mk = BF16 ? 0x7F80u : 0x7C00u;
+                    const int ch = 8 * c + 2 * y;
+                    nan[ch >> 5] |= ((w[y] & mk) == mk ? 1u : 0u) << (ch & 31);
+                    nan[ch >> 5] |= ((w[y] >> 16 & mk) == mk ? 2u : 0u) << (ch & 31);
+                  }
+                }
+              }
+            }
+          }
+          __syncwarp();
+        }
+        uint8_t *dst = static_cast<uint8_t *>(a.out) + 2 * ((int64_t)(j.q0 + tok) * a.Hq + j.h * G + (row - my_tok * G)) * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          float o[32];
+          if (je > js) {
+            tmem_ld32(to + 32 * c, o);
+          } else {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = 0.f;
+          }
+          if (real) {
+            uint32_t w[16];
+#pragma unroll
+            for (int y = 0; y < 16; ++y) {
+              float u = sees ? o[2 * y] * inv : 0.f, v = sees ? o[2 * y + 1] * inv : 0.f;
+              if (nan[c] >> (2 * y) & 1) u = NAN;
+              if (nan[c] >> (2 * y + 1) & 1) v = NAN;
+              w[y] = pack2<BF16>(u, v);
+            }
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+              reinterpret_cast<uint4 *>(dst)[4 * c + y] = make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+          }
+        }
+        if (je > js) {
+          tc_fence_before();
+          arrive(&ofree[i]);
+        }
+      }
+      arrive(&jfree[slot]);
+      if (jb < 0) break;
+    }
+    __syncwarp();
+  }
+
+  if (*abort_flag && lane == 0) set_err(pv.err, kErrTimeout);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+  pdl_trigger();
+}
+
+// [rows, heads, D] of 16-bit values as boxes of 64 channels: `inner` and
+// `outer` dimensions with their strides in elements.
+cudaError_t rows_map(CUtensorMap *m, bool bf, void *p, int D, int64_t n1, int64_t s1, int64_t n2, int64_t s2, int b1, int b2) {
+  const uint64_t dims[3] = {(uint64_t)D, (uint64_t)n1, (uint64_t)n2};
+  const uint64_t strides[2] = {(uint64_t)s1 * 2, (uint64_t)s2 * 2};
+  const uint32_t box[3] = {64, (uint32_t)b1, (uint32_t)b2}, one[3] = {1, 1, 1};
+  return encode_tensor_map_tiled(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, p, dims,
+                                 strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+cudaError_t pages_map(CUtensorMap *m, bool bf, const PagedView &v, void *p) {
+  const uint64_t page = 1ull << v.page_shift, row = (uint64_t)v.D * 2;
+  const uint64_t dims[4] = {(uint64_t)v.D, page, (uint64_t)v.Hkv, (uint64_t)v.n_pages};
+  const uint64_t strides[3] = {row, row * page, row * page * v.Hkv};
+  const uint32_t box[4] = {64, (uint32_t)page, 1, 1}, one[4] = {1, 1, 1, 1};
+  return encode_tensor_map_tiled(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p, dims,
+                                 strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
+template <int D, bool BF16, bool PAGED>
+cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
+  static std::atomic<bool> ready{false};
+  cudaError_t e = cudaSuccess;
+  if (!ready.load(std::memory_order_relaxed)) {
+    e = cudaFuncSetAttribute(attn_tc_kernel<D, BF16, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes);
+    if (e != cudaSuccess) return e;
+    ready.store(true, std::memory_order_relaxed);
+  }
+  TcArgs t;
+  t.a = a;
+  t.P = kTcT / a.G;
+  const int N = a.pv.n_tokens;
+  e = rows_map(&t.mq, BF16, a.q.p, D, a.Hq, a.q.hs, N, a.q.ts, a.G, t.P);
+  if (e == cudaSuccess)
+    e = PAGED ? pages_map(&t.mk, BF16, a.pv, a.pv.k) : rows_map(&t.mk, BF16, a.k.p, D, N, a.k.ts, a.pv.Hkv, a.k.hs, kTcT, 1);
+  if (e == cudaSuccess)
+    e = PAGED ? pages_map(&t.mv, BF16, a.pv, a.pv.v) : rows_map(&t.mv, BF16, a.v.p, D, N, a.v.ts, a.pv.Hkv, a.v.hs, kTcT, 1);
+  if (e != cudaSuccess) return e;
+  // at most so many jobs: every sequence's last one may be a partial one
+  const int64_t jobs = (int64_t)a.pv.Hkv * (N / (2 * t.P) + std::min(a.pv.B, N));
+  const int grid = (int)std::min<int64_t>(a.sms, jobs);
+  return launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3(grid), dim3(kTcThreads), Smem<D>::kBytes, st, t);
+}
+
+template <int D, bool BF16>
+cudaError_t launch_src(const AttnArgs &a, cudaStream_t st) {
+  return a.pv.k ? launch_t<D, BF16, true>(a, st) : launch_t<D, BF16, false>(a, st);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st) {
+  if (a.pv.B == 0 || a.pv.n_tokens == 0) return cudaSuccess;
+  const bool bf = dtype == kSrvBf16;
+  switch (a.pv.D) {
+    case 128: return bf ? launch_src<128, true>(a, st) : launch_src<128, false>(a, st);
+    case 64: return bf ? launch_src<64, true>(a, st) : launch_src<64, false>(a, st);
+    default: return cudaErrorInvalidValue;
+  }
+}
+
+}  // namespace kvk

@@ -64,7 +64,7 @@ __device__ Place find_place(const PagedView &v, int t, int lane) {
   const int c0 = v.cu[n], c1 = v.cu[n + 1];
   if (t < c0 || t >= c1) return p;
   p.seq = n;
-  p.pos = v.lens[n] - c1 + t;
+  p.pos = max(v.lens[n], 0) - c1 + t;
   if (p.pos < 0) return p;
   const int pg = p.pos >> v.page_shift;
   if (pg >= v.max_pages) {

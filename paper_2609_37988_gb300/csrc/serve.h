@@ -56,6 +56,7 @@ struct AttnArgs {
   int sms;
 };
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
+cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st);
 // CTAs that a split launch may use at most, and the partial slots of each
 constexpr int kRowsMaxCtas = 512;
 constexpr int kRowsPerUnit = 16;

@@ -137,6 +137,11 @@ PagedView view_of(const kvk_paged *p, int layer, const kvk_paged_batch *b) {
   return v;
 }
 
+cudaError_t launch_attn(const AttnArgs &a, int dtype, cudaStream_t st) {
+  if (a.pv.k && (int64_t)a.max_new * a.G <= 64) return launch_attn_rows(a, dtype, st);
+  return launch_attn_tc(a, dtype, st);
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNoWindow = 1 << 30;
 
@@ -343,7 +348,7 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.counter = reinterpret_cast<int32_t *>(p->ws + w.counter);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
-  const cudaError_t e = launch_attn_rows(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+  const cudaError_t e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;
 }
@@ -396,7 +401,7 @@ kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_
   a.window = window && window < kNoWindow ? window : kNoWindow;
   a.max_new = n_tokens;
   a.sig_log2 = softmax_scale * kLog2e;
-  e = launch_attn_rows(a, dtype, reinterpret_cast<cudaStream_t>(stream));
+  e = launch_attn(a, dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "prompt attention launch");
   return KVK_OK;
 }
