@@ -15,6 +15,7 @@ contiguous, any other strides (views of a fused projection, say).
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -26,6 +27,15 @@ __all__ = ["Rotary", "PagedCache", "prompt_attention", "KVKError"]
 
 _CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
+# A serving step's small calls take 3-8 us on the GPU, so the binding's own time
+# counts: structures are packed as bytes (0.05 us against 0.2 for a ctypes one),
+# each tensor's strides and shape are read once, and outputs come from
+# empty_like (1.0 us against 3.1 for torch.empty with shape, dtype and device).
+_pack_rows = struct.Struct("Pqq").pack              # kvk_rows
+_pack_batch = struct.Struct("PPPiiii").pack         # kvk_paged_batch
+assert struct.calcsize("Pqq") == ctypes.sizeof(Rows) and struct.calcsize("PPPiiii") == ctypes.sizeof(PagedBatch)
+_current_device = torch._C._cuda_getDevice
+
 
 def _code(t: torch.Tensor) -> int:
     code = _CODES.get(t.dtype)
@@ -34,48 +44,52 @@ def _code(t: torch.Tensor) -> int:
     return code
 
 
-def _rows(t: torch.Tensor, name: str, like: torch.Tensor = None, shape=None) -> Rows:
-    if t.dim() != 3 or not t.is_cuda or (t.shape[2] > 1 and t.stride(2) != 1):
-        raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, head_dim] with contiguous channels")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must be {tuple(shape)}, got {tuple(t.shape)}")
-    if like is not None:
-        if t.dtype != like.dtype:
-            raise TypeError(f"{name} is {t.dtype}, expected {like.dtype}")
-        if t.device != like.device:
-            raise ValueError(f"{name} is on {t.device}, expected {like.device}")
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+def _rows(t: torch.Tensor, name: str, dtype, index: int, shape) -> bytes:
+    """``t`` as a kvk_rows: ``shape`` (tokens, heads, head_dim) of ``dtype`` on
+    GPU ``index``, channels contiguous."""
+    if t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor {tuple(shape)}, got {tuple(t.shape)} on {t.device}")
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    ts, hs, cs = t.stride()
+    if cs != 1 and shape[2] > 1:
+        raise ValueError(f"{name} must have contiguous channels")
+    return _pack_rows(t.data_ptr(), ts, hs)
 
 
-def _ints(t: torch.Tensor, name: str, shape, device):
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape) or t.device != device:
-        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {device}")
+def _ints(t: torch.Tensor, name: str, shape, index: int) -> int:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on cuda:{index}")
     return t.data_ptr()
 
 
-class _On:
-    """Makes the tensors' device current where it is not (the library's calls
-    launch on the current device)."""
-
-    def __init__(self, device, stream):
-        self.prev = torch._C._cuda_getDevice()
-        self.want = device.index
-        if stream is not None and stream.device != device:
-            raise ValueError(f"stream of {stream.device}, tensors on {device}")
-
-    def __enter__(self):
-        if self.want != self.prev:
-            torch.cuda.set_device(self.want)
-
-    def __exit__(self, *exc):
-        if self.want != self.prev:
-            torch.cuda.set_device(self.prev)
+def _call(index: int, stream, fn, *args):
+    """The library's call on GPU ``index``, which it wants to be the current one."""
+    if stream is not None and stream.device.index != index:
+        raise ValueError(f"stream of {stream.device}, tensors on cuda:{index}")
+    if _current_device() == index:
+        st = fn(*args, _stream(stream))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, _stream(stream))
+    if st:
+        check(st)
 
 
-def _new(shape, dtype, device, stream):
-    out = torch.empty(shape, dtype=dtype, device=device)
+def _new_like(t: torch.Tensor, stream) -> torch.Tensor:
+    out = torch.empty_like(t, memory_format=torch.contiguous_format)
     if stream is not None:
         out.record_stream(stream)
+    return out
+
+
+def _out_like(out: torch.Tensor, t: torch.Tensor, stream) -> torch.Tensor:
+    if out is None:
+        return _new_like(t, stream)
+    if out.shape != t.shape or out.dtype is not t.dtype or out.device != t.device or not out.is_contiguous():
+        raise ValueError("out must be contiguous, of q's shape, dtype and device")
     return out
 
 
@@ -108,16 +122,17 @@ class Rotary:
         check(self.lib.kvk_rotary_create(head_dim, self.rotary_dim, self.n_axes, (ctypes.c_double * n)(*inv_freq),
                                          (ctypes.c_int32 * n)(*axes), int(adjacent), float(factor), ctypes.byref(h)))
         self.handle = h
+        self._apply = self.lib.kvk_rotary_apply
 
     def __del__(self):
         if getattr(self, "handle", None):
             self.lib.kvk_rotary_destroy(self.handle)
             self.handle = None
 
-    def _positions(self, positions, n, device):
+    def _positions(self, positions, n, index):
         if positions.dim() == 1:
             positions = positions.unsqueeze(0)
-        return _ints(positions, "positions", (self.n_axes, n), device)
+        return _ints(positions, "positions", (self.n_axes, n), index)
 
     def apply(self, q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, out=None, stream=None):
         """Rotates ``q`` and ``k`` (either may be ``None``) to ``positions``
@@ -126,24 +141,26 @@ class Rotary:
         x = q if q is not None else k
         if x is None:
             raise ValueError("q or k must be given")
-        if x.dim() != 3:
-            raise ValueError("q and k must be [tokens, heads, head_dim]")
-        n, dev = x.shape[0], x.device
-        args, res = [], []
-        for i, (t, name) in enumerate(((q, "q"), (k, "k"))):
-            if t is None:
-                args += [None, None, 0]
-                res.append(None)
-                continue
-            rows = _rows(t, name, x, (n, t.shape[1] if t.dim() == 3 else 0, self.head_dim))
-            o = out[i] if out is not None else _new(t.shape, t.dtype, dev, stream)
-            args += [rows, _rows(o, name + "_out", x, t.shape), t.shape[1]]
-            res.append(o)
-        pos = self._positions(positions, n, dev)
-        with _On(dev, stream):
-            check(self.lib.kvk_rotary_apply(self.handle, args[0], args[1], args[2], args[3], args[4], args[5], _code(x), n,
-                                            pos, _stream(stream)))
-        return tuple(res)
+        if x.dim() != 3 or (k is not None and k.dim() != 3) or not x.is_cuda:
+            raise ValueError("q and k must be CUDA tensors [tokens, heads, head_dim]")
+        n, d, index, dtype = x.shape[0], self.head_dim, x.get_device(), x.dtype
+        code = _code(x)
+        rq = oq = rk = ok = q_out = k_out = None
+        hq = hk = 0
+        if q is not None:
+            hq = q.shape[1]
+            shape = (n, hq, d)
+            rq = _rows(q, "q", dtype, index, shape)
+            q_out = _new_like(q, stream) if out is None else out[0]
+            oq = _rows(q_out, "q_out", dtype, index, shape)
+        if k is not None:
+            hk = k.shape[1]
+            shape = (n, hk, d)
+            rk = _rows(k, "k", dtype, index, shape)
+            k_out = _new_like(k, stream) if out is None else out[1]
+            ok = _rows(k_out, "k_out", dtype, index, shape)
+        _call(index, stream, self._apply, self.handle, rq, oq, hq, rk, ok, hk, code, n, self._positions(positions, n, index))
+        return q_out, k_out
 
 
 class PagedCache:
@@ -194,11 +211,13 @@ class PagedCache:
         self.workspace = torch.empty(ws.value, dtype=torch.uint8, device=dev)
         h = ctypes.c_void_p()
         ptrs = [(ctypes.c_void_p * n_layers)(*[t.data_ptr() for t in p]) for p in (k_pages, v_pages)]
-        with _On(dev, None):
+        with torch.cuda.device(dev):
             check(self.lib.kvk_paged_create(ctypes.byref(self.desc), ptrs[0], ptrs[1], _ptr(self.workspace), ws.value,
                                             ctypes.byref(h)))
             self.handle = h
             check(self.lib.kvk_paged_reset(h, _stream()))
+        self._index = dev.index
+        self._append, self._attend = self.lib.kvk_paged_append, self.lib.kvk_paged_attention
 
     def close(self):
         if getattr(self, "handle", None):
@@ -211,12 +230,12 @@ class PagedCache:
         except Exception:
             pass
 
-    def _batch(self, n, cu, lengths, table) -> PagedBatch:
+    def _batch(self, n, cu, lengths, table) -> bytes:
         if lengths.dim() != 1 or table.dim() != 2:
             raise ValueError("lengths must be [B], table [B, max_pages]")
-        B, dev = lengths.shape[0], self.device
-        return PagedBatch(_ints(cu, "cu", (B + 1,), dev), _ints(lengths, "lengths", (B,), dev),
-                          _ints(table, "table", (B, table.shape[1]), dev), B, table.shape[1], n)
+        B, width, index = lengths.shape[0], table.shape[1], self._index
+        return _pack_batch(_ints(cu, "cu", (B + 1,), index), _ints(lengths, "lengths", (B,), index),
+                           _ints(table, "table", (B, width), index), B, width, n, 0)
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, lengths: torch.Tensor,
                table: torch.Tensor, *, rotary: Rotary = None, positions: torch.Tensor = None, q: torch.Tensor = None,
@@ -225,26 +244,21 @@ class PagedCache:
         rotated on the way where ``rotary`` is given (to ``positions``, or to the
         tokens' own positions); rotates ``q`` beside them and returns it
         (``q_out`` may be ``q``).  Rows of ``q`` in no sequence stay unwritten."""
-        if k.dim() != 3:
-            raise ValueError("k must be [tokens, n_kv_heads, head_dim]")
-        n = k.shape[0]
-        like = self.k_pages[0]
+        n, index, dtype = k.shape[0], self._index, self.dtype
         shape = (n, self.n_kv_heads, self.head_dim)
-        rk, rv = _rows(k, "k", like, shape), _rows(v, "v", like, shape)
+        rk, rv = _rows(k, "k", dtype, index, shape), _rows(v, "v", dtype, index, shape)
         rq = ro = None
         if q is not None:
             shape = (n, self.n_q_heads, self.head_dim)
-            rq = _rows(q, "q", like, shape)
+            rq = _rows(q, "q", dtype, index, shape)
             if q_out is None:
-                q_out = _new(shape, q.dtype, q.device, stream)
-            ro = _rows(q_out, "q_out", like, shape)
+                q_out = _new_like(q, stream)
+            ro = _rows(q_out, "q_out", dtype, index, shape)
         if positions is not None and rotary is None:
             raise ValueError("positions without a rotary")
-        pos = 0 if positions is None else rotary._positions(positions, n, self.device)
-        b = self._batch(n, cu, lengths, table)
-        with _On(self.device, stream):
-            check(self.lib.kvk_paged_append(self.handle, layer, b, rk, rv, rotary.handle if rotary is not None else None,
-                                            pos, rq, ro, _stream(stream)))
+        pos = 0 if positions is None else rotary._positions(positions, n, index)
+        _call(index, stream, self._append, self.handle, layer, self._batch(n, cu, lengths, table), rk, rv,
+              rotary.handle if rotary is not None else None, pos, rq, ro)
         return q_out if q is not None else None
 
     def attend(self, layer: int, q: torch.Tensor, cu: torch.Tensor, lengths: torch.Tensor, table: torch.Tensor,
@@ -256,29 +270,17 @@ class PagedCache:
         them); a tight one lets decode steps run the form for few tokens.
         Returns ``[tokens, n_q_heads, head_dim]``; rows in no sequence stay
         unwritten."""
-        if q.dim() != 3:
-            raise ValueError("q must be [tokens, n_q_heads, head_dim]")
         n = q.shape[0]
-        rq = _rows(q, "q", self.k_pages[0], (n, self.n_q_heads, self.head_dim))
-        out = self._out(out, q, stream)
-        b = self._batch(n, cu, lengths, table)
-        with _On(self.device, stream):
-            check(self.lib.kvk_paged_attention(self.handle, layer, b, rq, float(scale), n if max_new is None else max_new,
-                                               window, _ptr(out), _stream(stream)))
-        return out
-
-    @staticmethod
-    def _out(out, q, stream):
-        if out is None:
-            return _new(q.shape, q.dtype, q.device, stream)
-        if out.shape != q.shape or out.dtype != q.dtype or out.device != q.device or not out.is_contiguous():
-            raise ValueError("out must be contiguous, of q's shape, dtype and device")
+        rq = _rows(q, "q", self.dtype, self._index, (n, self.n_q_heads, self.head_dim))
+        out = _out_like(out, q, stream)
+        _call(self._index, stream, self._attend, self.handle, layer, self._batch(n, cu, lengths, table), rq, scale,
+              n if max_new is None else max_new, window, out.data_ptr())
         return out
 
     def device_error(self, stream=None) -> int:
         """Synchronise, read and clear the device error word (0 = none)."""
         code = ctypes.c_int32()
-        with _On(self.device, stream):
+        with torch.cuda.device(self.device):
             st = self.lib.kvk_paged_get_device_error(self.handle, _stream(stream), ctypes.byref(code))
         if st not in (0, 7):
             check(st)
@@ -293,18 +295,18 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     - 1``; ``window``: a query sees that many positions at most (0: all).
     ``error``: an int32 tensor of one element that gets device error bits.
     Returns ``[tokens, H_q, head_dim]``; rows in no sequence stay unwritten."""
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q, k and v must be [tokens, heads, head_dim]")
+    if q.dim() != 3 or k.dim() != 3 or not q.is_cuda:
+        raise ValueError("q, k and v must be CUDA tensors [tokens, heads, head_dim]")
     n, hq, d = q.shape
+    index, dtype = q.get_device(), q.dtype
     kv = (n, k.shape[1], d)
-    rq, rk, rv = _rows(q, "q"), _rows(k, "k", q, kv), _rows(v, "v", q, kv)
-    out = PagedCache._out(out, q, stream)
+    rq = _rows(q, "q", dtype, index, q.shape)
+    rk, rv = _rows(k, "k", dtype, index, kv), _rows(v, "v", dtype, index, kv)
+    out = _out_like(out, q, stream)
     if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
         raise ValueError("cu_seqlens must be [sequences + 1]")
     B = cu_seqlens.shape[0] - 1
-    cu = _ints(cu_seqlens, "cu_seqlens", (B + 1,), q.device)
-    err = 0 if error is None else _ints(error, "error", (1,), q.device)
-    with _On(q.device, stream):
-        check(load().kvk_prompt_attention(rq, rk, rv, n, hq, kv[1], d, _code(q), cu, B, float(scale), window, _ptr(out), err,
-                                          _stream(stream)))
+    _call(index, stream, load().kvk_prompt_attention, rq, rk, rv, n, hq, kv[1], d, _code(q),
+          _ints(cu_seqlens, "cu_seqlens", (B + 1,), index), B, scale, window, out.data_ptr(),
+          0 if error is None else _ints(error, "error", (1,), index))
     return out

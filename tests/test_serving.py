@@ -44,8 +44,8 @@ def test_paged_plan(lib):
 
 def test_null_handles(lib):
     so = lib.load()
-    b = lib.PagedBatch()
-    r = lib.Rows(1, 128, 128)
+    b = ctypes.byref(lib.PagedBatch())
+    r = ctypes.byref(lib.Rows(1, 128, 128))
     code = ctypes.c_int32()
     assert so.kvk_paged_create(ctypes.byref(_paged(lib)), None, None, None, 0, None) == INVALID
     h = ctypes.c_void_p()
@@ -88,21 +88,23 @@ def test_rotary_create(lib):
     st, h = _rotary(lib)
     assert st == 0
     so = lib.load()
-    ok, apply = lib.Rows(256, 64, 64), so.kvk_rotary_apply
+    rows = lambda *a: ctypes.byref(lib.Rows(*a))  # noqa: E731
+    ok, apply = rows(256, 64, 64), so.kvk_rotary_apply
     assert apply(h, ok, ok, 1, None, None, 0, 7, 4, 256, None) == INVALID        # dtype
     assert apply(h, ok, ok, 1, None, None, 0, 1, -1, 256, None) == INVALID       # tokens
     assert apply(h, ok, ok, 1, None, None, 0, 1, 4, None, None) == INVALID       # positions
     assert apply(h, None, ok, 1, None, None, 0, 1, 4, 256, None) == INVALID      # q
     assert apply(h, ok, None, 1, None, None, 0, 1, 4, 256, None) == INVALID      # q_out
-    assert apply(h, lib.Rows(256, 0, 64), ok, 1, None, None, 0, 1, 4, 256, None) == INVALID   # one row for all tokens
-    assert apply(h, lib.Rows(256, 128, 0), ok, 2, None, None, 0, 1, 4, 256, None) == INVALID  # one row for all heads
+    assert apply(h, rows(256, 0, 64), ok, 1, None, None, 0, 1, 4, 256, None) == INVALID   # one row for all tokens
+    assert apply(h, rows(256, 128, 0), ok, 2, None, None, 0, 1, 4, 256, None) == INVALID  # one row for all heads
     assert apply(h, ok, ok, 1, None, None, 0, 1, 0, None, None) == 0             # no tokens
     assert so.kvk_rotary_destroy(h) == 0
 
 
 def test_prompt_attention_refusals(lib):
     so = lib.load()
-    ok = lib.Rows(256, 1024, 128)
+    rows = lambda *a: ctypes.byref(lib.Rows(*a))  # noqa: E731
+    ok = rows(256, 1024, 128)
 
     def call(q=ok, k=ok, v=ok, n=4, hq=8, hkv=8, d=128, dtype=lib.DTYPE_BF16, cu=256, B=1, scale=1.0, window=0, out=256):
         return so.kvk_prompt_attention(q, k, v, n, hq, hkv, d, dtype, cu, B, scale, window, out, None, None)
@@ -111,8 +113,8 @@ def test_prompt_attention_refusals(lib):
                      (dict(dtype=lib.DTYPE_F32), INVALID), (dict(cu=None), INVALID), (dict(out=None), INVALID), (dict(out=264), INVALID),
                      (dict(scale=0.0), INVALID), (dict(scale=float("inf")), INVALID), (dict(scale=float("nan")), INVALID),
                      (dict(window=-1), INVALID), (dict(n=-1), INVALID), (dict(B=-1), INVALID), (dict(n=2 ** 30), INVALID),
-                     (dict(q=None), INVALID), (dict(k=lib.Rows(264, 1024, 128)), INVALID), (dict(v=lib.Rows(256, 1020, 128)), INVALID),
-                     (dict(v=lib.Rows(256, 1024, 64)), INVALID), (dict(k=lib.Rows(256, -1024, 128)), INVALID)):
+                     (dict(q=None), INVALID), (dict(k=rows(264, 1024, 128)), INVALID), (dict(v=rows(256, 1020, 128)), INVALID),
+                     (dict(v=rows(256, 1024, 64)), INVALID), (dict(k=rows(256, -1024, 128)), INVALID)):
         assert call(**kw) == want, kw
     assert call(n=0, q=None, k=None, v=None, cu=None, out=None) == 0
     assert call(B=0, cu=None) == 0
