@@ -192,30 +192,37 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
     at.t = r;
   }
 
-  // copies: a thread moves piece cc of rows r0 + RS i
+  // Copies: a thread moves piece cc of rows r0 + RS i.  The pages of a tile's
+  // four 16-position groups are looked up a tile ahead: the copies would wait
+  // for the table's latency otherwise.
   constexpr int RS = kThreads / CH, NR = kT / RS;
   const int cc = tid % CH, r0 = tid / CH;
+  int pages[4];
+  auto look_up = [&](const At &x) {
+    const int32_t *tab = pv.table + (int64_t)x.b * pv.max_pages;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int t = x.lo + x.t * kT + 16 * i;
+      pages[i] = t < x.s.len ? tab[t >> pv.page_shift] : -1;
+    }
+  };
   auto copy_tile = [&](const At &x, int stage) {
     uint8_t *ks = sm + stage * 2 * kTile, *vs = ks + kTile;
-    const int32_t *tab = pv.table + (int64_t)x.b * pv.max_pages;
     const int t0 = x.lo + x.t * kT;
-    int last = -1;
-    int64_t base = 0;
-    bool good = false;
+    int64_t base[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool good = (unsigned)pages[i] < (unsigned)pv.n_pages;
+      if (!good && t0 + 16 * i < x.s.len) set_err(pv.err, kErrPage);
+      base[i] = good ? ((((int64_t)pages[i] * pv.Hkv + x.h) << pv.page_shift) + ((t0 + 16 * i) & ((1 << pv.page_shift) - 1))) * RB : -1;
+    }
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
-      const int r = r0 + RS * i, t = t0 + r, pg = t >> pv.page_shift;
-      bool ok = t < x.s.len;
+      const int r = r0 + RS * i;
+      const int64_t at = base[RS * i / 16];
+      const bool ok = at >= 0 && t0 + r < x.s.len;
+      const int64_t off = ok ? at + (r & 15) * RB + 16 * cc : 0;
       const int dst = r * RB + ((cc ^ (r & 7)) << 4);
-      if (ok && pg != last) {
-        const int page = tab[pg];
-        last = pg;
-        good = (unsigned)page < (unsigned)pv.n_pages;
-        if (!good) set_err(pv.err, kErrPage);
-        base = (((int64_t)(good ? page : 0) * pv.Hkv + x.h) << pv.page_shift) * RB;
-      }
-      ok = ok && good;
-      const int64_t off = ok ? base + (int64_t)(t & ((1 << pv.page_shift) - 1)) * RB + 16 * cc : 0;
       cp_async16(ks + dst, pv.k + off, ok);
       cp_async16(vs + dst, pv.v + off, ok);
     }
@@ -224,10 +231,14 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
   // the run's tiles are copied ahead of their use
   At ahead = at;
   int64_t w_ahead = w0;
+  look_up(ahead);
   auto fetch = [&](int stage) {
     if (w_ahead < w1) {
       copy_tile(ahead, stage);
-      if (++w_ahead < w1 && ++ahead.t >= ahead.nt) next_unit(ahead);
+      if (++w_ahead < w1) {
+        if (++ahead.t >= ahead.nt) next_unit(ahead);
+        look_up(ahead);
+      }
     }
     cp_async_commit();
   };

@@ -151,14 +151,22 @@ class Rotary:
             hq = q.shape[1]
             shape = (n, hq, d)
             rq = _rows(q, "q", dtype, index, shape)
-            q_out = _new_like(q, stream) if out is None else out[0]
-            oq = _rows(q_out, "q_out", dtype, index, shape)
+            if out is None:
+                q_out = _new_like(q, stream)
+                oq = _pack_rows(q_out.data_ptr(), hq * d, d)
+            else:
+                q_out = out[0]
+                oq = _rows(q_out, "q_out", dtype, index, shape)
         if k is not None:
             hk = k.shape[1]
             shape = (n, hk, d)
             rk = _rows(k, "k", dtype, index, shape)
-            k_out = _new_like(k, stream) if out is None else out[1]
-            ok = _rows(k_out, "k_out", dtype, index, shape)
+            if out is None:
+                k_out = _new_like(k, stream)
+                ok = _pack_rows(k_out.data_ptr(), hk * d, d)
+            else:
+                k_out = out[1]
+                ok = _rows(k_out, "k_out", dtype, index, shape)
         _call(index, stream, self._apply, self.handle, rq, oq, hq, rk, ok, hk, code, n, self._positions(positions, n, index))
         return q_out, k_out
 
@@ -253,7 +261,9 @@ class PagedCache:
             rq = _rows(q, "q", dtype, index, shape)
             if q_out is None:
                 q_out = _new_like(q, stream)
-            ro = _rows(q_out, "q_out", dtype, index, shape)
+                ro = _pack_rows(q_out.data_ptr(), shape[1] * shape[2], shape[2])
+            else:
+                ro = _rows(q_out, "q_out", dtype, index, shape)
         if positions is not None and rotary is None:
             raise ValueError("positions without a rotary")
         pos = 0 if positions is None else rotary._positions(positions, n, index)
