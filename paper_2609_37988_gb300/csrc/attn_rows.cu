@@ -11,9 +11,9 @@
 // the pieces of the others go to the workspace, and the CTA that adds the last
 // one joins them (fixed order, so results do not depend on who is last).
 //
-// A CTA: 4 warps, 16 positions of a tile each.  Tiles arrive in swizzled
-// shared memory by 16-byte cp.async, three in flight (96 KB per CTA at
-// head_dim 128); rows that hold no position arrive as zeros.  S = Q K^T and
+// A CTA: 4 warps, 16 positions of a tile each, and a warp that looks up pages
+// and copies key and value tiles by TMA through a ring (96 KB; each half of a
+// tile is refilled as soon as the four warps have read it).  S = Q K^T and
 // O += P V on mma.m16n8k16 with fp32 accumulation, the softmax online in base
 // 2, each warp with its own maxima and sums; P enters as hi + lo halves, whose
 // products are free beside the copies.
@@ -21,21 +21,24 @@
 // Non-finite values: weight 0 times an infinite value would be NaN, so tiles
 // that some row does not see in full are looked through first, and a warp whose
 // 16 positions have such a value adds them by plain arithmetic, row by row.
+#include <cuda.h>
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 
 #include "common.cuh"
 #include "kernels.h"
 #include "serve.h"
+#include "umma.cuh"
 
 namespace kvk {
 namespace {
 
 constexpr int kT = 64;        // positions per tile
-constexpr int kThreads = 128;
-constexpr int kStages = 3;
-constexpr int kErrCount = 4, kErrPage = 32;  // KVK_DEVERR_*
+constexpr int kThreads = 128;  // that compute; a warp beside them copies
+constexpr int kErrCount = 4, kErrTimeout = 8, kErrPage = 32;  // KVK_DEVERR_*
+constexpr uint32_t kWaits = 1u << 20;  // polls of up to 2 us each
 constexpr uint32_t kAll = 0xffffffffu;
 
 template <bool BF16>
@@ -100,20 +103,38 @@ struct At {
   Seq s;
 };
 
+struct RowsArgs {
+  CUtensorMap mk, mv;
+  AttnArgs a;
+};
+
+template <int D>
+constexpr int rows_stages() { return D == 128 ? 6 : 12; }  // key and value tiles in turn
+
 template <int D, bool BF16>
-__global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __grid_constant__ RowsArgs ra) {
   constexpr int RB = D * 2;            // bytes of a row
-  constexpr int CH = RB / 16;          // 16-byte pieces of a row
-  constexpr int kTile = kT * RB;       // bytes of a key (or value) tile
-  constexpr int KS = D / 16;
+  constexpr int kTile = kT * RB;       // bytes of a key (or value) tile: boxes of 64 channels
+  constexpr int KS = D / 16, NS = rows_stages<D>();
+  const AttnArgs &a = ra.a;
   extern __shared__ uint8_t sm_raw[];
-  uint8_t *sm = sm_raw + ((128u - (smem_u32(sm_raw) & 127u)) & 127u);
+  uint8_t *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
+  __shared__ uint64_t s_full[NS], s_free[NS];
+  __shared__ int s_abort;
   __shared__ int64_t s_total, s_start;
   __shared__ int s_b, s_last;
   __shared__ float2 s_ml[4][kRowsPerUnit];
   const PagedView &pv = a.pv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
+  if (tid == 0) {
+    for (int i = 0; i < NS; ++i) {
+      mbar_init(&s_full[i], 1);
+      mbar_init(&s_free[i], kThreads / 32);
+    }
+    s_abort = 0;
+    fence_mbar_init();
+  }
   pdl_wait();
 
   // the run of this CTA: tiles [w0, w1) of all
@@ -192,59 +213,82 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
     at.t = r;
   }
 
-  // Copies: a thread moves piece cc of rows r0 + RS i.  The pages of a tile's
-  // four 16-position groups are looked up a tile ahead: the copies would wait
-  // for the table's latency otherwise.
-  constexpr int RS = kThreads / CH, NR = kT / RS;
-  const int cc = tid % CH, r0 = tid / CH;
-  int pages[4];
-  auto look_up = [&](const At &x) {
-    const int32_t *tab = pv.table + (int64_t)x.b * pv.max_pages;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = x.lo + x.t * kT + 16 * i;
-      pages[i] = t < x.s.len ? tab[t >> pv.page_shift] : -1;
-    }
+  volatile int *abort_flag = &s_abort;
+  auto wait = [&](uint64_t *bar, uint32_t parity) {
+    if (mbar_wait_or_abort(bar, parity, kWaits, abort_flag)) return true;
+    *abort_flag = 1;
+    return false;
   };
-  auto copy_tile = [&](const At &x, int stage) {
-    uint8_t *ks = sm + stage * 2 * kTile, *vs = ks + kTile;
-    const int t0 = x.lo + x.t * kT;
-    int64_t base[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool good = (unsigned)pages[i] < (unsigned)pv.n_pages;
-      if (!good && t0 + 16 * i < x.s.len) set_err(pv.err, kErrPage);
-      base[i] = good ? ((((int64_t)pages[i] * pv.Hkv + x.h) << pv.page_shift) + ((t0 + 16 * i) & ((1 << pv.page_shift) - 1))) * RB : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      const int r = r0 + RS * i;
-      const int64_t at = base[RS * i / 16];
-      const bool ok = at >= 0 && t0 + r < x.s.len;
-      const int64_t off = ok ? at + (r & 15) * RB + 16 * cc : 0;
-      const int dst = r * RB + ((cc ^ (r & 7)) << 4);
-      cp_async16(ks + dst, pv.k + off, ok);
-      cp_async16(vs + dst, pv.v + off, ok);
-    }
+  int stage = 0;  // place in the ring and its round's parity
+  uint32_t par = 0;
+  auto next_stage = [&]() {
+    if (++stage == NS) stage = 0, par ^= 1;
   };
 
-  // the run's tiles are copied ahead of their use
-  At ahead = at;
-  int64_t w_ahead = w0;
-  look_up(ahead);
-  auto fetch = [&](int stage) {
-    if (w_ahead < w1) {
-      copy_tile(ahead, stage);
-      if (++w_ahead < w1) {
-        if (++ahead.t >= ahead.nt) next_unit(ahead);
-        look_up(ahead);
+  // a tile in shared memory: per part (the positions of one page, at most 64)
+  // boxes of 64 channels, 128-byte-swizzled rows
+  const int shift = min(pv.page_shift, 6), parts = kT >> shift, box = 128 << shift;
+  auto row_at = [&](int r) { return ((r >> shift) << shift) * RB + (r & ((1 << shift) - 1)) * 128; };
+
+  if (warp == kThreads / 32) {
+    // -- copies: a lane per part of a tile (the positions of one page), its
+    // page looked up a tile ahead; outside the pool reads as zeros
+    auto look_up = [&](const At &x) {
+      const int t = x.lo + x.t * kT + (lane << shift);
+      return lane < parts && t < x.s.len ? pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)] : pv.n_pages;
+    };
+    int page = look_up(at);
+    bool ok = true;
+    for (int64_t w = w0; w < w1 && ok; ++w) {
+      const int t = at.lo + at.t * kT + (lane << shift);
+      const int y = t & ((1 << pv.page_shift) - 1), h = at.h;
+      int now = page;
+      if ((unsigned)now >= (unsigned)pv.n_pages) {
+        if (lane < parts && t < at.s.len) set_err(pv.err, kErrPage);
+        now = pv.n_pages;
+      }
+      if (w + 1 < w1) {
+        if (++at.t >= at.nt) next_unit(at);
+        page = look_up(at);
+      }
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        int got = 1;
+        if (lane == 0) {
+          got = wait(&s_free[stage], par ^ 1);
+          if (got) mbar_expect_tx(&s_full[stage], kTile);
+        }
+        ok = __shfl_sync(kAll, got, 0) != 0;
+        if (!ok) break;
+        if (lane < parts)
+          tma_load_5d(sm + stage * kTile + (lane << shift) * RB, kv ? &ra.mv : &ra.mk, 0, y, 0, h, now, &s_full[stage]);
+        next_stage();
       }
     }
-    cp_async_commit();
-  };
-  for (int i = 0; i < kStages - 1; ++i) fetch(i);
+    if (*abort_flag && lane == 0) {  // the copies in flight land before the CTA ends
+      for (int i = 0; i < NS; ++i) {
+        if (par == 0 && i >= stage) break;
+        mbar_wait(&s_full[i], i < stage ? par : par ^ 1, kWaits);
+      }
+    }
+    if (*abort_flag && lane == 0) set_err(pv.err, kErrTimeout);
+    pdl_trigger();
+    return;
+  }
 
-  int stage = 0;
+  auto bar_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); };
+  auto any_of_all = [&](bool x) {  // a bar_sync too
+    uint32_t r;
+    asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(r)
+                 : "r"(x ? 1u : 0u), "n"(kThreads)
+                 : "memory");
+    return r != 0;
+  };
+  auto release = [&](int at_stage) {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&s_free[at_stage]);
+  };
   for (int64_t w = w0; w < w1;) {
     // a piece: tiles [t_begin, t_end) of one unit
     const int t_begin = at.t, t_end = (int)min((int64_t)at.nt, at.t + (w1 - w));
@@ -274,23 +318,27 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
     for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 
+    int k_stage = 0, v_stage = 0;
     for (; at.t < t_end; ++at.t, ++w) {
-      cp_async_wait<kStages - 2>();
-      __syncthreads();
-      fetch((stage + kStages - 1) % kStages);
-      const uint8_t *ks = sm + stage * 2 * kTile, *vs = ks + kTile;
+      if (!wait(&s_full[stage], par)) break;
+      k_stage = stage;
+      const uint8_t *ks = sm + stage * kTile;
+      next_stage();
       const int t0 = at.lo + at.t * kT + warp * 16;  // the warp's positions
       float s[2][4] = {};
       {
-        const int r = warp * 16 + (lane & 7) + ((lane & 16) >> 1), x = (lane >> 3) & 1;
+        const int r = warp * 16 + (lane & 7) + ((lane & 16) >> 1), x = (lane >> 3) & 1, at_r = row_at(r);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           uint32_t b0, b1, b2, b3;
-          ldmatrix_x4(b0, b1, b2, b3, ks + r * RB + (((2 * k + x) ^ (r & 7)) << 4));
+          ldmatrix_x4(b0, b1, b2, b3, ks + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
           mma<BF16>(s[0], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b0, b1);
           mma<BF16>(s[1], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b2, b3);
         }
       }
+      // the last tile's stages are kept: the warps' states meet there
+      const bool last = at.t + 1 == t_end;
+      if (!last) release(k_stage);
       const bool partial = t0 + 15 > lim_min || t0 < low_max;
       float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
@@ -335,13 +383,17 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
       split2<BF16>(s[0][2], s[0][3], ph[1], pl[1]);
       split2<BF16>(s[1][0], s[1][1], ph[2], pl[2]);
       split2<BF16>(s[1][2], s[1][3], ph[3], pl[3]);
-      const int r = warp * 16 + (lane & 15), x = lane >> 4;
+      if (!wait(&s_full[stage], par)) break;
+      v_stage = stage;
+      const uint8_t *vs = sm + stage * kTile;
+      next_stage();
+      const int r = warp * 16 + (lane & 15), x = lane >> 4, at_r = row_at(r);
       bool plain = false;
       if (partial) {
         bool ok = true;
 #pragma unroll
-        for (int k = 0; k < CH / 2; ++k) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(vs + r * RB + (((2 * k + x) ^ (r & 7)) << 4));
+        for (int k = 0; k < KS; ++k) {
+          const uint4 u = *reinterpret_cast<const uint4 *>(vs + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
           ok = ok && pair_finite<BF16>(u.x) && pair_finite<BF16>(u.y) && pair_finite<BF16>(u.z) && pair_finite<BF16>(u.w);
         }
         plain = __any_sync(kAll, !ok);
@@ -350,7 +402,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
           uint32_t b0, b1, b2, b3;
-          ldmatrix_x4_t(b0, b1, b2, b3, vs + r * RB + (((2 * k + x) ^ (r & 7)) << 4));
+          ldmatrix_x4_t(b0, b1, b2, b3, vs + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
           mma<BF16>(o[2 * k], ph[0], ph[1], ph[2], ph[3], b0, b1);
           mma<BF16>(o[2 * k + 1], ph[0], ph[1], ph[2], ph[3], b2, b3);
           mma<BF16>(o[2 * k], pl[0], pl[1], pl[2], pl[3], b0, b1);
@@ -366,10 +418,10 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
             const float f0 = __shfl_sync(kAll, s[1][2 * i], from), f1 = __shfl_sync(kAll, s[1][2 * i + 1], from);
             p[i] = y & 8 ? (y & 1 ? f1 : f0) : (y & 1 ? e1 : e0);
           }
-          const int rr = warp * 16 + y;
+          const int rr = warp * 16 + y, at_rr = row_at(rr);
 #pragma unroll
           for (int k = 0; k < D / 8; ++k) {
-            const uint32_t u = *reinterpret_cast<const uint32_t *>(vs + rr * RB + ((k ^ (rr & 7)) << 4) + 4 * c);
+            const uint32_t u = *reinterpret_cast<const uint32_t *>(vs + at_rr + (k >> 3) * box + (((k & 7) ^ (rr & 7)) << 4) + 4 * c);
             const float2 f = unpack2<BF16>(u);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
@@ -380,19 +432,19 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
           }
         }
       }
-      stage = (stage + 1) % kStages;
+      if (!last) release(v_stage);
     }
 
-    // the four warps' states are joined in the stage just read: no copy goes
-    // to it before every warp has passed the next tile's barrier
-    float *mg = reinterpret_cast<float *>(sm + (stage + kStages - 1) % kStages * 2 * kTile);  // [4][16][D]
+    // the four warps' states are joined in the two stages just read (keys in an
+    // even one, values in the next)
+    float *mg = reinterpret_cast<float *>(sm + k_stage * kTile);  // [4][16][D]
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       l[i] += __shfl_xor_sync(kAll, l[i], 1);
       l[i] += __shfl_xor_sync(kAll, l[i], 2);
       if (c == 0) s_ml[warp][g + 8 * i] = make_float2(m[i], l[i]);
     }
-    __syncthreads();
+    if (any_of_all(*abort_flag != 0)) break;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const int r = g + 8 * i;
@@ -403,7 +455,7 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
       for (int k = 0; k < D / 8; ++k)
         *reinterpret_cast<float2 *>(mg + ((warp * 16 + r) * D + 8 * k + 2 * c)) = make_float2(o[k][2 * i] * f, o[k][2 * i + 1] * f);
     }
-    __syncthreads();
+    bar_sync();
     const bool whole = t_begin == 0 && t_end == at.nt;
     // where the unit's tiles lie: the CTA that starts it and the last one
     const int64_t u0 = w - t_end;
@@ -443,13 +495,13 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
     }
     if (!whole) {
       __threadfence();
-      __syncthreads();
+      bar_sync();
       if (tid == 0) {
         const bool last = atomicAdd(a.counter + c0, 1) == c1 - c0;
         if (last) a.counter[c0] = 0;  // as the next call expects it
         s_last = last;
       }
-      __syncthreads();
+      bar_sync();
       if (s_last) {
         __threadfence();
         // thread (group, row, 4 channels): the pieces group, group + n, ...;
@@ -482,10 +534,10 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
           if (groups > 1) {
             float4 *sx = reinterpret_cast<float4 *>(mg);
             float2 *sl = reinterpret_cast<float2 *>(sx + kThreads);
-            __syncthreads();  // mg has been read
+            bar_sync();  // mg has been read
             sx[tid] = x;
             sl[tid] = make_float2(M, L);
-            __syncthreads();
+            bar_sync();
             if (tid < vecs)
               for (int i = 1; i < groups; ++i) join(M, L, x, sl[tid + i * vecs].x, sl[tid + i * vecs].y, sx[tid + i * vecs]);
           }
@@ -493,14 +545,23 @@ __global__ void __launch_bounds__(kThreads) attn_rows_kernel(const AttnArgs a) {
         }
       }
     }
+    fence_proxy_async();
+    bar_sync();
+    release(k_stage);
+    release(v_stage);
     if (w < w1 && at.t >= at.nt) next_unit(at);
   }
+  if (*abort_flag && lane == 0) set_err(pv.err, kErrTimeout);
   pdl_trigger();
 }
 
 template <int D, bool BF16>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
-  constexpr int smem = kStages * 2 * kT * D * 2 + 128;
+  constexpr int smem = rows_stages<D>() * kT * D * 2 + 1024;
+  RowsArgs ra;
+  memcpy(&ra.mk, a.wk, sizeof ra.mk);
+  memcpy(&ra.mv, a.wv, sizeof ra.mv);
+  ra.a = a;
   static std::atomic<bool> ready{false};
   if (!ready.load(std::memory_order_relaxed)) {
     const cudaError_t e =
@@ -512,7 +573,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / kT + 2;
   const int64_t tiles = (int64_t)a.pv.B * a.pv.Hkv * ((a.max_new * a.G + kRowsPerUnit - 1) / kRowsPerUnit) * cap;
   const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), tiles);
-  return launch_pdl(attn_rows_kernel<D, BF16>, dim3(grid), dim3(kThreads), smem, st, a);
+  return launch_pdl(attn_rows_kernel<D, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
 }
 
 }  // namespace

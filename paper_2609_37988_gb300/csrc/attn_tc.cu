@@ -26,6 +26,7 @@
 // in any case; dealt to the CTAs back and forth.
 #include <cuda.h>
 #include <math.h>
+#include <string.h>
 
 #include <algorithm>
 
@@ -73,20 +74,6 @@ struct Smem {
 static_assert(Smem<128>::kBytes <= 232448 && Smem<64>::kBytes <= 232448, "shared memory");
 static_assert(Smem<64>::kBytes > 116 * 1024, "one CTA (holding all TMEM columns) per SM");
 
-__device__ __forceinline__ void tma3(void *dst, const CUtensorMap *m, int x, int y, int z, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
-      : "memory");
-}
-__device__ __forceinline__ void tma4(void *dst, const CUtensorMap *m, int x, int y, int z, int w, uint64_t *bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-          smem_u32(dst)),
-      "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(smem_u32(bar))
-      : "memory");
-}
 // 32 columns of this warp's lanes, not waited for
 __device__ __forceinline__ void tmem_ld32_nw(uint32_t taddr, float *v) {
   uint32_t r[32];
@@ -280,14 +267,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       __syncwarp();
       if (lane < (1 + j.two) * NB) {
         const int i = lane / NB, half = lane % NB;
-        tma3(sm + SM::kQ + i * SM::kTile + half * kBox, &t.mq, 64 * half, j.h * G, j.q0 + j.tok0 + i * P, qfull);
+        tma_load_3d(sm + SM::kQ + i * SM::kTile + half * kBox, &t.mq, 64 * half, j.h * G, j.q0 + j.tok0 + i * P, qfull);
       }
       // page of this lane's part of a tile, one tile ahead
-      const int pages = PAGED ? kTcT >> pv.page_shift : 1;
+      const int shift = PAGED ? min(pv.page_shift, 6) : 7, parts = kTcT >> shift;
       const int part = lane / NB, half = lane % NB;
       auto page_of = [&](int jt) {
-        const int pos = j.lo + jt * kTcT + (part << pv.page_shift);
-        if (part >= pages || pos >= j.p0 + j.n) return pv.n_pages;  // outside: reads as zeros
+        const int pos = j.lo + jt * kTcT + (part << shift);
+        if (part >= parts || pos >= j.p0 + j.n) return pv.n_pages;  // outside: reads as zeros
         const int page = pv.table[(int64_t)j.b * pv.max_pages + (pos >> pv.page_shift)];
         if ((unsigned)page < (unsigned)pv.n_pages) return page;
         set_err(pv.err, kErrPage);
@@ -305,11 +292,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           __syncwarp();
           uint8_t *dst = sm + SM::kRing + s * SM::kTile + half * kBox;
           const CUtensorMap *m = kv ? &t.mv : &t.mk;
-          if (lane < pages * NB) {
+          if (lane < parts * NB) {
             if (PAGED)
-              tma4(dst + (part << pv.page_shift) * 128, m, 64 * half, 0, j.h, page, &full[s]);
+              tma_load_4d(dst + (part << shift) * 128, m, 64 * half, (part << shift) & ((1 << pv.page_shift) - 1), j.h, page,
+                          &full[s]);
             else
-              tma3(dst, m, 64 * half, j.q0 + j.lo + jt * kTcT, j.h, &full[s]);
+              tma_load_3d(dst, m, 64 * half, j.q0 + j.lo + jt * kTcT, j.h, &full[s]);
           }
           if (++s == NS) s = 0, ph ^= 1;
         }
@@ -663,16 +651,6 @@ cudaError_t rows_map(CUtensorMap *m, bool bf, void *p, int D, int64_t n1, int64_
                                  strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
-cudaError_t pages_map(CUtensorMap *m, bool bf, const PagedView &v, void *p) {
-  const uint64_t page = 1ull << v.page_shift, row = (uint64_t)v.D * 2;
-  const uint64_t dims[4] = {(uint64_t)v.D, page, (uint64_t)v.Hkv, (uint64_t)v.n_pages};
-  const uint64_t strides[3] = {row, row * page, row * page * v.Hkv};
-  const uint32_t box[4] = {64, (uint32_t)page, 1, 1}, one[4] = {1, 1, 1, 1};
-  return encode_tensor_map_tiled(m, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, p, dims,
-                                 strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-}
-
 template <int D, bool BF16, bool PAGED>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   static std::atomic<bool> ready{false};
@@ -687,10 +665,13 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   t.P = kTcT / a.G;
   const int N = a.pv.n_tokens;
   e = rows_map(&t.mq, BF16, a.q.p, D, a.Hq, a.q.hs, N, a.q.ts, a.G, t.P);
-  if (e == cudaSuccess)
-    e = PAGED ? pages_map(&t.mk, BF16, a.pv, a.pv.k) : rows_map(&t.mk, BF16, a.k.p, D, N, a.k.ts, a.pv.Hkv, a.k.hs, kTcT, 1);
-  if (e == cudaSuccess)
-    e = PAGED ? pages_map(&t.mv, BF16, a.pv, a.pv.v) : rows_map(&t.mv, BF16, a.v.p, D, N, a.v.ts, a.pv.Hkv, a.v.hs, kTcT, 1);
+  if (PAGED) {
+    memcpy(&t.mk, a.mk, sizeof t.mk);
+    memcpy(&t.mv, a.mv, sizeof t.mv);
+  } else {
+    if (e == cudaSuccess) e = rows_map(&t.mk, BF16, a.k.p, D, N, a.k.ts, a.pv.Hkv, a.k.hs, kTcT, 1);
+    if (e == cudaSuccess) e = rows_map(&t.mv, BF16, a.v.p, D, N, a.v.ts, a.pv.Hkv, a.v.hs, kTcT, 1);
+  }
   if (e != cudaSuccess) return e;
   // at most so many jobs: every sequence's last one may be a partial one
   const int64_t jobs = (int64_t)a.pv.Hkv * (N / (2 * t.P) + std::min(a.pv.B, N));
@@ -704,6 +685,20 @@ cudaError_t launch_src(const AttnArgs &a, cudaStream_t st) {
 }
 
 }  // namespace
+
+// [pages, KV heads, slots, D] as boxes of up to 64 slots x 64 channels, or
+// (`whole`) x all channels, 64 at a time one behind another
+cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, bool whole) {
+  const uint64_t row = (uint64_t)D * 2, P = (uint64_t)page, H = (uint64_t)Hkv, N = (uint64_t)n_pages;
+  const uint64_t dims4[4] = {(uint64_t)D, P, H, N}, strides4[3] = {row, row * P, row * P * H};
+  const uint64_t dims5[5] = {64, P, (uint64_t)D / 64, H, N}, strides5[4] = {row, 128, row * P, row * P * H};
+  const uint32_t rows = (uint32_t)std::min(page, 64);
+  const uint32_t box4[4] = {64, rows, 1, 1}, box5[5] = {64, rows, (uint32_t)D / 64, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  return encode_tensor_map_tiled(out, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, whole ? 5 : 4,
+                                 pool, whole ? dims5 : dims4, whole ? strides5 : strides4, whole ? box5 : box4, one,
+                                 CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                 CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
 
 cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st) {
   if (a.pv.B == 0 || a.pv.n_tokens == 0) return cudaSuccess;

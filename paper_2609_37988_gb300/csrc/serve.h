@@ -51,10 +51,12 @@ struct AttnArgs {
   void *out;              // [n_tokens, Hq, D]
   int Hq, G, window, max_new;
   float sig_log2;
+  const void *mk, *mv, *wk, *wv;  // the pages' tensor maps (host memory, 128 bytes each): halves, whole rows
   float *part;            // partial results, kPartSlots of rows_part() floats
   int32_t *counter;       // zero between calls
   int sms;
 };
+cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, bool whole);
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
 cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st);
 // CTAs that a split launch may use at most, and the partial slots of each

@@ -25,9 +25,14 @@ struct kvk_rotary {
   int head_dim;
 };
 
+struct PageMap {
+  alignas(64) uint8_t bytes[128];
+};
+
 struct kvk_paged {
   kvk_paged_desc d;
   std::vector<uint8_t *> k, v;
+  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys, values, both again in whole rows
   uint8_t *ws;
   int device, sms, page_shift;
 };
@@ -261,6 +266,7 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
       p->k.push_back(static_cast<uint8_t *>(k_pages[l]));
       p->v.push_back(static_cast<uint8_t *>(v_pages[l]));
     }
+    p->maps.resize((size_t)desc->n_layers * 4);
   } catch (const std::bad_alloc &) {
     delete p;
     return fail(KVK_ERR_INVALID_ARG, "out of host memory");
@@ -272,6 +278,14 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
   if (e != cudaSuccess) {
     delete p;
     return kvk_internal_cuda_error(e, "querying the device");
+  }
+  const bool bf = desc->dtype == KVK_DTYPE_BF16;
+  for (int i = 0; i < desc->n_layers * 4 && e == cudaSuccess; ++i)
+    e = make_pages_map(p->maps[i].bytes, bf, i & 1 ? p->v[i / 4] : p->k[i / 4], desc->head_dim, desc->page_size, desc->n_kv_heads,
+                       desc->n_pages, (i & 2) != 0);
+  if (e != cudaSuccess) {
+    delete p;
+    return kvk_internal_cuda_error(e, "encoding the pages' tensor maps");
   }
   *out = p;
   return KVK_OK;
@@ -348,6 +362,11 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.counter = reinterpret_cast<int32_t *>(p->ws + w.counter);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
+  const PageMap *maps = &p->maps[(size_t)layer * 4];
+  a.mk = maps[0].bytes;
+  a.mv = maps[1].bytes;
+  a.wk = maps[2].bytes;
+  a.wv = maps[3].bytes;
   const cudaError_t e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;
