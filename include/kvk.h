@@ -551,8 +551,8 @@ typedef struct kvk_paged kvk_paged;
 /* The batch of a call; device pointers.  lengths count the positions held with
  * the new tokens: token j of sequence b's n_b new ones sits at position
  * lengths[b] - n_b + j.  table [batch, max_pages]: sequence b's position t is
- * slot t % page_size of page table[b][t / page_size]; entries from its last
- * page on are not read. */
+ * slot t % page_size of page table[b][t / page_size]; entries behind its last
+ * page are not read.  max_pages * page_size: at most 2^26. */
 typedef struct {
   const int32_t *cu_new;   /* [batch + 1], not decreasing, within [0, n_tokens] */
   const int32_t *lengths;  /* [batch] */

@@ -3,20 +3,24 @@
 //
 // Query j of sequence b sits at position p = len_b - n_b + j and sees
 // positions max(0, p - window + 1) .. p; head h reads KV head h / G.  Rows
-// r = j G + (head in its group) of a (sequence, KV head) go in units of 16, so
-// that a key or value byte is read once for all of them.  A unit's positions
-// go in tiles of 64; the tiles of all units, one behind another, are cut into
-// equal runs, one per CTA (two CTAs per SM are resident), whatever the
-// sequences' lengths are.  A unit that a run covers whole is written at once;
-// the pieces of the others go to the workspace, and the CTA that adds the last
-// one joins them (fixed order, so results do not depend on who is last).
+// r = j G + (head in its group) of a (sequence, KV head) go in units of 8 or 16,
+// so that a key or value byte is read once for all of them; with small pages a
+// unit takes HC = 2 or 4 KV heads side by side, whose parts of a page adjoin,
+// so that a copy is 16 KB either way.  A unit's positions go in tiles of
+// 64 / HC; the tiles of all units, one behind another, are cut into equal runs,
+// one per CTA (two CTAs per SM are resident), whatever the sequences' lengths
+// are.  A unit that a run covers whole is written at once; the pieces of the
+// others go to the workspace, with a note of where they lie, and a second kernel
+// joins them, a CTA per row (one CTA per unit that did it behind its own run
+// took 50 us for 152 pieces of 20 rows).
 //
-// A CTA: 4 warps, 16 positions of a tile each, and a warp that looks up pages
-// and copies key and value tiles by TMA through a ring (96 KB; each half of a
-// tile is refilled as soon as the four warps have read it).  S = Q K^T and
-// O += P V on mma.m16n8k16 with fp32 accumulation, the softmax online in base
-// 2, each warp with its own maxima and sums; P enters as hi + lo halves, whose
-// products are free beside the copies.
+// A CTA: 4 warps, 16 positions of one head's tile each, and a warp that looks
+// up pages and copies key and value tiles by TMA through a ring (96 KB; each
+// half of a tile is refilled as soon as the four warps have read it).  Scores
+// and results are computed transposed, S^T = K Q^T and O^T += V^T P^T on
+// mma.m16n8k16 (positions and channels in the 16, query rows in the 8: few rows
+// waste little), fp32 accumulation, the softmax online in base 2, each warp with
+// its own maxima and sums; P enters as hi + lo halves.
 //
 // Non-finite values: weight 0 times an infinite value would be NaN, so tiles
 // that some row does not see in full are looked through first, and a warp whose
@@ -35,9 +39,10 @@
 namespace kvk {
 namespace {
 
-constexpr int kT = 64;        // positions per tile
+constexpr int kT = 64;        // positions x KV heads of a tile
 constexpr int kThreads = 128;  // that compute; a warp beside them copies
 constexpr int kErrCount = 4, kErrTimeout = 8, kErrPage = 32;  // KVK_DEVERR_*
+constexpr int kMinShare = 4;   // tiles of a run at least
 constexpr uint32_t kWaits = 1u << 20;  // polls of up to 2 us each
 constexpr uint32_t kAll = 0xffffffffu;
 
@@ -65,10 +70,11 @@ struct Seq {
 };
 __device__ __forceinline__ Seq load_seq(const PagedView &v, int b, int max_new) {
   Seq s;
-  const int c0 = min(max(v.cu[b], 0), v.n_tokens);
-  s.n = min(max(v.cu[b + 1], c0), v.n_tokens) - c0;
+  const int e0 = v.cu[b], e1 = v.cu[b + 1], len = v.lens[b];
+  const int c0 = min(max(e0, 0), v.n_tokens);
+  s.n = min(max(e1, c0), v.n_tokens) - c0;
   s.q0 = c0;
-  s.len = max(v.lens[b], 0);
+  s.len = max(len, 0);
   const int64_t cap = (int64_t)v.max_pages << v.page_shift;
   if (s.n > max_new || s.len > cap) {
     set_err(v.err, kErrCount);
@@ -77,28 +83,42 @@ __device__ __forceinline__ Seq load_seq(const PagedView &v, int b, int max_new) 
   }
   return s;
 }
-// Positions [lo, hi) that the rows of unit block rb see (lo a multiple of the
-// tile; at least one tile, so that rows that see nothing get their zeros).
-__device__ __forceinline__ void block_range(const Seq &s, int G, int window, int rb, int &lo, int &nt) {
-  const int first = s.len - s.n + rb * kRowsPerUnit / G;
-  const int last = s.len - s.n + min(s.n * G - 1, rb * kRowsPerUnit + kRowsPerUnit - 1) / G;
-  lo = max(0, first - window + 1) / kT * kT;
-  nt = max(1, (last + kT - lo) / kT);
+// Positions from lo (a multiple of the tile) in nt tiles that the rows of unit
+// block rb (RU rows) see; at least one tile, so that rows that see nothing get
+// their zeros.
+template <int RU>
+__device__ __forceinline__ void block_range(const Seq &s, const AttnArgs &a, int rb, int &lo, int &nt) {
+  int first = s.len - s.n, last = s.len - 1;
+  if (s.n * a.G > RU) {
+    last = first + min(s.n * a.G - 1, rb * RU + RU - 1) / a.G;
+    first += rb * RU / a.G;
+  }
+  const int sh = a.pt_shift;
+  lo = max(0, first - a.window + 1) >> sh << sh;
+  nt = max(1, (last + (1 << sh) - lo) >> sh);
 }
-__device__ __forceinline__ int row_blocks(const Seq &s, int G) { return (s.n * G + kRowsPerUnit - 1) / kRowsPerUnit; }
-__device__ __forceinline__ int seq_tiles(const Seq &s, int G, int window) {
+template <int RU>
+__device__ __forceinline__ int row_blocks(const Seq &s, int G) { return (s.n * G + RU - 1) / RU; }
+// Tiles of a sequence, per unit of heads.
+template <int RU>
+__device__ __forceinline__ int seq_tiles(const Seq &s, const AttnArgs &a) {
   int sum = 0;
-  for (int rb = 0; rb < row_blocks(s, G); ++rb) {
+  for (int rb = 0; rb < row_blocks<RU>(s, a.G); ++rb) {
     int lo, nt;
-    block_range(s, G, window, rb, lo, nt);
+    block_range<RU>(s, a, rb, lo, nt);
     sum += nt;
   }
   return sum;
 }
+// x / y, in 32 bits where they do (a 64-bit division takes 500 cycles)
+__device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
+  if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+  return x / y;
+}
 
 // A place in the list of tiles.
 struct At {
-  int b, h, rb, t;   // sequence, KV head, row block, tile of the unit
+  int b, h, rb, t;   // sequence, unit of KV heads, row block, tile of the unit
   int lo, nt;        // the unit's first position and tiles
   Seq s;
 };
@@ -108,26 +128,100 @@ struct RowsArgs {
   AttnArgs a;
 };
 
+// 4 channels (v-th four) of row r of a (sequence, KV head), divided by its sum.
+// A row before position 0 sees nothing and gives zeros.
+template <int D, bool BF16>
+__device__ __forceinline__ void store_row(const AttnArgs &a, int q0, int p_base, int head, int r, int v, float4 x, float L) {
+  const int j = r / a.G;
+  const bool sees = p_base + j >= 0;
+  const float inv = sees ? 1.f / L : 0.f;
+  if (!sees) x = make_float4(0.f, 0.f, 0.f, 0.f);
+  uint8_t *dst = static_cast<uint8_t *>(a.out) + 2 * (((int64_t)(q0 + j) * a.Hq + head * a.G + (r - j * a.G)) * D + 4 * v);
+  *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<BF16>(x.x * inv, x.y * inv), pack2<BF16>(x.z * inv, x.w * inv));
+}
+
+// Joins the pieces of the units that the first kernel cut.  A thread takes 4
+// channels of a row; a CTA has one row, its groups of threads every
+// `groups`-th piece and meeting in shared memory, where there are rows for no
+// more (long contexts of few sequences), else a row per group.  The last CTA
+// clears the list for the next call.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a) {
+  constexpr int V = D / 4, groups = kThreads / V, U = 8;
+  __shared__ float4 sx[kThreads];
+  __shared__ float2 sl[kThreads];
+  const int tid = threadIdx.x, v = tid % V, grp = tid / V;
+  const int rows = a.hc * a.rows;
+  pdl_wait();
+  const int n = *reinterpret_cast<volatile int *>(&a.list->n) * rows;
+  const bool wide = n <= (int)gridDim.x;
+  const int step = wide ? groups : 1;
+  for (int item = wide ? blockIdx.x : blockIdx.x * groups + grp; item < n; item += gridDim.x * (wide ? 1 : groups)) {
+    const RowsSplit u = a.list->unit[item / rows];
+    const int y = item % rows, c0 = u.first, hd = y / u.rows, r = y - hd * u.rows;
+    if (y >= a.hc * u.rows) continue;
+    float M = -INFINITY, L = 0.f;
+    float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int p0 = c0 + (wide ? grp : 0); p0 <= u.last; p0 += U * step) {
+      float4 z[U];
+      float pm[U], pl[U];
+#pragma unroll
+      for (int i = 0; i < U; ++i) {
+        const int p = p0 + i * step;
+        const float *src = a.part + ((int64_t)(2 * p + (p == c0)) * kRowsMaxHeads + hd) * rows_part(D);
+        const bool in = p <= u.last;
+        z[i] = in ? __ldcg(reinterpret_cast<const float4 *>(src + r * D + 4 * v)) : make_float4(0.f, 0.f, 0.f, 0.f);
+        pm[i] = in ? __ldcg(src + kRowsPerUnit * D + r) : -INFINITY;
+        pl[i] = in ? __ldcg(src + kRowsPerUnit * (D + 1) + r) : 0.f;
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) join(M, L, x, pm[i], pl[i], z[i]);
+    }
+    if (wide) {
+      sx[tid] = x;
+      sl[tid] = make_float2(M, L);
+      __syncthreads();
+      if (grp > 0) break;
+#pragma unroll
+      for (int i = 1; i < groups; ++i) join(M, L, x, sl[tid + i * V].x, sl[tid + i * V].y, sx[tid + i * V]);
+    }
+    store_row<D, BF16>(a, u.q0, u.p_base, u.head + hd, u.row0 + r, v, x, L);
+  }
+  pdl_trigger();
+  // every CTA has read n before it counts itself
+  __syncthreads();
+  if (tid == 0) {
+    __threadfence();
+    if (atomicInc(&a.list->done, gridDim.x - 1) == gridDim.x - 1) a.list->n = 0;
+  }
+}
+
 template <int D>
 constexpr int rows_stages() { return D == 128 ? 6 : 12; }  // key and value tiles in turn
 
-template <int D, bool BF16>
+// NB: query rows of a unit in blocks of 8
+template <int D, int NB, bool BF16>
 __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __grid_constant__ RowsArgs ra) {
   constexpr int RB = D * 2;            // bytes of a row
-  constexpr int kTile = kT * RB;       // bytes of a key (or value) tile: boxes of 64 channels
-  constexpr int KS = D / 16, NS = rows_stages<D>();
+  constexpr int kTile = kT * RB;       // bytes of a key (or value) tile
+  constexpr int KS = D / 16, NS = rows_stages<D>(), RU = 8 * NB;
   const AttnArgs &a = ra.a;
   extern __shared__ uint8_t sm_raw[];
   uint8_t *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
   __shared__ uint64_t s_full[NS], s_free[NS];
-  __shared__ int s_abort;
-  __shared__ int64_t s_total, s_start;
-  __shared__ int s_b, s_last;
-  __shared__ float2 s_ml[4][kRowsPerUnit];
+  __shared__ int s_abort, s_mine, s_share;
+  __shared__ At s_at;
+  __shared__ float2 s_ml[4][RU];
   const PagedView &pv = a.pv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int g = lane >> 2, c = lane & 3;
-  if (tid == 0) {
+  const int HC = a.hc, units = pv.Hkv / HC;
+  const int per_head = 4 / HC, hh = warp / per_head, sub = warp % per_head;  // the warp's head and positions
+  if (tid == 128) {
+    prefetch_tensor_map(&ra.mk);
+    prefetch_tensor_map(&ra.mv);
+  }
+  if (tid == 64) {
     for (int i = 0; i < NS; ++i) {
       mbar_init(&s_full[i], 1);
       mbar_init(&s_free[i], kThreads / 32);
@@ -137,55 +231,12 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
   }
   pdl_wait();
 
-  // the run of this CTA: tiles [w0, w1) of all
-  if (warp == 0) {
-    int64_t total = 0;
-    for (int b = lane; b < pv.B; b += 32) total += (int64_t)pv.Hkv * seq_tiles(load_seq(pv, b, a.max_new), a.G, a.window);
-    for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
-    const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
-    const int64_t w0 = share * blockIdx.x;
-    int64_t before = 0;
-    int found = -1;
-    if (w0 < total) {
-      for (int b0 = 0; b0 < pv.B && found < 0; b0 += 32) {
-        int64_t x = 0;
-        if (b0 + lane < pv.B) x = (int64_t)pv.Hkv * seq_tiles(load_seq(pv, b0 + lane, a.max_new), a.G, a.window);
-        int64_t sum = x;
-        for (int o = 1; o < 32; o <<= 1) {
-          const int64_t y = __shfl_up_sync(kAll, sum, o);
-          if (lane >= o) sum += y;
-        }
-        const uint32_t past = __ballot_sync(kAll, before + sum > w0);
-        if (past) {
-          const int f = __ffs(past) - 1;
-          found = b0 + f;
-          before += __shfl_sync(kAll, sum - x, f);
-        } else {
-          before += __shfl_sync(kAll, sum, 31);
-        }
-      }
-    }
-    if (lane == 0) {
-      s_total = total;
-      s_b = found;
-      s_start = before;
-    }
-  }
-  __syncthreads();
-  const int64_t total = s_total;
-  const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)1);
-  const int64_t w0 = share * blockIdx.x, w1 = min(total, w0 + share);
-  if (w0 >= w1) {
-    pdl_trigger();
-    return;
-  }
-
-  auto settle = [&](At &x) { block_range(x.s, a.G, a.window, x.rb, x.lo, x.nt); };
+  auto settle = [&](At &x) { block_range<RU>(x.s, a, x.rb, x.lo, x.nt); };
   auto next_unit = [&](At &x) {
     x.t = 0;
-    if (++x.rb >= row_blocks(x.s, a.G)) {
+    if (++x.rb >= row_blocks<RU>(x.s, a.G)) {
       x.rb = 0;
-      if (++x.h >= pv.Hkv) {
+      if (++x.h >= units) {
         x.h = 0;
         do {
           if (++x.b >= pv.B) return;  // behind the last unit: not used again
@@ -195,23 +246,70 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     }
     settle(x);
   };
-  At at;
-  {
-    at.b = s_b;
-    at.s = load_seq(pv, at.b, a.max_new);
-    int64_t off = w0 - s_start;
-    const int per = seq_tiles(at.s, a.G, a.window);
-    at.h = (int)(off / per);
-    int r = (int)(off - (int64_t)at.h * per);
-    at.rb = 0;
-    settle(at);
-    while (r >= at.nt) {
-      r -= at.nt;
-      ++at.rb;
-      settle(at);
+
+  // the run of this CTA: `mine` tiles from s_at on
+  if (warp == 0) {
+    int64_t before = 0, total = 0;  // tiles of the sequences before this lane's chunk
+    Seq sq = {0, 0, 0};
+    int per = 0;
+    auto chunk = [&](int b0) {
+      const bool in = b0 + lane < pv.B;
+      if (in) sq = load_seq(pv, b0 + lane, a.max_new);
+      per = in ? seq_tiles<RU>(sq, a) : 0;
+      uint32_t x = per;  // 32 sequences of at most 2^22 tiles and 8 row blocks each
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(kAll, x, o);
+        if (lane >= o) x += y;
+      }
+      return (int64_t)units * x;  // up to and with this lane's sequence
+    };
+    int64_t upto = 0;
+    for (int b0 = 0; b0 < pv.B; b0 += 32) {
+      upto = chunk(b0);
+      total += __shfl_sync(kAll, upto, 31);
     }
-    at.t = r;
+    const int64_t share = max(div_pos(total + gridDim.x - 1, gridDim.x), (int64_t)kMinShare);
+    const int64_t w0 = share * blockIdx.x;
+    if (w0 < total) {
+      for (int b0 = 0;; b0 += 32) {
+        if (pv.B > 32) upto = chunk(b0);
+        const uint32_t past = __ballot_sync(kAll, before + upto > w0);
+        if (past) {
+          if (lane == __ffs(past) - 1) {
+            At x;
+            x.b = b0 + lane;
+            x.s = sq;
+            const int64_t off = w0 - (before + upto - (int64_t)units * per);
+            x.h = (int)div_pos(off, per);
+            int r = (int)(off - (int64_t)x.h * per);
+            x.rb = 0;
+            settle(x);
+            while (r >= x.nt) {
+              r -= x.nt;
+              ++x.rb;
+              settle(x);
+            }
+            x.t = r;
+            s_at = x;
+          }
+          break;
+        }
+        before += __shfl_sync(kAll, upto, 31);
+      }
+    }
+    if (lane == 0) {
+      s_mine = w0 < total ? (int)min(share, total - w0) : 0;
+      s_share = (int)min(share, (int64_t)1 << 30);
+    }
   }
+  __syncthreads();
+  const int mine = s_mine;
+  if (mine == 0) {
+    pdl_trigger();
+    return;
+  }
+  At at = s_at;
 
   volatile int *abort_flag = &s_abort;
   auto wait = [&](uint64_t *bar, uint32_t parity) {
@@ -226,28 +324,28 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
   };
 
   // a tile in shared memory: per part (the positions of one page, at most 64)
-  // boxes of 64 channels, 128-byte-swizzled rows
-  const int shift = min(pv.page_shift, 6), parts = kT >> shift, box = 128 << shift;
-  auto row_at = [&](int r) { return ((r >> shift) << shift) * RB + (r & ((1 << shift) - 1)) * 128; };
+  // and KV head boxes of 64 channels, 128-byte-swizzled rows
+  const int pt = 1 << a.pt_shift, shift = a.part_shift, parts = pt >> shift, box = 128 << shift;
+  auto row_at = [&](int r) { return ((r >> shift) * HC + hh) * (RB << shift) + (r & ((1 << shift) - 1)) * 128; };
 
   if (warp == kThreads / 32) {
-    // -- copies: a lane per part of a tile (the positions of one page), its
-    // page looked up a tile ahead; outside the pool reads as zeros
+    // -- copies: a lane per part of a tile, its page looked up a tile ahead;
+    // outside the pool reads as zeros
     auto look_up = [&](const At &x) {
-      const int t = x.lo + x.t * kT + (lane << shift);
+      const int t = x.lo + x.t * pt + (lane << shift);
       return lane < parts && t < x.s.len ? pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)] : pv.n_pages;
     };
     int page = look_up(at);
     bool ok = true;
-    for (int64_t w = w0; w < w1 && ok; ++w) {
-      const int t = at.lo + at.t * kT + (lane << shift);
-      const int y = t & ((1 << pv.page_shift) - 1), h = at.h;
+    for (int w = 0; w < mine && ok; ++w) {
+      const int t = at.lo + at.t * pt + (lane << shift);
+      const int y = t & ((1 << pv.page_shift) - 1), h = at.h * HC;
       int now = page;
       if ((unsigned)now >= (unsigned)pv.n_pages) {
         if (lane < parts && t < at.s.len) set_err(pv.err, kErrPage);
         now = pv.n_pages;
       }
-      if (w + 1 < w1) {
+      if (w + 1 < mine) {
         if (++at.t >= at.nt) next_unit(at);
         page = look_up(at);
       }
@@ -261,7 +359,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
         ok = __shfl_sync(kAll, got, 0) != 0;
         if (!ok) break;
         if (lane < parts)
-          tma_load_5d(sm + stage * kTile + (lane << shift) * RB, kv ? &ra.mv : &ra.mk, 0, y, 0, h, now, &s_full[stage]);
+          tma_load_5d(sm + stage * kTile + (lane << shift) * RB * HC, kv ? &ra.mv : &ra.mk, 0, y, 0, h, now, &s_full[stage]);
         next_stage();
       }
     }
@@ -289,111 +387,128 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     __syncwarp();
     if (lane == 0) mbar_arrive(&s_free[at_stage]);
   };
-  for (int64_t w = w0; w < w1;) {
+  // lanes' rows of a 16-position tile: of the keys as the A operand, of the
+  // values as its transpose
+  const int rk = sub * 16 + (lane & 15), xk = lane >> 4, at_k = row_at(rk);
+  const int rv = sub * 16 + (lane & 7) + ((lane & 16) >> 1), xv = (lane >> 3) & 1, at_v = row_at(rv);
+  for (int w = 0; w < mine;) {
     // a piece: tiles [t_begin, t_end) of one unit
-    const int t_begin = at.t, t_end = (int)min((int64_t)at.nt, at.t + (w1 - w));
-    const int R = min(kRowsPerUnit, at.s.n * a.G - at.rb * kRowsPerUnit);
+    const int t_begin = at.t, t_end = min(at.nt, at.t + (mine - w)), w_begin = w;
+    const int row0 = at.rb * RU, R = min(RU, at.s.n * a.G - row0);
     const int p_base = at.s.len - at.s.n;
-    uint32_t qf[KS][4];
-    int lim[2], low[2];
-    bool real[2];
+    // Q^T as the B operand (row 8 nb + g), and the positions that rows
+    // 8 nb + 2 c + e see
+    uint32_t qf[KS][NB][2];
+    int lim[2 * NB], low[2 * NB];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = at.rb * kRowsPerUnit + g + 8 * i, j = r / a.G;
-      real[i] = g + 8 * i < R;
-      lim[i] = real[i] ? p_base + j : -1;
-      low[i] = lim[i] - a.window + 1;
-      const uint8_t *src = a.q.p + 2 * ((int64_t)(at.s.q0 + (real[i] ? j : 0)) * a.q.ts +
-                                        (int64_t)(at.h * a.G + (real[i] ? r - j * a.G : 0)) * a.q.hs);
+    for (int nb = 0; nb < NB; ++nb) {
+      const int r = row0 + 8 * nb + g, j = r / a.G;
+      const bool real = 8 * nb + g < R;
+      const uint8_t *src = a.q.p + 2 * ((int64_t)(at.s.q0 + (real ? j : 0)) * a.q.ts +
+                                        (int64_t)((at.h * HC + hh) * a.G + (real ? r - j * a.G : 0)) * a.q.hs);
 #pragma unroll
       for (int k = 0; k < KS; ++k)
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-          qf[k][2 * x + i] = real[i] ? *reinterpret_cast<const uint32_t *>(src + 32 * k + 16 * x + 4 * c) : 0u;
-    }
-    const int lim_min = p_base + at.rb * kRowsPerUnit / a.G;                     // of the first row
-    const int low_max = p_base + (at.rb * kRowsPerUnit + R - 1) / a.G - a.window + 1;  // of the last
-    float o[D / 8][4];
+          qf[k][nb][x] = real ? *reinterpret_cast<const uint32_t *>(src + 32 * k + 16 * x + 4 * c) : 0u;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      for (int e = 0; e < 2; ++e) {
+        const int rr = 8 * nb + 2 * c + e;
+        lim[2 * nb + e] = rr < R ? p_base + (row0 + rr) / a.G : -1;
+        low[2 * nb + e] = lim[2 * nb + e] - a.window + 1;
+      }
+    }
+    const int lim_min = p_base + row0 / a.G;                          // of the first row
+    const int low_max = p_base + (row0 + R - 1) / a.G - a.window + 1;  // of the last
+    float o[NB][KS][4];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int i = 0; i < KS; ++i) o[nb][i][0] = o[nb][i][1] = o[nb][i][2] = o[nb][i][3] = 0.f;
+    float m[2 * NB], l[2 * NB];
+#pragma unroll
+    for (int i = 0; i < 2 * NB; ++i) m[i] = -INFINITY, l[i] = 0.f;
 
     int k_stage = 0, v_stage = 0;
     for (; at.t < t_end; ++at.t, ++w) {
       if (!wait(&s_full[stage], par)) break;
       k_stage = stage;
-      const uint8_t *ks = sm + stage * kTile;
+      const uint8_t *ks = sm + stage * kTile + at_k;
       next_stage();
-      const int t0 = at.lo + at.t * kT + warp * 16;  // the warp's positions
-      float s[2][4] = {};
-      {
-        const int r = warp * 16 + (lane & 7) + ((lane & 16) >> 1), x = (lane >> 3) & 1, at_r = row_at(r);
+      const int t0 = at.lo + at.t * pt + sub * 16;  // the warp's positions
+      // two chains of products (even and odd k-steps): one is latency
+      float s[NB][4] = {}, s1[NB][4] = {};
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          uint32_t b0, b1, b2, b3;
-          ldmatrix_x4(b0, b1, b2, b3, ks + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
-          mma<BF16>(s[0], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b0, b1);
-          mma<BF16>(s[1], qf[k][0], qf[k][1], qf[k][2], qf[k][3], b2, b3);
-        }
+      for (int k = 0; k < KS; ++k) {
+        uint32_t a0, a1, a2, a3;
+        ldmatrix_x4(a0, a1, a2, a3, ks + (k >> 2) * box + (((2 * (k & 3) + xk) ^ (rk & 7)) << 4));
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) mma<BF16>(k & 1 ? s1[nb] : s[nb], a0, a1, a2, a3, qf[k][nb][0], qf[k][nb][1]);
       }
       // the last tile's stages are kept: the warps' states meet there
       const bool last = at.t + 1 == t_end;
       if (!last) release(k_stage);
       const bool partial = t0 + 15 > lim_min || t0 < low_max;
-      float mx[2] = {-INFINITY, -INFINITY};
+      float mx[2 * NB];
+      bool more = false;
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = e >> 1, t = t0 + 8 * nb + 2 * c + (e & 1);
-          float x = s[nb][e] * a.sig_log2;
-          if (partial && (t > lim[i] || t < low[i])) x = -INFINITY;
-          s[nb][e] = x;
-          mx[i] = fmaxf(mx[i], x);
+        for (int e = 0; e < 2; ++e) {
+          const int i = 2 * nb + e;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const int t = t0 + g + 8 * y;
+            float x = (s[nb][2 * y + e] + s1[nb][2 * y + e]) * a.sig_log2;
+            if (partial && (t > lim[i] || t < low[i])) x = -INFINITY;
+            s[nb][2 * y + e] = x;
+          }
+          mx[i] = fmaxf(s[nb][e], s[nb][2 + e]);
+          more = more || mx[i] > m[i];
         }
+      if (__any_sync(kAll, more)) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(kAll, mx[i], 1));
-        mx[i] = fmaxf(mx[i], __shfl_xor_sync(kAll, mx[i], 2));
-      }
-      if (__any_sync(kAll, mx[0] > m[0] || mx[1] > m[1])) {
+        for (int i = 0; i < 2 * NB; ++i) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+          for (int y = 4; y < 32; y <<= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(kAll, mx[i], y));
           const float mn = fmaxf(m[i], mx[i]);
           const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - mn);
           if (m[i] != mn) {
             l[i] *= f;
 #pragma unroll
-            for (int k = 0; k < D / 8; ++k) o[k][2 * i] *= f, o[k][2 * i + 1] *= f;
+            for (int k = 0; k < KS; ++k) o[i >> 1][k][i & 1] *= f, o[i >> 1][k][2 + (i & 1)] *= f;
           }
           m[i] = mn;
         }
       }
-      const float ref[2] = {m[0] == -INFINITY ? 0.f : m[0], m[1] == -INFINITY ? 0.f : m[1]};
+      // P^T as the B operand, hi and lo
+      uint32_t ph[NB][2], pl[NB][2];
 #pragma unroll
-      for (int nb = 0; nb < 2; ++nb)
+      for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          s[nb][e] = fast_exp2(s[nb][e] - ref[e >> 1]);
-          l[e >> 1] += s[nb][e];
+          const float ref = m[2 * nb + (e & 1)];
+          s[nb][e] = fast_exp2(s[nb][e] - (ref == -INFINITY ? 0.f : ref));
+          l[2 * nb + (e & 1)] += s[nb][e];
         }
-      // P as the A operand: rows g, g + 8; positions 2c.. of either half
-      uint32_t ph[4], pl[4];
-      split2<BF16>(s[0][0], s[0][1], ph[0], pl[0]);
-      split2<BF16>(s[0][2], s[0][3], ph[1], pl[1]);
-      split2<BF16>(s[1][0], s[1][1], ph[2], pl[2]);
-      split2<BF16>(s[1][2], s[1][3], ph[3], pl[3]);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          uint32_t h, lo;
+          split2<BF16>(s[nb][2 * y], s[nb][2 * y + 1], h, lo);
+          ph[nb][y] = movmatrix_t(h);
+          pl[nb][y] = movmatrix_t(lo);
+        }
+      }
       if (!wait(&s_full[stage], par)) break;
       v_stage = stage;
       const uint8_t *vs = sm + stage * kTile;
       next_stage();
-      const int r = warp * 16 + (lane & 15), x = lane >> 4, at_r = row_at(r);
       bool plain = false;
       if (partial) {
         bool ok = true;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(vs + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
+          const uint4 u = *reinterpret_cast<const uint4 *>(vs + at_k + (k >> 2) * box + (((2 * (k & 3) + xk) ^ (rk & 7)) << 4));
           ok = ok && pair_finite<BF16>(u.x) && pair_finite<BF16>(u.y) && pair_finite<BF16>(u.z) && pair_finite<BF16>(u.w);
         }
         plain = __any_sync(kAll, !ok);
@@ -401,179 +516,156 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
       if (!plain) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          uint32_t b0, b1, b2, b3;
-          ldmatrix_x4_t(b0, b1, b2, b3, vs + at_r + (k >> 2) * box + (((2 * (k & 3) + x) ^ (r & 7)) << 4));
-          mma<BF16>(o[2 * k], ph[0], ph[1], ph[2], ph[3], b0, b1);
-          mma<BF16>(o[2 * k + 1], ph[0], ph[1], ph[2], ph[3], b2, b3);
-          mma<BF16>(o[2 * k], pl[0], pl[1], pl[2], pl[3], b0, b1);
-          mma<BF16>(o[2 * k + 1], pl[0], pl[1], pl[2], pl[3], b2, b3);
+          uint32_t a0, a1, a2, a3;
+          ldmatrix_x4_t(a0, a1, a2, a3, vs + at_v + (k >> 2) * box + (((2 * (k & 3) + xv) ^ (rv & 7)) << 4));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            mma<BF16>(o[nb][k], a0, a1, a2, a3, ph[nb][0], ph[nb][1]);
+            mma<BF16>(o[nb][k], a0, a1, a2, a3, pl[nb][0], pl[nb][1]);
+          }
         }
       } else {
+#pragma unroll 1
         for (int y = 0; y < 16; ++y) {
-          const int from = (lane & ~3) | ((y & 7) >> 1), t = t0 + y;
-          float p[2];
+          const int rr = sub * 16 + y, t = t0 + y;
+          const uint8_t *row = vs + row_at(rr);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const float e0 = __shfl_sync(kAll, s[0][2 * i], from), e1 = __shfl_sync(kAll, s[0][2 * i + 1], from);
-            const float f0 = __shfl_sync(kAll, s[1][2 * i], from), f1 = __shfl_sync(kAll, s[1][2 * i + 1], from);
-            p[i] = y & 8 ? (y & 1 ? f1 : f0) : (y & 1 ? e1 : e0);
-          }
-          const int rr = warp * 16 + y, at_rr = row_at(rr);
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int k = 0; k < D / 8; ++k) {
-            const uint32_t u = *reinterpret_cast<const uint32_t *>(vs + at_rr + (k >> 3) * box + (((k & 7) ^ (rr & 7)) << 4) + 4 * c);
-            const float2 f = unpack2<BF16>(u);
+            for (int e = 0; e < 2; ++e) {
+              const float p0 = __shfl_sync(kAll, s[nb][e], (y & 7) * 4 + c), p1 = __shfl_sync(kAll, s[nb][2 + e], (y & 7) * 4 + c);
+              const float p = y & 8 ? p1 : p0;
+              if (t <= lim[2 * nb + e] && t >= low[2 * nb + e]) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-              if (t <= lim[i] && t >= low[i]) {
-                o[k][2 * i] += p[i] * f.x;
-                o[k][2 * i + 1] += p[i] * f.y;
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                  for (int z = 0; z < 2; ++z) {
+                    const uint16_t u = *reinterpret_cast<const uint16_t *>(
+                        row + (k >> 2) * box + (((2 * (k & 3) + z) ^ (rr & 7)) << 4) + 2 * g);
+                    o[nb][k][2 * z + e] += p * unpack2<BF16>(u).x;
+                  }
               }
-          }
+            }
         }
       }
       if (!last) release(v_stage);
     }
 
-    // the four warps' states are joined in the two stages just read (keys in an
-    // even one, values in the next)
-    float *mg = reinterpret_cast<float *>(sm + k_stage * kTile);  // [4][16][D]
+    // The warps' states meet in the two stages just read (keys in an even one,
+    // values in the next), channels of row r turned by 8 (r / 2) against bank
+    // conflicts.
+    float *mg = reinterpret_cast<float *>(sm + k_stage * kTile);  // [4][RU][D]
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] += __shfl_xor_sync(kAll, l[i], 1);
-      l[i] += __shfl_xor_sync(kAll, l[i], 2);
-      if (c == 0) s_ml[warp][g + 8 * i] = make_float2(m[i], l[i]);
+    for (int i = 0; i < 2 * NB; ++i) {
+#pragma unroll
+      for (int y = 4; y < 32; y <<= 1) l[i] += __shfl_xor_sync(kAll, l[i], y);
+      if (g == 0) s_ml[warp][8 * (i >> 1) + 2 * c + (i & 1)] = make_float2(m[i], l[i]);
     }
     if (any_of_all(*abort_flag != 0)) break;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int r = g + 8 * i;
-      const float M = fmaxf(fmaxf(s_ml[0][r].x, s_ml[1][r].x), fmaxf(s_ml[2][r].x, s_ml[3][r].x));
-      const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - M);
+    for (int i = 0; i < 2 * NB; ++i) {
+      const int r = 8 * (i >> 1) + 2 * c + (i & 1);
+      float M = m[i];
+      for (int y = 0; y < per_head; ++y) M = fmaxf(M, s_ml[hh * per_head + y][r].x);
       // a warp that saw nothing has zeros, and 0 * f stays 0; NaN sums stay NaN
+      const float f = m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - M);
+      float *dst = mg + (warp * RU + r) * D;
 #pragma unroll
-      for (int k = 0; k < D / 8; ++k)
-        *reinterpret_cast<float2 *>(mg + ((warp * 16 + r) * D + 8 * k + 2 * c)) = make_float2(o[k][2 * i] * f, o[k][2 * i + 1] * f);
+      for (int k = 0; k < KS; ++k)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) dst[(16 * k + 8 * z + g + 8 * (r >> 1)) & (D - 1)] = o[i >> 1][k][2 * z + (i & 1)] * f;
     }
-    bar_sync();
     const bool whole = t_begin == 0 && t_end == at.nt;
-    // where the unit's tiles lie: the CTA that starts it and the last one
-    const int64_t u0 = w - t_end;
-    const int c0 = (int)(u0 / share), c1 = (int)((u0 + at.nt - 1) / share);
-    float *part = a.part + (int64_t)(2 * blockIdx.x + (blockIdx.x == c0)) * rows_part(D);
-    auto store = [&](int r, int v, float4 x, float L) {
-      const int rr = at.rb * kRowsPerUnit + r, j = rr / a.G;
-      // a row before position 0 sees nothing and gives zeros
-      const bool sees = p_base + j >= 0;
-      const float inv = sees ? 1.f / L : 0.f;
-      if (!sees) x = make_float4(0.f, 0.f, 0.f, 0.f);
-      uint8_t *dst = static_cast<uint8_t *>(a.out) +
-                     2 * (((int64_t)(at.s.q0 + j) * a.Hq + at.h * a.G + (rr - j * a.G)) * D + 4 * v);
-      *reinterpret_cast<uint2 *>(dst) = make_uint2(pack2<BF16>(x.x * inv, x.y * inv), pack2<BF16>(x.z * inv, x.w * inv));
-    };
-    for (int e = tid; e < R * (D / 4); e += kThreads) {
-      const int r = e / (D / 4), v = e % (D / 4);
-      const float M = fmaxf(fmaxf(s_ml[0][r].x, s_ml[1][r].x), fmaxf(s_ml[2][r].x, s_ml[3][r].x));
-      float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-      float L = 0.f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 y = *reinterpret_cast<const float4 *>(mg + (i * 16 + r) * D + 4 * v);
-        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
-        const float2 ml = s_ml[i][r];
+    float *part = a.part + ((int64_t)(2 * blockIdx.x + (t_begin == 0)) * kRowsMaxHeads + hh) * rows_part(D);
+    // lane r: row r's sum and where it goes
+    float inv = 0.f;
+    uint32_t row_off = 0;
+    if (lane < R) {
+      float M = s_ml[hh * per_head][lane].x, L = 0.f;
+      for (int i = 1; i < per_head; ++i) M = fmaxf(M, s_ml[hh * per_head + i][lane].x);
+      for (int i = 0; i < per_head; ++i) {
+        const float2 ml = s_ml[hh * per_head + i][lane];
         L += ml.y * (ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M));
       }
-      if (whole) {
-        store(r, v, x, L);
-      } else {
-        __stcg(reinterpret_cast<float4 *>(part + r * D + 4 * v), x);
-        if (v == 0) {
-          __stcg(part + kRowsPerUnit * D + r, M);
-          __stcg(part + kRowsPerUnit * (D + 1) + r, L);
-        }
+      const int rr = row0 + lane, j = rr / a.G;
+      row_off = (uint32_t)((at.s.q0 + j) * a.Hq + (at.h * HC + hh) * a.G + (rr - j * a.G));
+      // a row before position 0 sees nothing and gives zeros
+      inv = p_base + j >= 0 ? 1.f / L : -1.f;
+      if (!whole && sub == 0) {
+        __stcg(part + kRowsPerUnit * D + lane, M);
+        __stcg(part + kRowsPerUnit * (D + 1) + lane, L);
       }
     }
-    if (!whole) {
-      __threadfence();
-      bar_sync();
-      if (tid == 0) {
-        const bool last = atomicAdd(a.counter + c0, 1) == c1 - c0;
-        if (last) a.counter[c0] = 0;  // as the next call expects it
-        s_last = last;
-      }
-      bar_sync();
-      if (s_last) {
-        __threadfence();
-        // thread (group, row, 4 channels): the pieces group, group + n, ...;
-        // the groups meet in shared memory
-        const int vecs = R * (D / 4), groups = max(1, kThreads / vecs);
-        for (int e0 = 0; e0 < vecs; e0 += kThreads) {
-          const int e = e0 + tid % min(vecs, kThreads), grp = vecs < kThreads ? tid / vecs : 0;
-          const int r = e / (D / 4), v = e % (D / 4);
-          const bool on = e < vecs && grp < groups;
-          float M = -INFINITY, L = 0.f;
-          float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (on) {
-            constexpr int U = 8;
-            for (int p0 = c0 + grp; p0 <= c1; p0 += U * groups) {
-              float4 y[U];
-              float pm[U], pl[U];
-#pragma unroll
-              for (int u = 0; u < U; ++u) {
-                const int p = p0 + u * groups;
-                const float *src = a.part + (int64_t)(2 * p + (p == c0)) * rows_part(D);
-                const bool in = p <= c1;
-                y[u] = in ? __ldcg(reinterpret_cast<const float4 *>(src + r * D + 4 * v)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                pm[u] = in ? __ldcg(src + kRowsPerUnit * D + r) : -INFINITY;
-                pl[u] = in ? __ldcg(src + kRowsPerUnit * (D + 1) + r) : 0.f;
-              }
-#pragma unroll
-              for (int u = 0; u < U; ++u) join(M, L, x, pm[u], pl[u], y[u]);
-            }
-          }
-          if (groups > 1) {
-            float4 *sx = reinterpret_cast<float4 *>(mg);
-            float2 *sl = reinterpret_cast<float2 *>(sx + kThreads);
-            bar_sync();  // mg has been read
-            sx[tid] = x;
-            sl[tid] = make_float2(M, L);
-            bar_sync();
-            if (tid < vecs)
-              for (int i = 1; i < groups; ++i) join(M, L, x, sl[tid + i * vecs].x, sl[tid + i * vecs].y, sx[tid + i * vecs]);
-          }
-          if (on && grp == 0) store(r, v, x, L);
-        }
-      }
-    }
-    fence_proxy_async();
     bar_sync();
-    release(k_stage);
-    release(v_stage);
-    if (w < w1 && at.t >= at.nt) next_unit(at);
+    // the warps of a head share its rows, 4 channels a lane
+    constexpr int V = D / 4, RW = 32 / V;  // rows of a warp at a time
+    const int v = lane % V;
+#pragma unroll 4
+    for (int i = 0; i < RU; i += RW * per_head) {
+      const int r = i + sub * RW + lane / V;
+      const float f = __shfl_sync(kAll, inv, r & 31);
+      const uint32_t off = __shfl_sync(kAll, row_off, r & 31);
+      if (r < R) {
+        const float *src = mg + ((hh * per_head) * RU + r) * D + ((4 * v + 8 * (r >> 1)) & (D - 1));
+        float4 x = *reinterpret_cast<const float4 *>(src);
+        for (int y = 1; y < per_head; ++y) {
+          const float4 z = *reinterpret_cast<const float4 *>(src + y * RU * D);
+          x.x += z.x, x.y += z.y, x.z += z.z, x.w += z.w;
+        }
+        if (!whole) {
+          __stcg(reinterpret_cast<float4 *>(part + r * D + 4 * v), x);
+        } else {
+          if (f < 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
+          *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + ((uint64_t)off * D + 4 * v) * 2) =
+              make_uint2(pack2<BF16>(x.x * f, x.y * f), pack2<BF16>(x.z * f, x.w * f));
+        }
+      }
+    }
+    if (!whole && t_begin == 0 && tid == 0) {
+      const int at_list = atomicAdd(&a.list->n, 1);  // a CTA adds one at most
+      const int last = (int)blockIdx.x + (w_begin + at.nt - 1) / s_share;
+      a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, row0, R};
+    }
+    if (w < mine) {
+      fence_proxy_async();
+      bar_sync();
+      release(k_stage);
+      release(v_stage);
+      if (at.t >= at.nt) next_unit(at);
+    }
   }
   if (*abort_flag && lane == 0) set_err(pv.err, kErrTimeout);
   pdl_trigger();
 }
 
-template <int D, bool BF16>
+template <int D, int NB, bool BF16>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   constexpr int smem = rows_stages<D>() * kT * D * 2 + 1024;
   RowsArgs ra;
   memcpy(&ra.mk, a.wk, sizeof ra.mk);
   memcpy(&ra.mv, a.wv, sizeof ra.mv);
   ra.a = a;
+  ra.a.rows = std::min(8 * NB, a.max_new * a.G);
   static std::atomic<bool> ready{false};
   if (!ready.load(std::memory_order_relaxed)) {
     const cudaError_t e =
-        cudaFuncSetAttribute(attn_rows_kernel<D, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        cudaFuncSetAttribute(attn_rows_kernel<D, NB, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     ready.store(true, std::memory_order_relaxed);
   }
-  // two CTAs per SM, no more of them than tiles that there can be
-  const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / kT + 2;
-  const int64_t tiles = (int64_t)a.pv.B * a.pv.Hkv * ((a.max_new * a.G + kRowsPerUnit - 1) / kRowsPerUnit) * cap;
-  const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), tiles);
-  return launch_pdl(attn_rows_kernel<D, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
+  // two CTAs per SM, no more of them than runs that there can be
+  const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / (kT / a.hc) + 2;
+  const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * ((a.max_new * a.G + 8 * NB - 1) / (8 * NB)) * cap;
+  const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), (tiles + kMinShare - 1) / kMinShare);
+  const cudaError_t e = launch_pdl(attn_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
+  if (e != cudaSuccess) return e;
+  // a unit cut in pieces starts in a CTA of its own; eight of the joining CTAs
+  // fit an SM
+  return launch_pdl(attn_join_kernel<D, BF16>, dim3(std::min(grid * a.hc * ra.a.rows, 8 * a.sms)), dim3(kThreads), 0, st, ra.a);
+}
+template <int D, bool BF16>
+cudaError_t launch_rows(const AttnArgs &a, cudaStream_t st) {
+  return a.max_new * a.G <= 8 ? launch_t<D, 1, BF16>(a, st) : launch_t<D, 2, BF16>(a, st);
 }
 
 }  // namespace
@@ -582,8 +674,8 @@ cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st) {
   if (a.pv.B == 0 || a.pv.n_tokens == 0) return cudaSuccess;
   const bool bf = dtype == kSrvBf16;
   switch (a.pv.D) {
-    case 128: return bf ? launch_t<128, true>(a, st) : launch_t<128, false>(a, st);
-    case 64: return bf ? launch_t<64, true>(a, st) : launch_t<64, false>(a, st);
+    case 128: return bf ? launch_rows<128, true>(a, st) : launch_rows<128, false>(a, st);
+    case 64: return bf ? launch_rows<64, true>(a, st) : launch_rows<64, false>(a, st);
     default: return cudaErrorInvalidValue;
   }
 }

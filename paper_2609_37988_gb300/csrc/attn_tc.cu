@@ -687,13 +687,14 @@ cudaError_t launch_src(const AttnArgs &a, cudaStream_t st) {
 }  // namespace
 
 // [pages, KV heads, slots, D] as boxes of up to 64 slots x 64 channels, or
-// (`whole`) x all channels, 64 at a time one behind another
-cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, bool whole) {
+// (`heads` > 0) x all channels, 64 at a time one behind another, x so many heads
+cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads) {
+  const bool whole = heads > 0;
   const uint64_t row = (uint64_t)D * 2, P = (uint64_t)page, H = (uint64_t)Hkv, N = (uint64_t)n_pages;
   const uint64_t dims4[4] = {(uint64_t)D, P, H, N}, strides4[3] = {row, row * P, row * P * H};
   const uint64_t dims5[5] = {64, P, (uint64_t)D / 64, H, N}, strides5[4] = {row, 128, row * P, row * P * H};
   const uint32_t rows = (uint32_t)std::min(page, 64);
-  const uint32_t box4[4] = {64, rows, 1, 1}, box5[5] = {64, rows, (uint32_t)D / 64, 1, 1}, one[5] = {1, 1, 1, 1, 1};
+  const uint32_t box4[4] = {64, rows, 1, 1}, box5[5] = {64, rows, (uint32_t)D / 64, (uint32_t)heads, 1}, one[5] = {1, 1, 1, 1, 1};
   return encode_tensor_map_tiled(out, bf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, whole ? 5 : 4,
                                  pool, whole ? dims5 : dims4, whole ? strides5 : strides4, whole ? box5 : box4, one,
                                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,

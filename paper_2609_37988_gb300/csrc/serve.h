@@ -43,6 +43,18 @@ struct RotArgs {
 };
 cudaError_t launch_rotary(const RotArgs &a, int dtype, cudaStream_t st);
 
+// Units of the few-token form whose tiles lie in several CTAs' runs.
+constexpr int kRowsMaxCtas = 320;
+struct RowsSplit {
+  int32_t first, last;    // the CTAs where it starts and ends
+  int32_t q0, p_base, head, row0, rows;
+};
+struct RowsList {         // n and done are zero between calls
+  int32_t n;
+  uint32_t done;
+  RowsSplit unit[kRowsMaxCtas];
+};
+
 // Attention of packed queries over pages (pv.k set) or over packed keys and
 // values (k, v), causal, each query seeing at most `window` positions.
 struct AttnArgs {
@@ -50,18 +62,25 @@ struct AttnArgs {
   Rows q, k, v;
   void *out;              // [n_tokens, Hq, D]
   int Hq, G, window, max_new;
+  int hc, rows;           // few-token form: KV heads of a unit, its rows at most
+  int part_shift, pt_shift;  // positions of one copy, of a tile (log2)
   float sig_log2;
   const void *mk, *mv, *wk, *wv;  // the pages' tensor maps (host memory, 128 bytes each): halves, whole rows
   float *part;            // partial results, kPartSlots of rows_part() floats
-  int32_t *counter;       // zero between calls
+  RowsList *list;
   int sms;
 };
-cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, bool whole);
+cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads);
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
 cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st);
 // CTAs that a split launch may use at most, and the partial slots of each
-constexpr int kRowsMaxCtas = 512;
-constexpr int kRowsPerUnit = 16;
+constexpr int kRowsPerUnit = 16, kRowsMaxHeads = 4;
+// KV heads of a unit: as many as make a copy 64 rows of one page
+constexpr int rows_heads(int page, int Hkv) {
+  int hc = 1;
+  while (hc < kRowsMaxHeads && 2 * hc * page <= 64 && Hkv % (2 * hc) == 0) hc *= 2;
+  return hc;
+}
 // floats of one partial: rows of D sums, then maxima, then totals
 __host__ __device__ constexpr int rows_part(int D) { return kRowsPerUnit * (D + 2); }
 

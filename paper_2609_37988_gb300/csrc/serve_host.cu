@@ -32,7 +32,7 @@ struct PageMap {
 struct kvk_paged {
   kvk_paged_desc d;
   std::vector<uint8_t *> k, v;
-  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys, values, both again in whole rows
+  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys, values, both again for the few-token form
   uint8_t *ws;
   int device, sms, page_shift;
 };
@@ -79,14 +79,14 @@ kvk_status check_heads(int Hq, int Hkv, int D, int dtype) {
 }
 
 struct PagedWs {
-  size_t err, counter, part, total;
+  size_t err, list, part, total;
 };
 PagedWs paged_ws(int D) {
   PagedWs w;
   w.err = 0;
-  w.counter = 256;
-  w.part = w.counter + (size_t)kRowsMaxCtas * 4;
-  w.total = w.part + (size_t)2 * kRowsMaxCtas * rows_part(D) * sizeof(float);
+  w.list = 256;
+  w.part = w.list + ((sizeof(RowsList) + 255) & ~(size_t)255);
+  w.total = w.part + (size_t)2 * kRowsMaxCtas * kRowsMaxHeads * rows_part(D) * sizeof(float);
   return w;
 }
 
@@ -114,8 +114,8 @@ kvk_status check_call(const kvk_paged *p, int layer, const kvk_paged_batch *b, b
   if (!b) return fail(KVK_ERR_INVALID_ARG, "null batch");
   if (b->batch < 0 || b->n_tokens < 0 || b->max_pages < 0)
     return fail(KVK_ERR_INVALID_ARG, "batch, n_tokens and max_pages must not be negative");
-  if ((int64_t)b->max_pages * p->d.page_size > (1 << 28))
-    return fail(KVK_ERR_INVALID_ARG, "max_pages %d: more than 2^28 positions", b->max_pages);
+  if ((int64_t)b->max_pages * p->d.page_size > (1 << 26))
+    return fail(KVK_ERR_INVALID_ARG, "max_pages %d: more than 2^26 positions", b->max_pages);
   if ((int64_t)b->n_tokens * p->d.n_q_heads > (1 << 30)) return fail(KVK_ERR_INVALID_ARG, "n_tokens too large");
   empty = b->batch == 0 || b->n_tokens == 0;
   if (empty) return KVK_OK;
@@ -282,7 +282,7 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
   const bool bf = desc->dtype == KVK_DTYPE_BF16;
   for (int i = 0; i < desc->n_layers * 4 && e == cudaSuccess; ++i)
     e = make_pages_map(p->maps[i].bytes, bf, i & 1 ? p->v[i / 4] : p->k[i / 4], desc->head_dim, desc->page_size, desc->n_kv_heads,
-                       desc->n_pages, (i & 2) != 0);
+                       desc->n_pages, i & 2 ? rows_heads(desc->page_size, desc->n_kv_heads) : 0);
   if (e != cudaSuccess) {
     delete p;
     return kvk_internal_cuda_error(e, "encoding the pages' tensor maps");
@@ -359,9 +359,12 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.max_new = max_new < batch->n_tokens ? max_new : batch->n_tokens;
   a.sig_log2 = softmax_scale * kLog2e;
   const PagedWs w = paged_ws(p->d.head_dim);
-  a.counter = reinterpret_cast<int32_t *>(p->ws + w.counter);
+  a.list = reinterpret_cast<RowsList *>(p->ws + w.list);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
+  a.hc = rows_heads(p->d.page_size, p->d.n_kv_heads);
+  a.part_shift = p->page_shift < 6 ? p->page_shift : 6;
+  a.pt_shift = a.hc == 4 ? 4 : a.hc == 2 ? 5 : 6;
   const PageMap *maps = &p->maps[(size_t)layer * 4];
   a.mk = maps[0].bytes;
   a.mv = maps[1].bytes;
