@@ -12,7 +12,9 @@
 // are.  A unit that a run covers whole is written at once; the pieces of the
 // others go to the workspace, with a note of where they lie, and a second kernel
 // joins them, a CTA per row (one CTA per unit that did it behind its own run
-// took 50 us for 152 pieces of 20 rows).
+// took 50 us for 152 pieces of 20 rows).  Where no sequence can have more than
+// kWholeCtx positions, CTAs take whole units of one KV head and nothing has to
+// be joined: the second launch costs the caller more than the longer runs do.
 //
 // A CTA: 4 warps, 16 positions of one head's tile each, and a warp that looks
 // up pages and copies key and value tiles by TMA through a ring (96 KB; each
@@ -43,6 +45,7 @@ constexpr int kT = 64;        // positions x KV heads of a tile
 constexpr int kThreads = 128;  // that compute; a warp beside them copies
 constexpr int kErrCount = 4, kErrTimeout = 8, kErrPage = 32;  // KVK_DEVERR_*
 constexpr int kMinShare = 4;   // tiles of a run at least
+constexpr int kWholeCtx = 512;
 constexpr uint32_t kWaits = 1u << 20;  // polls of up to 2 us each
 constexpr uint32_t kAll = 0xffffffffu;
 
@@ -255,7 +258,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     auto chunk = [&](int b0) {
       const bool in = b0 + lane < pv.B;
       if (in) sq = load_seq(pv, b0 + lane, a.max_new);
-      per = in ? seq_tiles<RU>(sq, a) : 0;
+      per = !in ? 0 : a.whole ? row_blocks<RU>(sq, a.G) : seq_tiles<RU>(sq, a);
       uint32_t x = per;  // 32 sequences of at most 2^22 tiles and 8 row blocks each
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -269,7 +272,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
       upto = chunk(b0);
       total += __shfl_sync(kAll, upto, 31);
     }
-    const int64_t share = max(div_pos(total + gridDim.x - 1, gridDim.x), (int64_t)kMinShare);
+    const int64_t share = max(div_pos(total + gridDim.x - 1, gridDim.x), (int64_t)(a.whole ? 1 : kMinShare));
     const int64_t w0 = share * blockIdx.x;
     if (w0 < total) {
       for (int b0 = 0;; b0 += 32) {
@@ -283,15 +286,24 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
             const int64_t off = w0 - (before + upto - (int64_t)units * per);
             x.h = (int)div_pos(off, per);
             int r = (int)(off - (int64_t)x.h * per);
-            x.rb = 0;
+            x.rb = a.whole ? r : 0;
             settle(x);
-            while (r >= x.nt) {
+            while (!a.whole && r >= x.nt) {
               r -= x.nt;
               ++x.rb;
               settle(x);
             }
-            x.t = r;
+            x.t = a.whole ? 0 : r;
             s_at = x;
+            s_mine = (int)min(share, total - w0);
+            if (a.whole) {  // units to tiles
+              int tiles = x.nt;
+              for (int u = 1; u < (int)min(share, total - w0); ++u) {
+                next_unit(x);
+                tiles += x.nt;
+              }
+              s_mine = tiles;
+            }
           }
           break;
         }
@@ -299,7 +311,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
       }
     }
     if (lane == 0) {
-      s_mine = w0 < total ? (int)min(share, total - w0) : 0;
+      if (w0 >= total) s_mine = 0;
       s_share = (int)min(share, (int64_t)1 << 30);
     }
   }
@@ -642,8 +654,8 @@ template <int D, int NB, bool BF16>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   constexpr int smem = rows_stages<D>() * kT * D * 2 + 1024;
   RowsArgs ra;
-  memcpy(&ra.mk, a.wk, sizeof ra.mk);
-  memcpy(&ra.mv, a.wv, sizeof ra.mv);
+  memcpy(&ra.mk, a.whole ? a.ok : a.wk, sizeof ra.mk);
+  memcpy(&ra.mv, a.whole ? a.ov : a.wv, sizeof ra.mv);
   ra.a = a;
   ra.a.rows = std::min(8 * NB, a.max_new * a.G);
   static std::atomic<bool> ready{false};
@@ -656,9 +668,10 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   // two CTAs per SM, no more of them than runs that there can be
   const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / (kT / a.hc) + 2;
   const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * ((a.max_new * a.G + 8 * NB - 1) / (8 * NB)) * cap;
-  const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), (tiles + kMinShare - 1) / kMinShare);
+  const int64_t runs = a.whole ? tiles / cap : (tiles + kMinShare - 1) / kMinShare;
+  const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), runs);
   const cudaError_t e = launch_pdl(attn_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || a.whole) return e;
   // a unit cut in pieces starts in a CTA of its own; eight of the joining CTAs
   // fit an SM
   return launch_pdl(attn_join_kernel<D, BF16>, dim3(std::min(grid * a.hc * ra.a.rows, 8 * a.sms)), dim3(kThreads), 0, st, ra.a);
@@ -670,8 +683,13 @@ cudaError_t launch_rows(const AttnArgs &a, cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st) {
-  if (a.pv.B == 0 || a.pv.n_tokens == 0) return cudaSuccess;
+cudaError_t launch_attn_rows(const AttnArgs &in, int dtype, cudaStream_t st) {
+  if (in.pv.B == 0 || in.pv.n_tokens == 0) return cudaSuccess;
+  AttnArgs a = in;
+  a.whole = ((int64_t)a.pv.max_pages << a.pv.page_shift) <= kWholeCtx;
+  a.hc = a.whole ? 1 : rows_heads(1 << a.pv.page_shift, a.pv.Hkv);
+  a.part_shift = std::min(a.pv.page_shift, 6);
+  a.pt_shift = a.hc == 4 ? 4 : a.hc == 2 ? 5 : 6;
   const bool bf = dtype == kSrvBf16;
   switch (a.pv.D) {
     case 128: return bf ? launch_rows<128, true>(a, st) : launch_rows<128, false>(a, st);

@@ -62,10 +62,12 @@ struct AttnArgs {
   Rows q, k, v;
   void *out;              // [n_tokens, Hq, D]
   int Hq, G, window, max_new;
-  int hc, rows;           // few-token form: KV heads of a unit, its rows at most
+  int hc, rows, whole;    // few-token form: KV heads of a unit, its rows at most, units never cut
   int part_shift, pt_shift;  // positions of one copy, of a tile (log2)
   float sig_log2;
-  const void *mk, *mv, *wk, *wv;  // the pages' tensor maps (host memory, 128 bytes each): halves, whole rows
+  // the pages' tensor maps (host memory, 128 bytes each): boxes of 64 channels,
+  // of whole rows of rows_heads() KV heads, of whole rows of one
+  const void *mk, *mv, *wk, *wv, *ok, *ov;
   float *part;            // partial results, kPartSlots of rows_part() floats
   RowsList *list;
   int sms;

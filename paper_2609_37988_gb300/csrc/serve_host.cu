@@ -32,7 +32,7 @@ struct PageMap {
 struct kvk_paged {
   kvk_paged_desc d;
   std::vector<uint8_t *> k, v;
-  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys, values, both again for the few-token form
+  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys and values, three times
   uint8_t *ws;
   int device, sms, page_shift;
 };
@@ -266,7 +266,7 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
       p->k.push_back(static_cast<uint8_t *>(k_pages[l]));
       p->v.push_back(static_cast<uint8_t *>(v_pages[l]));
     }
-    p->maps.resize((size_t)desc->n_layers * 4);
+    p->maps.resize((size_t)desc->n_layers * 6);
   } catch (const std::bad_alloc &) {
     delete p;
     return fail(KVK_ERR_INVALID_ARG, "out of host memory");
@@ -280,9 +280,10 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
     return kvk_internal_cuda_error(e, "querying the device");
   }
   const bool bf = desc->dtype == KVK_DTYPE_BF16;
-  for (int i = 0; i < desc->n_layers * 4 && e == cudaSuccess; ++i)
-    e = make_pages_map(p->maps[i].bytes, bf, i & 1 ? p->v[i / 4] : p->k[i / 4], desc->head_dim, desc->page_size, desc->n_kv_heads,
-                       desc->n_pages, i & 2 ? rows_heads(desc->page_size, desc->n_kv_heads) : 0);
+  const int heads[3] = {0, rows_heads(desc->page_size, desc->n_kv_heads), 1};
+  for (int i = 0; i < desc->n_layers * 6 && e == cudaSuccess; ++i)
+    e = make_pages_map(p->maps[i].bytes, bf, i & 1 ? p->v[i / 6] : p->k[i / 6], desc->head_dim, desc->page_size, desc->n_kv_heads,
+                       desc->n_pages, heads[i % 6 / 2]);
   if (e != cudaSuccess) {
     delete p;
     return kvk_internal_cuda_error(e, "encoding the pages' tensor maps");
@@ -362,14 +363,13 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.list = reinterpret_cast<RowsList *>(p->ws + w.list);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
-  a.hc = rows_heads(p->d.page_size, p->d.n_kv_heads);
-  a.part_shift = p->page_shift < 6 ? p->page_shift : 6;
-  a.pt_shift = a.hc == 4 ? 4 : a.hc == 2 ? 5 : 6;
-  const PageMap *maps = &p->maps[(size_t)layer * 4];
+  const PageMap *maps = &p->maps[(size_t)layer * 6];
   a.mk = maps[0].bytes;
   a.mv = maps[1].bytes;
   a.wk = maps[2].bytes;
   a.wv = maps[3].bytes;
+  a.ok = maps[4].bytes;
+  a.ov = maps[5].bytes;
   const cudaError_t e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;
