@@ -23,7 +23,10 @@
 //
 // Jobs in order of their distance from their sequence's end, all sequences
 // side by side: the longest first where lengths are equal, the short ones last
-// in any case; dealt to the CTAs back and forth.
+// in any case; dealt to the CTAs back and forth.  Chunks over pages that make
+// few jobs go in equal runs of tiles instead, one per CTA: jobs that a run cuts
+// leave their pieces (result, reference and sum of each row) in the workspace,
+// and a second kernel joins them.
 #include <cuda.h>
 #include <math.h>
 #include <string.h>
@@ -58,7 +61,13 @@ struct Job {
   int js[2], je[2];     // tiles that either query tile sees: [js, je)
   int first, low;       // tiles in [low, first] positions are seen by every row
   int two, bad;         // second query tile; values that are not finite
+  int slot;             // where a piece of a job goes; -1: a whole job
 };
+
+// floats of a piece's query tile: D / 4 x 128 rows x 4 results, then references
+// and sums
+constexpr int tc_part(int D) { return kTcT * (D + 2); }
+constexpr int kTcMinShare = 4;  // tiles of a run at least
 
 template <int D>
 struct Smem {
@@ -168,28 +177,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 
   if (warp == 9) {
     // -- schedule and copies ---------------------------------------------------
-    auto blocks = [&](int b) {
-      int q0;
-      return (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P);
-    };
-    int total = 0, most = 0;
-    for (int b = lane; b < pv.B; b += 32) {
-      const int x = blocks(b);
-      total += x;
-      most = max(most, x);
-    }
-    total = (int)__reduce_add_sync(kAll, (unsigned)total);
-    most = (int)__reduce_max_sync(kAll, (unsigned)most);
-    // jobs at most `d` blocks from their sequence's end
-    auto upto = [&](int d) {
-      unsigned s = 0;
-      for (int b = lane; b < pv.B; b += 32) s += min(blocks(b), d);
-      return (int)__reduce_add_sync(kAll, s);
-    };
-    const int n_jobs = total * pv.Hkv, step = gridDim.x;
     int s = 0;          // ring place and its round's parity
     uint32_t ph = 0;
     int loads = 0;      // query loads so far
+    int k = 0;          // jobs handed out
     // lane 0 waits, the warp goes on together
     auto wait0 = [&](uint64_t *b, uint32_t parity) {
       int ok = 1;
@@ -197,71 +188,53 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       return __shfl_sync(kAll, ok, 0) != 0;
     };
     constexpr int NB = D / 64;
-    for (int k = 0;; ++k) {
-      const int idx = k * step + (k & 1 ? step - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    // describes block `blk` of sequence b (2 P tokens), KV head h
+    auto describe = [&](int b, int h, int blk, int q0, int n) {
       Job j = {};
-      const bool go = idx < n_jobs;
-      if (go) {
-        const int r = idx / pv.Hkv;
-        j.h = idx - r * pv.Hkv;
-        int d0 = 0, d1 = most, f0 = 0;  // upto(d0) <= r < upto(d1)
-        while (d1 - d0 > 1) {
-          const int mid = (d0 + d1) / 2, f = upto(mid);
-          if (f <= r)
-            d0 = mid, f0 = f;
-          else
-            d1 = mid;
+      j.b = b;
+      j.h = h;
+      j.q0 = q0;
+      j.n = n;
+      j.slot = -1;
+      int len = n;
+      if (PAGED) {
+        len = max(pv.lens[b], 0);
+        const int64_t cap = (int64_t)pv.max_pages << pv.page_shift;
+        if (len > cap || n > a.max_new) {
+          if (lane == 0) set_err(pv.err, kErrCount);
+          len = (int)min((int64_t)len, cap);
         }
-        int rem = r - f0;
-        for (int b0 = 0;; b0 += 32) {
-          const uint32_t in = __ballot_sync(kAll, b0 + lane < pv.B && blocks(min(b0 + lane, pv.B - 1)) > d0);
-          const int c = __popc(in);
-          if (rem < c) {
-            j.b = b0 + (int)__fns(in, 0, rem + 1);
-            break;
-          }
-          rem -= c;
-        }
-        j.n = seq_tokens(pv, j.b, j.q0);
-        int len = j.n;
-        if (PAGED) {
-          len = max(pv.lens[j.b], 0);
-          const int64_t cap = (int64_t)pv.max_pages << pv.page_shift;
-          if (len > cap || j.n > a.max_new) {
-            if (lane == 0) set_err(pv.err, kErrCount);
-            len = (int)min((int64_t)len, cap);
-          }
-        }
-        j.p0 = len - j.n;
-        j.tok0 = ((j.n + 2 * P - 1) / (2 * P) - 1 - d0) * 2 * P;
-        j.two = j.tok0 + P < j.n;
-        const int lo0 = max(0, j.p0 + j.tok0 - a.window + 1);
-        j.lo = lo0 / kTcT * kTcT;
-        int last = 0;
-        for (int i = 0; i < 1 + j.two; ++i) {
-          const int f = j.p0 + j.tok0 + i * P, l = j.p0 + min(j.n, j.tok0 + (i + 1) * P) - 1;
-          if (l >= 0) {
-            j.js[i] = (max(0, f - a.window + 1) - j.lo) / kTcT;
-            j.je[i] = (l - j.lo) / kTcT + 1;
-          }
-          last = l;
-        }
-        j.nt = max(j.je[0], j.je[1]);
-        j.first = j.p0 + j.tok0;
-        j.low = last - a.window + 1;
-      } else {
-        j.b = -1;
       }
+      j.p0 = len - n;
+      j.tok0 = blk * 2 * P;
+      j.two = j.tok0 + P < n;
+      j.lo = max(0, j.p0 + j.tok0 - a.window + 1) / kTcT * kTcT;
+      int last = 0;
+      for (int i = 0; i < 1 + j.two; ++i) {
+        const int f = j.p0 + j.tok0 + i * P, l = j.p0 + min(n, j.tok0 + (i + 1) * P) - 1;
+        if (l >= 0) {
+          j.js[i] = (max(0, f - a.window + 1) - j.lo) / kTcT;
+          j.je[i] = (l - j.lo) / kTcT + 1;
+        }
+        last = l;
+      }
+      j.nt = max(j.je[0], j.je[1]);
+      j.first = j.p0 + j.tok0;
+      j.low = last - a.window + 1;
+      return j;
+    };
+    // hands a job out and copies its tiles
+    auto emit = [&](const Job &j) {
       const int slot = k & 1;
-      if (k >= 2 && !wait0(&jfree[slot], (k / 2 - 1) & 1)) break;
+      if (k >= 2 && !wait0(&jfree[slot], (k / 2 - 1) & 1)) return false;
+      ++k;
       if (lane == 0) {
         jobs[slot] = j;
         mbar_arrive(&jfull[slot]);
       }
       __syncwarp();
-      if (!go) break;
-      if (j.nt == 0) continue;
-      if (loads > 0 && !wait0(qfree, (loads - 1) & 1)) break;
+      if (j.b < 0 || j.nt == 0) return true;
+      if (loads > 0 && !wait0(qfree, (loads - 1) & 1)) return false;
       ++loads;
       if (lane == 0) mbar_expect_tx(qfull, (1 + j.two) * NB * G * P * 128);
       __syncwarp();
@@ -281,13 +254,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         return pv.n_pages;
       };
       int page = PAGED ? page_of(0) : 0;
-      bool ok = true;
-      for (int jt = 0; jt < j.nt && ok; ++jt) {
+      for (int jt = 0; jt < j.nt; ++jt) {
         const int page_next = PAGED && jt + 1 < j.nt ? page_of(jt + 1) : 0;
 #pragma unroll
         for (int kv = 0; kv < 2; ++kv) {
-          ok = wait0(&free_[s], ph ^ 1);
-          if (!ok) break;
+          if (!wait0(&free_[s], ph ^ 1)) return false;
           if (lane == 0) mbar_expect_tx(&full[s], SM::kTile);
           __syncwarp();
           uint8_t *dst = sm + SM::kRing + s * SM::kTile + half * kBox;
@@ -303,8 +274,141 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         }
         page = page_next;
       }
-      if (!ok) break;
+      return true;
+    };
+    auto blocks = [&](int b) {
+      int q0;
+      return (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P);
+    };
+    Job end = {};
+    end.b = -1;
+    bool ok = true;
+    if (PAGED && a.runs) {
+      // tiles of one KV head of a sequence (describe()'s nt of every block), a
+      // job of none counting as one
+      auto head_tiles = [&](int b) {
+        int q0, sum = 0;
+        const int n = seq_tokens(pv, b, q0);
+        const int p0 = (int)min((int64_t)max(pv.lens[b], 0), (int64_t)pv.max_pages << pv.page_shift) - n;
+        for (int tok = 0; tok < n; tok += 2 * P) {
+          const int last = p0 + min(n, tok + 2 * P) - 1, lo = max(0, p0 + tok - a.window + 1) / kTcT;
+          sum += last < 0 ? 1 : last / kTcT - lo + 1;
+        }
+        return sum;
+      };
+      int64_t total = 0;
+      for (int b = lane; b < pv.B; b += 32) total += (int64_t)pv.Hkv * head_tiles(b);
+      for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
+      const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kTcMinShare);
+      const int64_t w0 = share * blockIdx.x;
+      int left = (int)max(min(share, total - w0), (int64_t)0);
+      if (left > 0) {
+        // the sequence, head, block and tile where the run starts
+        int b = 0, h = 0, blk = 0, t = 0;
+        int64_t off = 0;
+        for (int b0 = 0;; b0 += 32) {
+          const int64_t x = b0 + lane < pv.B ? (int64_t)pv.Hkv * head_tiles(b0 + lane) : 0;
+          int64_t sum = x;
+          for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(kAll, sum, o);
+            if (lane >= o) sum += y;
+          }
+          const uint32_t past = __ballot_sync(kAll, off + sum > w0);
+          if (past) {
+            const int f = __ffs(past) - 1;
+            b = b0 + f;
+            off = w0 - (off + __shfl_sync(kAll, sum - x, f));
+            break;
+          }
+          off += __shfl_sync(kAll, sum, 31);
+        }
+        int q0, n = seq_tokens(pv, b, q0);
+        const int per = head_tiles(b);
+        h = (int)(off / per);
+        t = (int)(off - (int64_t)h * per);
+        Job j = describe(b, h, 0, q0, n);
+        while (t >= max(1, j.nt)) {
+          t -= max(1, j.nt);
+          j = describe(b, h, ++blk, q0, n);
+        }
+        while (ok) {
+          const int nt = max(1, j.nt), t1 = min(nt, t + left);
+          if (t > 0 || t1 < nt) {  // a piece: tiles [t, t1)
+            j.slot = 2 * blockIdx.x + (t == 0);
+            if (t == 0 && lane == 0) {
+              const int at = atomicAdd(&a.tc_list->n, 1);  // a CTA adds one at most
+              const int before = (int)(share - left);
+              a.tc_list->unit[at] =
+                  TcSplit{(int)blockIdx.x, (int)blockIdx.x + (before + nt - 1) / (int)share, j.q0, j.n, j.p0, j.tok0, j.h};
+            }
+            j.lo += t * kTcT;
+            for (int i = 0; i < 2; ++i) {
+              j.js[i] = max(j.js[i] - t, 0);
+              j.je[i] = min(j.je[i], t1) - t;
+              if (j.js[i] >= j.je[i]) j.js[i] = j.je[i] = 0;
+            }
+            j.nt = t1 - t;
+          }
+          ok = emit(j);
+          left -= t1 - t;
+          if (left == 0) break;
+          t = 0;
+          if (++blk >= (n + 2 * P - 1) / (2 * P)) {
+            blk = 0;
+            if (++h >= pv.Hkv) {
+              h = 0;
+              do {
+                n = seq_tokens(pv, ++b, q0);
+              } while (n == 0);
+            }
+          }
+          j = describe(b, h, blk, q0, n);
+        }
+      }
+    } else {
+      int total = 0, most = 0;
+      for (int b = lane; b < pv.B; b += 32) {
+        const int x = blocks(b);
+        total += x;
+        most = max(most, x);
+      }
+      total = (int)__reduce_add_sync(kAll, (unsigned)total);
+      most = (int)__reduce_max_sync(kAll, (unsigned)most);
+      // jobs at most `d` blocks from their sequence's end
+      auto upto = [&](int d) {
+        unsigned sum = 0;
+        for (int b = lane; b < pv.B; b += 32) sum += min(blocks(b), d);
+        return (int)__reduce_add_sync(kAll, sum);
+      };
+      const int n_jobs = total * pv.Hkv, step = gridDim.x;
+      for (int i = 0; ok; ++i) {
+        const int idx = i * step + (i & 1 ? step - 1 - (int)blockIdx.x : (int)blockIdx.x);
+        if (idx >= n_jobs) break;
+        const int r = idx / pv.Hkv;
+        int d0 = 0, d1 = most, f0 = 0;  // upto(d0) <= r < upto(d1)
+        while (d1 - d0 > 1) {
+          const int mid = (d0 + d1) / 2, f = upto(mid);
+          if (f <= r)
+            d0 = mid, f0 = f;
+          else
+            d1 = mid;
+        }
+        int rem = r - f0, b = 0;
+        for (int b0 = 0;; b0 += 32) {
+          const uint32_t in = __ballot_sync(kAll, b0 + lane < pv.B && blocks(min(b0 + lane, pv.B - 1)) > d0);
+          const int c = __popc(in);
+          if (rem < c) {
+            b = b0 + (int)__fns(in, 0, rem + 1);
+            break;
+          }
+          rem -= c;
+        }
+        int q0;
+        const int n = seq_tokens(pv, b, q0);
+        ok = emit(describe(b, idx - r * pv.Hkv, (n + 2 * P - 1) / (2 * P) - 1 - d0, q0, n));
+      }
     }
+    if (ok) emit(end);
     // after a wait that gave up: the copies in flight land before the CTA ends
     if (*abort_flag && lane == 0) {
       if (loads > 0) mbar_wait(qfull, (loads - 1) & 1, kWaits);
@@ -598,6 +702,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           }
           __syncwarp();
         }
+        const int slot_out = j.slot;
+        float *part = a.part + ((int64_t)2 * slot_out + i) * tc_part(D) + 4 * row;
+        if (slot_out >= 0) {  // the piece's reference and sum
+          part[kTcT * D - 3 * row] = m == -INFINITY ? m : m - kShift;
+          part[kTcT * (D + 1) - 3 * row] = l;
+        }
         uint8_t *dst = static_cast<uint8_t *>(a.out) + 2 * ((int64_t)(j.q0 + tok) * a.Hq + j.h * G + (row - my_tok * G)) * D;
 #pragma unroll
         for (int c = 0; c < D / 32; ++c) {
@@ -608,7 +718,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = 0.f;
           }
-          if (real) {
+          if (slot_out >= 0 && real) {
+#pragma unroll
+            for (int y = 0; y < 8; ++y) {
+              float4 x = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
+              if (nan[c] >> (4 * y) & 1) x.x = NAN;
+              if (nan[c] >> (4 * y) & 2) x.y = NAN;
+              if (nan[c] >> (4 * y) & 4) x.z = NAN;
+              if (nan[c] >> (4 * y) & 8) x.w = NAN;
+              __stcg(reinterpret_cast<float4 *>(part + (8 * c + y) * (4 * kTcT)), x);
+            }
+          } else if (real) {
             uint32_t w[16];
 #pragma unroll
             for (int y = 0; y < 16; ++y) {
@@ -639,6 +759,58 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   tc_fence_after();
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
   pdl_trigger();
+}
+
+// Joins the pieces of the jobs that runs cut: a CTA takes 16 channels of a
+// query tile, a thread a row.
+template <int D, bool BF16>
+__global__ void __launch_bounds__(kTcT) attn_tc_join_kernel(const AttnArgs a, int P) {
+  const int row = threadIdx.x, tok_row = row / a.G;
+  constexpr int C = D / 16;
+  pdl_wait();
+  const int n = *reinterpret_cast<volatile int *>(&a.tc_list->n) * 2 * C;
+  for (int item = blockIdx.x; item < n; item += gridDim.x) {
+    const TcSplit u = a.tc_list->unit[item / (2 * C)];
+    const int i = item / C & 1, c = item % C;
+    const int tok = u.tok0 + i * P + tok_row;
+    if (tok_row >= P || tok >= u.n) continue;
+    float M = -INFINITY, L = 0.f, x[16];
+#pragma unroll
+    for (int y = 0; y < 16; ++y) x[y] = 0.f;
+    for (int p = u.first; p <= u.last; ++p) {
+      const float *part = a.part + (int64_t)(2 * (2 * p + (p == u.first)) + i) * tc_part(D);
+      const float pm = __ldcg(part + kTcT * D + row), pl = __ldcg(part + kTcT * (D + 1) + row);
+      float4 z[4];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) z[y] = __ldcg(reinterpret_cast<const float4 *>(part + (4 * c + y) * (4 * kTcT) + 4 * row));
+      if (pm == -INFINITY && pl == 0.f) continue;  // saw nothing
+      const float m = fmaxf(M, pm), f = M == -INFINITY ? 0.f : fast_exp2(M - m), h = pm == -INFINITY ? 0.f : fast_exp2(pm - m);
+      M = m;
+      L = L * f + pl * h;
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        x[4 * y] = x[4 * y] * f + z[y].x * h;
+        x[4 * y + 1] = x[4 * y + 1] * f + z[y].y * h;
+        x[4 * y + 2] = x[4 * y + 2] * f + z[y].z * h;
+        x[4 * y + 3] = x[4 * y + 3] * f + z[y].w * h;
+      }
+    }
+    const bool sees = u.p0 + tok >= 0;
+    const float inv = sees ? 1.f / L : 0.f;
+    uint32_t w[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) w[y] = sees ? pack2<BF16>(x[2 * y] * inv, x[2 * y + 1] * inv) : 0u;
+    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) +
+                                           2 * (((int64_t)(u.q0 + tok) * a.Hq + u.h * a.G + (row - tok_row * a.G)) * D + 16 * c));
+    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  }
+  pdl_trigger();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (atomicInc(&a.tc_list->done, gridDim.x - 1) == gridDim.x - 1) a.tc_list->n = 0;
+  }
 }
 
 // [rows, heads, D] of 16-bit values as boxes of 64 channels: `inner` and
@@ -675,8 +847,16 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   // at most so many jobs: every sequence's last one may be a partial one
   const int64_t jobs = (int64_t)a.pv.Hkv * (N / (2 * t.P) + std::min(a.pv.B, N));
-  const int grid = (int)std::min<int64_t>(a.sms, jobs);
-  return launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3(grid), dim3(kTcThreads), Smem<D>::kBytes, st, t);
+  // Runs where there are fewer than four jobs per SM at least (every token in
+  // one sequence).
+  t.a.runs = PAGED && (int64_t)a.pv.Hkv * ((N + 2 * t.P - 1) / (2 * t.P)) < 4 * a.sms;
+  if (!t.a.runs)
+    return launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(kTcThreads),
+                      Smem<D>::kBytes, st, t);
+  const int grid = std::min(a.sms, kTcMaxCtas);
+  e = launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3(grid), dim3(kTcThreads), Smem<D>::kBytes, st, t);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attn_tc_join_kernel<D, BF16>, dim3(std::min(grid * 2 * D / 16, 8 * a.sms)), dim3(kTcT), 0, st, t.a, t.P);
 }
 
 template <int D, bool BF16>

@@ -55,6 +55,17 @@ struct RowsList {         // n and done are zero between calls
   RowsSplit unit[kRowsMaxCtas];
 };
 
+// Jobs of the tensor-core form whose tiles lie in several CTAs' runs, likewise.
+constexpr int kTcMaxCtas = 160;
+struct TcSplit {
+  int32_t first, last, q0, n, p0, tok0, h;
+};
+struct TcList {
+  int32_t n;
+  uint32_t done;
+  TcSplit unit[kTcMaxCtas];
+};
+
 // Attention of packed queries over pages (pv.k set) or over packed keys and
 // values (k, v), causal, each query seeing at most `window` positions.
 struct AttnArgs {
@@ -68,8 +79,10 @@ struct AttnArgs {
   // the pages' tensor maps (host memory, 128 bytes each): boxes of 64 channels,
   // of whole rows of rows_heads() KV heads, of whole rows of one
   const void *mk, *mv, *wk, *wv, *ok, *ov;
-  float *part;            // partial results, kPartSlots of rows_part() floats
+  float *part;            // partial results
   RowsList *list;
+  TcList *tc_list;
+  int runs;               // tensor-core form: equal runs of tiles
   int sms;
 };
 cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads);

@@ -79,14 +79,17 @@ kvk_status check_heads(int Hq, int Hkv, int D, int dtype) {
 }
 
 struct PagedWs {
-  size_t err, list, part, total;
+  size_t err, list, tc_list, part, total;
 };
 PagedWs paged_ws(int D) {
   PagedWs w;
   w.err = 0;
   w.list = 256;
-  w.part = w.list + ((sizeof(RowsList) + 255) & ~(size_t)255);
-  w.total = w.part + (size_t)2 * kRowsMaxCtas * kRowsMaxHeads * rows_part(D) * sizeof(float);
+  w.tc_list = w.list + ((sizeof(RowsList) + 255) & ~(size_t)255);
+  w.part = w.tc_list + ((sizeof(TcList) + 255) & ~(size_t)255);
+  // two pieces per CTA of either form
+  const size_t rows = (size_t)2 * kRowsMaxCtas * kRowsMaxHeads * rows_part(D), tc = (size_t)2 * kTcMaxCtas * 2 * 128 * (D + 2);
+  w.total = w.part + (rows > tc ? rows : tc) * sizeof(float);
   return w;
 }
 
@@ -142,8 +145,12 @@ PagedView view_of(const kvk_paged *p, int layer, const kvk_paged_batch *b) {
   return v;
 }
 
+// Rows of a KV head up to which the form for few tokens is the faster one (us,
+// few / tensor cores, 14B-shaped layer: 4 x 8192 positions, 10 rows 39 / 40, 20
+// rows 54 / 40; 1 x 1024, 10 rows 17 / 18).
+constexpr int kFewRows = 16;
 cudaError_t launch_attn(const AttnArgs &a, int dtype, cudaStream_t st) {
-  if (a.pv.k && (int64_t)a.max_new * a.G <= 64) return launch_attn_rows(a, dtype, st);
+  if (a.pv.k && (int64_t)a.max_new * a.G <= kFewRows) return launch_attn_rows(a, dtype, st);
   return launch_attn_tc(a, dtype, st);
 }
 
@@ -361,6 +368,7 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.sig_log2 = softmax_scale * kLog2e;
   const PagedWs w = paged_ws(p->d.head_dim);
   a.list = reinterpret_cast<RowsList *>(p->ws + w.list);
+  a.tc_list = reinterpret_cast<TcList *>(p->ws + w.tc_list);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
   const PageMap *maps = &p->maps[(size_t)layer * 6];
