@@ -31,6 +31,8 @@
 #include <math.h>
 #include <string.h>
 
+#include <type_traits>
+
 #include <algorithm>
 
 #include "common.cuh"
@@ -418,107 +420,111 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       }
     }
   } else if (warp == 8) {
-    // -- products ---------------------------------------------------------------
-    if (lane == 0) {
-      constexpr uint32_t id_s = BF16 ? umma_idesc(128, kTcT, false, false) : umma_idesc_f16(128, kTcT, false, false);
-      constexpr uint32_t id_v = BF16 ? umma_idesc(128, D, false, true) : umma_idesc_f16(128, D, false, true);
-      constexpr uint32_t hi = umma_desc_hi_sw128(1024);
-      int s = 0;
-      uint32_t ph = 0;
-      int loads = 0;
-      uint32_t cleans = 0;  // parity of either stage's vclean
-      int tiles[2] = {0, 0}, done[2] = {0, 0};  // tiles, and jobs with any, of either query tile
-      auto scores = [&](int i, int at) {
-        const uint32_t q = umma_desc_lo(smem_u32(sm + SM::kQ + i * SM::kTile), 16);
-        const uint32_t kk = umma_desc_lo(smem_u32(sm + SM::kRing + at * SM::kTile), 16);
+    // -- products.  The whole warp runs the loop and one lane issues: operands
+    // then stay in uniform registers, and a product is issued in fewer cycles
+    // than it takes (a lone lane needed as many, so that every wait between
+    // products left the pipe idle).
+    constexpr uint32_t id_s = BF16 ? umma_idesc(128, kTcT, false, false) : umma_idesc_f16(128, kTcT, false, false);
+    constexpr uint32_t id_v = BF16 ? umma_idesc(128, D, false, true) : umma_idesc_f16(128, D, false, true);
+    constexpr uint32_t hi = umma_desc_hi_sw128(1024);
+    const uint32_t ring = smem_u32(sm + SM::kRing), q_at = umma_desc_lo(smem_u32(sm + SM::kQ), 16);
+    const bool leader = elect_one();
+    int s = 0;
+    uint32_t ph = 0, loads = 0, cleans = 0;   // cleans: parity of either stage's vclean
+    uint32_t tiles[2] = {0, 0}, done[2] = {0, 0};  // of either query tile: parity of its tiles, jobs with any
+    auto scores = [&](auto I, int at) {
+      constexpr int i = decltype(I)::value;
+      const uint32_t q = q_at + i * (SM::kTile >> 4), kk = umma_desc_lo(ring + at * SM::kTile, 16);
 #pragma unroll
-        for (int b = 0; b < D / 64; ++b)
+      for (int b = 0; b < D / 64; ++b)
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            umma_f16_ss_w(tS + 128 * i, q + b * (kBox >> 4) + 2 * x, kk + b * (kBox >> 4) + 2 * x, hi, id_s, b + x > 0);
-        umma_commit(&sfull[i]);
-      };
-      auto values = [&](int i, int at, bool acc) {
-        const uint32_t vv = umma_desc_lo(smem_u32(sm + SM::kRing + at * SM::kTile), kBox);
+        for (int x = 0; x < 4; ++x)
+          umma_f16_ss_if(leader, tS + 128 * i, q + b * (kBox >> 4) + 2 * x, kk + b * (kBox >> 4) + 2 * x, hi, id_s, b + x > 0);
+      umma_commit_if(leader, &sfull[i]);
+    };
+    auto values = [&](auto I, int at, bool acc) {
+      constexpr int i = decltype(I)::value;
+      const uint32_t vv = umma_desc_lo(ring + at * SM::kTile, kBox);
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          if (!wait(&pfull[2 * i + hf], tiles[i] & 1)) return false;
-          tc_fence_after();
-#pragma unroll
-          for (int x = 4 * hf; x < 4 * hf + 4; ++x)
-            umma_f16_ts_w(tO + D * i, tS + 128 * i + 8 * x, vv + 128 * x, hi, id_v, acc || x > 0);
-        }
-        umma_commit(&odone[i]);
-        ++tiles[i];
-        return true;
-      };
-      bool ok = true;
-      for (int k = 0; ok; ++k) {
-        const int slot = k & 1;
-        if (!wait(&jfull[slot], (k / 2) & 1)) break;
-        const Job j = jobs[slot];
-        mbar_arrive(&jfree[slot]);
-        if (j.b < 0) break;
-        if (j.nt == 0) continue;
-        if (!wait(qfull, loads & 1)) break;
-        ++loads;
-        // K of tile 0
-        if (!wait(&full[s], ph)) break;
+      for (int hf = 0; hf < 2; ++hf) {
+        if (!wait(&pfull[2 * i + hf], tiles[i])) return false;
         tc_fence_after();
-        for (int i = 0; i < 2; ++i)
-          if (j.js[i] == 0 && j.je[i] > 0) scores(i, s);
-        umma_commit(&free_[s]);
-        if (j.nt == 1) umma_commit(qfree);
-        int sv = s + 1, phv = ph;
-        if (sv == NS) sv = 0, phv ^= 1;
-        for (int jt = 0; jt < j.nt && ok; ++jt) {
-          const int t0 = j.lo + jt * kTcT;
-          int sk = sv + 1, phk = phv;
-          if (sk == NS) sk = 0, phk ^= 1;
-          bool have_v = false, have_k = false;
-          for (int i = 0; i < 2 && ok; ++i) {
-            if (jt >= j.js[i] && jt < j.je[i]) {
-              if (!have_v) {
-                ok = wait(&full[sv], phv);
-                if (ok && (t0 + kTcT - 1 > j.first || t0 < j.low)) {
-                  ok = wait(&vclean[sv], cleans >> sv & 1);
-                  cleans ^= 1u << sv;
-                }
-                tc_fence_after();
-                have_v = true;
-              }
-              if (ok && jt == j.js[i]) {
-                // the tile's last result has been read
-                if (done[i] > 0) ok = wait(&ofree[i], (done[i] - 1) & 1);
-                ++done[i];
-              }
-              if (ok) ok = values(i, sv, jt > j.js[i]);
-            }
-            if (ok && jt + 1 >= j.js[i] && jt + 1 < j.je[i]) {
-              if (!have_k) {
-                ok = wait(&full[sk], phk);
-                tc_fence_after();
-                have_k = true;
-              }
-              if (ok) scores(i, sk);
-            }
-          }
-          if (!ok) break;
-          umma_commit(&free_[sv]);
-          if (jt + 1 < j.nt) {
-            umma_commit(&free_[sk]);
-            if (jt + 2 == j.nt) umma_commit(qfree);
-          }
-          s = sk, ph = phk;
-          sv = sk + 1, phv = phk;
-          if (sv == NS) sv = 0, phv ^= 1;
+#pragma unroll
+        for (int x = 4 * hf; x < 4 * hf + 4; ++x)
+          umma_f16_ts_if(leader, tO + D * i, tS + 128 * i + 8 * x, vv + 128 * x, hi, id_v, acc || x > 0);
+      }
+      umma_commit_if(leader, &odone[i]);
+      tiles[i] ^= 1;
+      return true;
+    };
+    constexpr std::integral_constant<int, 0> i0;
+    constexpr std::integral_constant<int, 1> i1;
+    bool ok = true;
+    for (int k = 0; ok; ++k) {
+      const int slot = k & 1;
+      if (!wait(&jfull[slot], (k / 2) & 1)) break;
+      const Job *j = &jobs[slot];
+      const int jb = j->b, nt = j->nt, lo = j->lo, first = j->first, low = j->low;
+      const int js0 = j->js[0], je0 = j->je[0], js1 = j->js[1], je1 = j->je[1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&jfree[slot]);
+      if (jb < 0) break;
+      if (nt == 0) continue;
+      if (!wait(qfull, loads)) break;
+      loads ^= 1;
+      // K of tile 0
+      if (!wait(&full[s], ph)) break;
+      tc_fence_after();
+      if (js0 == 0 && je0 > 0) scores(i0, s);
+      if (js1 == 0 && je1 > 0) scores(i1, s);
+      umma_commit_if(leader, &free_[s]);
+      if (nt == 1) umma_commit_if(leader, qfree);
+      if (++s == NS) s = 0, ph ^= 1;
+      for (int jt = 0; jt < nt; ++jt) {
+        // V of this tile at s, K of the next at sk
+        int sk = s + 1;
+        uint32_t phk = ph;
+        if (sk == NS) sk = 0, phk ^= 1;
+        const bool more = jt + 1 < nt;
+        const int t0 = lo + jt * kTcT;
+        if (!(ok = wait(&full[s], ph))) break;
+        if (t0 + kTcT - 1 > first || t0 < low) {
+          if (!(ok = wait(&vclean[s], cleans >> s & 1))) break;
+          cleans ^= 1u << s;
         }
+        // either tile's values, then its next scores: a tile's softmax runs
+        // beside the other's products
+        auto half = [&](auto I, int js, int je) {
+          constexpr int i = decltype(I)::value;
+          if (jt >= js && jt < je) {
+            if (jt == js) {  // the tile's last result has been read
+              if (done[i] > 0 && !wait(&ofree[i], (done[i] - 1) & 1)) return false;
+              ++done[i];
+            }
+            if (!values(I, s, jt > js)) return false;
+          }
+          if (more && i == 0) {
+            if (!wait(&full[sk], phk)) return false;
+            tc_fence_after();
+          }
+          if (jt + 1 >= js && jt + 1 < je) scores(I, sk);
+          return true;
+        };
+        if (!(ok = half(i0, js0, je0))) break;
+        if (!(ok = half(i1, js1, je1))) break;
+        umma_commit_if(leader, &free_[s]);
+        if (more) {
+          umma_commit_if(leader, &free_[sk]);
+          if (jt + 2 == nt) umma_commit_if(leader, qfree);
+        }
+        s = sk, ph = phk;
+        if (more && ++s == NS) s = 0, ph ^= 1;
       }
-      // after a wait that gave up: the products in flight end before TMEM is freed
-      if (*abort_flag) {
-        umma_commit(drain);
-        mbar_wait(drain, 0, kWaits);
-      }
+    }
+    // after a wait that gave up: the products in flight end before TMEM is freed
+    if (*abort_flag) {
+      umma_commit_if(leader, drain);
+      mbar_wait(drain, 0, kWaits);
     }
     __syncwarp();
   } else if (warp >= 10) {

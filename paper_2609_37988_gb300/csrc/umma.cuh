@@ -67,6 +67,37 @@ __device__ __forceinline__ void umma_f16_ss_w(uint32_t d_tmem, uint32_t a_lo, ui
       "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate ? 1 : 0)
       : "memory");
 }
+// The same products and commits issued by whole warps, of which the lane with
+// `leader` set (elect_one) issues: the operands are the warp's and can stay in
+// uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t e;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(e));
+  return e != 0;
+}
+__device__ __forceinline__ void umma_f16_ss_if(bool leader, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t hi,
+                                               uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n .reg .b64 da, db;\n setp.ne.b32 p, %5, 0;\n setp.ne.b32 e, %6, 0;\n mov.b64 da, {%1, %3};\n"
+      " mov.b64 db, {%2, %3};\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %4, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_lo), "r"(b_lo), "r"(hi), "r"(idesc), "r"(accumulate ? 1 : 0), "r"(leader ? 1 : 0)
+      : "memory");
+}
+__device__ __forceinline__ void umma_f16_ts_if(bool leader, uint32_t d_tmem, uint32_t a_tmem, uint32_t b_lo, uint32_t b_hi,
+                                               uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p, e;\n .reg .b64 db;\n setp.ne.b32 p, %5, 0;\n setp.ne.b32 e, %6, 0;\n mov.b64 db, {%2, %3};\n"
+      " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate ? 1 : 0), "r"(leader ? 1 : 0)
+      : "memory");
+}
+__device__ __forceinline__ void umma_commit_if(bool leader, uint64_t *bar) {
+  asm volatile(
+      "{\n .reg .pred e;\n setp.ne.b32 e, %1, 0;\n"
+      " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(bar)),
+      "r"(leader ? 1 : 0)
+      : "memory");
+}
 // the words of umma_desc(addr, lbo, sbo, 2) (128-byte swizzle)
 __device__ __forceinline__ uint32_t umma_desc_lo(uint32_t addr, uint32_t lbo) {
   return ((addr >> 4) & 0x3FFF) | (((lbo >> 4) & 0x3FFF) << 16);
