@@ -9,11 +9,18 @@
 // nothing else, and cospi/sinpi of the leading 32 bits follow.  (The angle in
 // binary32 would be off by 0.06 at position 10^6.)
 //
-// Memory-bound: every channel is read once and written once.  A CTA takes
-// `tok` tokens; 2 * VEC channels per thread and step (two 16-byte pieces), the
-// first ones loaded before the angles, whose latency they hide.  Rounding:
-// binary32 arithmetic, one rounding to the stored type.
+// Memory-bound: every channel is read once and written once.  A thread keeps one
+// place in the rows of one token, 2 * VEC channels (two 16-byte pieces), with
+// its cosines and sines in registers, and goes over a part of the token's heads,
+// always with the next two rows' loads in flight; the first two leave before
+// the angles are worked out.  (A thread that keeps a head and goes over tokens
+// reads twice the bytes of its data in cosines and sines from shared memory:
+// 16384 tokens of a 14B-shaped layer took 84-147 us so.)  Rounding: binary32
+// arithmetic, one rounding to the stored type.
 #include <math.h>
+
+#include <algorithm>
+#include <type_traits>
 
 #include "common.cuh"
 #include "kernels.h"
@@ -23,6 +30,8 @@ namespace kvk {
 namespace {
 
 constexpr int kRotThreads = 256;
+constexpr int kRotTokens = 16;  // of a CTA at most
+
 constexpr int kErrCapacity = 2, kErrPage = 32;  // KVK_DEVERR_*
 
 template <typename T>
@@ -46,6 +55,50 @@ template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC) Piece {
   T x[VEC];
 };
+template <typename T>
+constexpr bool kIsBf16 = std::is_same<T, __nv_bfloat16>::value;
+
+// Pairs (x, y) -> (x c - y s, y c + x s) of two pieces, (c, s) = w[i]: channel i
+// of x0 with channel i of x1, or neighbours.
+template <typename T, int VEC>
+__device__ __forceinline__ void rotate(Piece<T, VEC> &x0, Piece<T, VEC> &x1, const float2 *w, bool adjacent) {
+  if constexpr (sizeof(T) == 2 && VEC % 2 == 0) {
+    constexpr int N = VEC / 2;  // words of a piece
+    uint32_t(&u)[N] = reinterpret_cast<uint32_t(&)[N]>(x0), (&v)[N] = reinterpret_cast<uint32_t(&)[N]>(x1);
+    constexpr bool B = kIsBf16<T>;
+    if (!adjacent) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float2 x = unpack2<B>(u[i]), y = unpack2<B>(v[i]), p = w[2 * i], q = w[2 * i + 1];
+        u[i] = pack2<B>(x.x * p.x - y.x * p.y, x.y * q.x - y.y * q.y);
+        v[i] = pack2<B>(y.x * p.x + x.x * p.y, y.y * q.x + x.y * q.y);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const float2 x = unpack2<B>(u[i]), y = unpack2<B>(v[i]), p = w[i], q = w[N + i];
+        u[i] = pack2<B>(x.x * p.x - x.y * p.y, x.y * p.x + x.x * p.y);
+        v[i] = pack2<B>(y.x * q.x - y.y * q.y, y.y * q.x + y.x * q.y);
+      }
+    }
+  } else {
+    auto turn = [&](T &a, T &b, float2 r) {
+      const float x = to_f(a), y = to_f(b);
+      a = from_f<T>(x * r.x - y * r.y);
+      b = from_f<T>(y * r.x + x * r.y);
+    };
+    if (!adjacent || VEC == 1) {
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) turn(x0.x[i], x1.x[i], w[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i + 1 < VEC; i += 2) {
+        turn(x0.x[i], x0.x[i + 1], w[i / 2]);
+        turn(x1.x[i], x1.x[i + 1], w[(VEC + i) / 2]);
+      }
+    }
+  }
+}
 
 // Where token t goes: its sequence and position, or nothing.
 struct Place {
@@ -81,150 +134,101 @@ __device__ Place find_place(const PagedView &v, int t, int lane) {
 }
 
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotArgs a, int tok, uint32_t ipr_magic) {
+__global__ void __launch_bounds__(kRotThreads) rotary_kernel(const __grid_constant__ RotArgs a, int tok) {
   extern __shared__ float2 cs[];  // [tok][n_freq]
-  __shared__ Place s_place[8];
+  __shared__ Place s_place[kRotTokens];
   using P = Piece<T, VEC>;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int t0 = blockIdx.x * tok;
-  const int nt = min(tok, a.n_tokens - t0);
-  const int ipr = a.D / (2 * VEC);              // steps of a row
-  const int rows = a.Hq + a.Hk + a.Hv;
-  const int half = a.t.n_freq, rot = half / VEC;
-  const int total = nt * rows * ipr;
+  const int t0 = blockIdx.x * tok, nt = min(tok, a.n_tokens - t0);
+  const int half = a.t.n_freq;
   const bool paged = a.pv.k != nullptr;
 
-  // step e: row r of the CTA's tokens, pieces at channels c0 and c1; the
-  // first `turn` kinds are rotated with frequencies f..
-  struct Step {
-    const T *src;
-    T *dst;       // null: not stored
-    int c0, c1, f, j;
-    bool turn;
-  };
-  auto decode = [&](int e, bool want_dst) {
-    Step s;
-    const int row = ipr == 1 ? e : (int)__umulhi((uint32_t)e, ipr_magic), c = e - row * ipr;
-    s.j = row / rows;
-    const int h = row - s.j * rows;
-    const int64_t t = t0 + s.j;
-    const Rows *in, *out;
-    int hh = h;
-    bool to_page = false;
-    uint8_t *pages = nullptr;
-    if (h < a.Hq) {
-      in = &a.q;
-      out = &a.qo;
-    } else if (h < a.Hq + a.Hk) {
-      hh = h - a.Hq;
-      in = &a.k;
-      out = &a.ko;
-      to_page = paged;
-      pages = a.pv.k;
-    } else {
-      hh = h - a.Hq - a.Hk;
-      in = &a.v;
-      out = &a.v;
-      to_page = true;
-      pages = a.pv.v;
-    }
-    s.src = reinterpret_cast<const T *>(in->p) + t * in->ts + hh * in->hs;
-    s.turn = h < a.Hq + a.Hk && c < rot;
-    s.f = c * VEC;
-    if (s.turn) {
-      s.c0 = a.t.adjacent ? 2 * VEC * c : VEC * c;
-      s.c1 = a.t.adjacent ? s.c0 + VEC : s.c0 + half;
-    } else {
-      s.c0 = 2 * VEC * c;  // channels behind the rotated ones (2 * half of them), or a value row's
-      s.c1 = s.c0 + VEC;
-    }
-    s.dst = nullptr;
-    if (want_dst) {
-      const Place &pl = s_place[s.j];
-      if (to_page) {
-        if (pl.slot >= 0)
-          s.dst = reinterpret_cast<T *>(pages) + (pl.slot + ((int64_t)hh << a.pv.page_shift)) * a.D;
-      } else if (!paged || pl.seq >= 0) {
-        s.dst = reinterpret_cast<T *>(out->p) + t * out->ts + hh * out->hs;
-      }
-    }
-    return s;
-  };
+  // this thread's place: piece c of the rows of token j, heads g, g + step, ...
+  const int ipr = a.D / (2 * VEC), groups = kRotThreads / ipr, step = groups / tok;
+  const int grp = tid / ipr, c = tid - grp * ipr, j = grp / step, g = grp - j * step;
+  const bool on = j < nt;
+  const bool turn = c < half / VEC;
+  const int f = c * VEC;
+  // channels: the turned ones, or those behind them (2 half of them)
+  const int c0 = turn && !a.t.adjacent ? f : 2 * f, c1 = turn && !a.t.adjacent ? f + half : c0 + VEC;
+  const int64_t t = t0 + j;
 
+  // row r of the token: queries, then keys, then values
+  const int rows = a.Hq + a.Hk + a.Hv;
+  auto load = [&](int r, P &x0, P &x1) {
+    if (!on || r >= rows) return;
+    const bool q = r < a.Hq, v = r >= a.Hq + a.Hk;
+    const Rows &in = q ? a.q : v ? a.v : a.k;
+    const T *src = reinterpret_cast<const T *>(in.p) + t * in.ts + (r - (q ? 0 : v ? a.Hq + a.Hk : a.Hq)) * in.hs;
+    x0 = *reinterpret_cast<const P *>(src + (v ? 2 * f : c0));
+    x1 = *reinterpret_cast<const P *>(src + (v ? 2 * f + VEC : c1));
+  };
   pdl_wait();
-  // the first step's data, before the angles
-  P x0, x1;
-  if (tid < total) {
-    const Step s = decode(tid, false);
-    x0 = *reinterpret_cast<const P *>(s.src + s.c0);
-    x1 = *reinterpret_cast<const P *>(s.src + s.c1);
-  }
+  P xa[2], xb[2];
+  load(g, xa[0], xa[1]);
+  load(g + step, xb[0], xb[1]);
   if (paged) {
-    for (int j = warp; j < nt; j += kRotThreads / 32) {
-      const Place p = find_place(a.pv, t0 + j, lane);
-      if (lane == 0) s_place[j] = p;
+    for (int i = warp; i < nt; i += kRotThreads / 32) {
+      const Place p = find_place(a.pv, t0 + i, lane);
+      if (lane == 0) s_place[i] = p;
     }
     if (!a.pos) __syncthreads();
   }
   for (int i = tid; i < nt * half; i += kRotThreads) {
-    const int j = i / half, f = i - j * half;
-    const int p = a.pos ? a.pos[(int64_t)a.t.axis[f] * a.n_tokens + t0 + j] : s_place[j].pos;
+    const int jj = i / half, fr = i - jj * half;
+    const int p = a.pos ? a.pos[(int64_t)a.t.axis[fr] * a.n_tokens + t0 + jj] : s_place[jj].pos;
     // the angle's leading 32 bits, a signed fraction of a turn
-    const uint64_t turn = a.t.step[f] * (uint64_t)(int64_t)p;
-    const float x = (float)(int32_t)(uint32_t)(turn >> 32) * 0x1p-31f;  // in half turns
-    float sn, c;
-    sincospif(x, &sn, &c);
-    cs[i] = make_float2(c * a.t.factor, sn * a.t.factor);
+    const uint64_t angle = a.t.step[fr] * (uint64_t)(int64_t)p;
+    const float x = (float)(int32_t)(uint32_t)(angle >> 32) * 0x1p-31f;  // in half turns
+    float sn, cn;
+    sincospif(x, &sn, &cn);
+    cs[i] = make_float2(cn * a.t.factor, sn * a.t.factor);
   }
   __syncthreads();
-  for (int e = tid; e < total; e += kRotThreads) {
-    const Step s = decode(e, true);
-    if (e != tid) {
-      x0 = *reinterpret_cast<const P *>(s.src + s.c0);
-      x1 = *reinterpret_cast<const P *>(s.src + s.c1);
-    }
-    if (!s.dst) continue;
-    if (s.turn) {
-      const float2 *w = cs + s.j * half + s.f;
-      P y0, y1;
-      if (!a.t.adjacent) {
+  if (on) {
+    float2 w[VEC];
+    if (turn) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float u = to_f(x0.x[i]), v = to_f(x1.x[i]);
-          y0.x[i] = from_f<T>(u * w[i].x - v * w[i].y);
-          y1.x[i] = from_f<T>(v * w[i].x + u * w[i].y);
-        }
+      for (int i = 0; i < VEC; ++i) w[i] = cs[j * half + f + i];
+    }
+    const Place pl = paged ? s_place[j] : Place{0, 0, 0};
+    auto finish = [&](int r, P &x0, P &x1) {
+      if (r >= rows) return;
+      const bool q = r < a.Hq, v = r >= a.Hq + a.Hk;
+      T *dst;
+      if (q || !paged) {
+        if (pl.seq < 0) return;
+        const Rows &out = q ? a.qo : a.ko;
+        dst = reinterpret_cast<T *>(out.p) + t * out.ts + (r - (q ? 0 : a.Hq)) * out.hs;
       } else {
-        T in[2 * VEC], out[2 * VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) in[i] = x0.x[i], in[VEC + i] = x1.x[i];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-          const float u = to_f(in[2 * i]), v = to_f(in[2 * i + 1]);
-          out[2 * i] = from_f<T>(u * w[i].x - v * w[i].y);
-          out[2 * i + 1] = from_f<T>(v * w[i].x + u * w[i].y);
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) y0.x[i] = out[i], y1.x[i] = out[VEC + i];
+        if (pl.slot < 0) return;
+        dst = reinterpret_cast<T *>(v ? a.pv.v : a.pv.k) +
+              (pl.slot + ((int64_t)(r - (v ? a.Hq + a.Hk : a.Hq)) << a.pv.page_shift)) * a.D;
       }
-      x0 = y0;
-      x1 = y1;
+      if (!v && turn) rotate<T, VEC>(x0, x1, w, a.t.adjacent);
+      *reinterpret_cast<P *>(dst + (v ? 2 * f : c0)) = x0;
+      *reinterpret_cast<P *>(dst + (v ? 2 * f + VEC : c1)) = x1;
+    };
+    for (int r = g; r < rows; r += 2 * step) {
+      finish(r, xa[0], xa[1]);
+      load(r + 2 * step, xa[0], xa[1]);
+      finish(r + step, xb[0], xb[1]);
+      load(r + 3 * step, xb[0], xb[1]);
     }
-    *reinterpret_cast<P *>(s.dst + s.c0) = x0;
-    *reinterpret_cast<P *>(s.dst + s.c1) = x1;
   }
   pdl_trigger();
 }
 
 template <typename T, int VEC>
 cudaError_t launch_t(const RotArgs &a, cudaStream_t st) {
-  const int ipr = a.D / (2 * VEC);
-  // One token per CTA fills the machine soonest; with thousands of tokens
-  // four per CTA leave fewer CTAs to start.
-  const int tok = a.n_tokens >= 4096 ? 4 : 1;
-  const dim3 grid((a.n_tokens + tok - 1) / tok);
-  const uint32_t magic = (uint32_t)(((1ull << 32) + ipr - 1) / ipr);
-  return launch_pdl(rotary_kernel<T, VEC>, grid, dim3(kRotThreads), (size_t)tok * a.t.n_freq * sizeof(float2), st, a, tok, magic);
+  // Tokens of a CTA: as many as leave a thread six rows or so (16384 tokens of a
+  // 14B-shaped layer: 104, 78, 66, 77 us with 1, 2, 4, 8), fewer where that would
+  // leave SMs without work: one token per CTA is the quickest for few.
+  const int ipr = a.D / (2 * VEC), groups = kRotThreads / ipr, rows = a.Hq + a.Hk + a.Hv;
+  int tok = 1;
+  while (2 * tok <= std::min(kRotTokens, groups) && 2 * tok * rows <= 7 * groups && a.n_tokens / (2 * tok) >= 600) tok *= 2;
+  return launch_pdl(rotary_kernel<T, VEC>, dim3((a.n_tokens + tok - 1) / tok), dim3(kRotThreads),
+                    (size_t)tok * a.t.n_freq * sizeof(float2), st, a, tok);
 }
 
 bool rows_aligned(const Rows &r, int elem) {
