@@ -101,10 +101,11 @@ __device__ __forceinline__ void tmem_ld32_nw(uint32_t taddr, float *v) {
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
+// Sets the top bit of a half where w's half is not finite: an exponent of all
+// ones carries out of its field.
 template <bool BF16>
-__device__ __forceinline__ bool pair_fine(uint32_t w) {
-  constexpr uint32_t m = BF16 ? 0x7F80u : 0x7C00u;
-  return (w & m) != m && (w >> 16 & m) != m;
+__device__ __forceinline__ uint32_t carries(uint32_t w) {
+  return BF16 ? (w & 0x7F807F80u) + 0x00800080u : (w & 0x7C007C00u) + 0x04000400u;
 }
 template <bool BF16>
 __device__ __forceinline__ uint32_t pair_scrubbed(uint32_t w) {
@@ -112,6 +113,12 @@ __device__ __forceinline__ uint32_t pair_scrubbed(uint32_t w) {
   if ((w & m) == m) w &= 0xFFFF0000u;
   if ((w >> 16 & m) == m) w &= 0xFFFFu;
   return w;
+}
+
+// x / y, in 32 bits where they do (a 64-bit division takes 500 cycles)
+__device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
+  if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+  return x / y;
 }
 
 // Tokens of sequence b, its first one in the batch.
@@ -158,6 +165,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     }
     *abort_flag = 0;
     fence_mbar_init();
+  }
+  if (warp == 9 && lane == 0) {
+    prefetch_tensor_map(&t.mq);
+    prefetch_tensor_map(&t.mk);
+    prefetch_tensor_map(&t.mv);
   }
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tbase)), "n"(512)
@@ -278,9 +290,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       }
       return true;
     };
-    auto blocks = [&](int b) {
+    // blocks of sequence b; those of the first 128 stay in registers, four a lane
+    auto read_blocks = [&](int b) {
       int q0;
-      return (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P);
+      return b < pv.B ? (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P) : 0;
     };
     Job end = {};
     end.b = -1;
@@ -291,6 +304,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       auto head_tiles = [&](int b) {
         int q0, sum = 0;
         const int n = seq_tokens(pv, b, q0);
+        if (n == 0) return 0;
         const int p0 = (int)min((int64_t)max(pv.lens[b], 0), (int64_t)pv.max_pages << pv.page_shift) - n;
         for (int tok = 0; tok < n; tok += 2 * P) {
           const int last = p0 + min(n, tok + 2 * P) - 1, lo = max(0, p0 + tok - a.window + 1) / kTcT;
@@ -298,18 +312,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         }
         return sum;
       };
-      int64_t total = 0;
-      for (int b = lane; b < pv.B; b += 32) total += (int64_t)pv.Hkv * head_tiles(b);
+      const int tiles0 = lane < pv.B ? head_tiles(lane) : 0;
+      int64_t total = (int64_t)pv.Hkv * tiles0;
+      for (int b = lane + 32; b < pv.B; b += 32) total += (int64_t)pv.Hkv * head_tiles(b);
       for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
-      const int64_t share = max((total + gridDim.x - 1) / gridDim.x, (int64_t)kTcMinShare);
+      const int64_t share = max(div_pos(total + gridDim.x - 1, gridDim.x), (int64_t)kTcMinShare);
       const int64_t w0 = share * blockIdx.x;
       int left = (int)max(min(share, total - w0), (int64_t)0);
       if (left > 0) {
         // the sequence, head, block and tile where the run starts
         int b = 0, h = 0, blk = 0, t = 0;
         int64_t off = 0;
+        int per = 0;  // of the sequence found
         for (int b0 = 0;; b0 += 32) {
-          const int64_t x = b0 + lane < pv.B ? (int64_t)pv.Hkv * head_tiles(b0 + lane) : 0;
+          const int tl = b0 == 0 ? tiles0 : b0 + lane < pv.B ? head_tiles(b0 + lane) : 0;
+          const int64_t x = (int64_t)pv.Hkv * tl;
           int64_t sum = x;
           for (int o = 1; o < 32; o <<= 1) {
             const int64_t y = __shfl_up_sync(kAll, sum, o);
@@ -319,14 +336,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           if (past) {
             const int f = __ffs(past) - 1;
             b = b0 + f;
+            per = __shfl_sync(kAll, tl, f);
             off = w0 - (off + __shfl_sync(kAll, sum - x, f));
             break;
           }
           off += __shfl_sync(kAll, sum, 31);
         }
         int q0, n = seq_tokens(pv, b, q0);
-        const int per = head_tiles(b);
-        h = (int)(off / per);
+        h = (int)div_pos(off, per);
         t = (int)(off - (int64_t)h * per);
         Job j = describe(b, h, 0, q0, n);
         while (t >= max(1, j.nt)) {
@@ -368,18 +385,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         }
       }
     } else {
-      int total = 0, most = 0;
-      for (int b = lane; b < pv.B; b += 32) {
-        const int x = blocks(b);
+      int nb[4], total = 0, most = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) nb[i] = read_blocks(lane + 32 * i);
+      auto each = [&](auto &&f) {  // of this lane's sequences
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f(nb[i]);
+        for (int b = lane + 128; b < pv.B; b += 32) f(read_blocks(b));
+      };
+      each([&](int x) {
         total += x;
         most = max(most, x);
-      }
+      });
       total = (int)__reduce_add_sync(kAll, (unsigned)total);
       most = (int)__reduce_max_sync(kAll, (unsigned)most);
       // jobs at most `d` blocks from their sequence's end
       auto upto = [&](int d) {
         unsigned sum = 0;
-        for (int b = lane; b < pv.B; b += 32) sum += min(blocks(b), d);
+        each([&](int x) { sum += min(x, d); });
         return (int)__reduce_add_sync(kAll, sum);
       };
       const int n_jobs = total * pv.Hkv, step = gridDim.x;
@@ -397,7 +420,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         }
         int rem = r - f0, b = 0;
         for (int b0 = 0;; b0 += 32) {
-          const uint32_t in = __ballot_sync(kAll, b0 + lane < pv.B && blocks(min(b0 + lane, pv.B - 1)) > d0);
+          const int x = b0 == 0 ? nb[0] : b0 == 32 ? nb[1] : b0 == 64 ? nb[2] : b0 == 96 ? nb[3] : read_blocks(b0 + lane);
+          const uint32_t in = __ballot_sync(kAll, x > d0);
           const int c = __popc(in);
           if (rem < c) {
             b = b0 + (int)__fns(in, 0, rem + 1);
@@ -550,17 +574,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         if (t0 + kTcT - 1 > first || t0 < low) {
           uint4 *x = reinterpret_cast<uint4 *>(sm + SM::kRing + s * SM::kTile) + (warp - 10) * (SM::kTile / 32);
           bool fine = true;
+#pragma unroll 1
           for (int e = lane; e < SM::kTile / 32; e += 32 * 8) {
             uint4 u[8];
+            uint32_t any = 0;
 #pragma unroll
             for (int y = 0; y < 8; ++y) u[y] = x[e + 32 * y];
 #pragma unroll
             for (int y = 0; y < 8; ++y)
-              if (!(pair_fine<BF16>(u[y].x) && pair_fine<BF16>(u[y].y) && pair_fine<BF16>(u[y].z) && pair_fine<BF16>(u[y].w))) {
-                x[e + 32 * y] = make_uint4(pair_scrubbed<BF16>(u[y].x), pair_scrubbed<BF16>(u[y].y),
-                                           pair_scrubbed<BF16>(u[y].z), pair_scrubbed<BF16>(u[y].w));
-                fine = false;
+              any |= carries<BF16>(u[y].x) | carries<BF16>(u[y].y) | carries<BF16>(u[y].z) | carries<BF16>(u[y].w);
+            if (any & 0x80008000u) {
+              fine = false;
+#pragma unroll 1
+              for (int y = 0; y < 8; ++y) {
+                const uint4 w = x[e + 32 * y];
+                x[e + 32 * y] = make_uint4(pair_scrubbed<BF16>(w.x), pair_scrubbed<BF16>(w.y), pair_scrubbed<BF16>(w.z),
+                                           pair_scrubbed<BF16>(w.w));
               }
+            }
           }
           if (!fine) {
             js.bad = 1;
@@ -614,8 +645,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           const int past = lim - t0, before = low - t0;  // columns [before, past] are seen
           if (__any_sync(kAll, past < kTcT - 1 || before > 0)) {
 #pragma unroll
-            for (int c = 0; c < 128; ++c)
-              if (c > past || c < before) x[c] = -INFINITY;
+            for (int c = 0; c < 128; c += 32) {
+              const int to = min(max(past + 1 - c, 0), 32), from = min(max(before - c, 0), 32);
+              const uint32_t seen = (uint32_t)(((1ull << to) - 1) & ~((1ull << from) - 1));
+#pragma unroll
+              for (int y = 0; y < 32; ++y) x[c + y] = seen >> y & 1 ? x[c + y] : -INFINITY;
+            }
           }
           float mx[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
