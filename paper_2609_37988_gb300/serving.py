@@ -11,6 +11,9 @@ contiguous, any other strides (views of a fused projection, say).
     q = pages.append(layer, k, v, cu, lengths, table, rotary=rot, positions=pos, q=q)
     o = pages.attend(layer, q, cu, lengths, table, scale, max_new=1)
     o = prompt_attention(q, k, v, cu, scale)          # before anything is cached
+
+Calls run on the current stream, or on ``stream``: the caller then orders it with
+the streams its tensors belong to, and keeps them until it has run.
 """
 from __future__ import annotations
 
@@ -47,12 +50,9 @@ def _code(t: torch.Tensor) -> int:
 def _rows(t: torch.Tensor, name: str, dtype, index: int, shape) -> bytes:
     """``t`` as a kvk_rows: ``shape`` (tokens, heads, head_dim) of ``dtype`` on
     GPU ``index``, channels contiguous."""
-    if t.shape != shape or not t.is_cuda:
-        raise ValueError(f"{name} must be a CUDA tensor {tuple(shape)}, got {tuple(t.shape)} on {t.device}")
-    if t.dtype is not dtype:
-        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
-    if t.get_device() != index:
-        raise ValueError(f"{name} is on {t.device}, expected cuda:{index}")
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != index:
+        raise (TypeError if t.dtype is not dtype else ValueError)(
+            f"{name} must be {dtype} {tuple(shape)} on cuda:{index}, got {t.dtype} {tuple(t.shape)} on {t.device}")
     ts, hs, cs = t.stride()
     if cs != 1 and shape[2] > 1:
         raise ValueError(f"{name} must have contiguous channels")
@@ -60,9 +60,16 @@ def _rows(t: torch.Tensor, name: str, dtype, index: int, shape) -> bytes:
 
 
 def _ints(t: torch.Tensor, name: str, shape, index: int) -> int:
-    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
+    if t.shape != shape or t.dtype is not torch.int32 or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on cuda:{index}")
     return t.data_ptr()
+
+
+def _shape(t: torch.Tensor, name: str):
+    shape = t.shape
+    if len(shape) != 3 or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, head_dim]")
+    return shape
 
 
 def _call(index: int, stream, fn, *args):
@@ -79,10 +86,10 @@ def _call(index: int, stream, fn, *args):
 
 
 def _new_like(t: torch.Tensor, stream) -> torch.Tensor:
-    out = torch.empty_like(t, memory_format=torch.contiguous_format)
-    if stream is not None:
-        out.record_stream(stream)
-    return out
+    if stream is None:
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
+    with torch.cuda.stream(stream):  # the memory is that stream's
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def _out_like(out: torch.Tensor, t: torch.Tensor, stream) -> torch.Tensor:
@@ -141,9 +148,7 @@ class Rotary:
         x = q if q is not None else k
         if x is None:
             raise ValueError("q or k must be given")
-        if x.dim() != 3 or (k is not None and k.dim() != 3) or not x.is_cuda:
-            raise ValueError("q and k must be CUDA tensors [tokens, heads, head_dim]")
-        n, d, index, dtype = x.shape[0], self.head_dim, x.get_device(), x.dtype
+        n, d, index, dtype = _shape(x, "q or k")[0], self.head_dim, x.get_device(), x.dtype
         code = _code(x)
         rq = oq = rk = ok = q_out = k_out = None
         hq = hk = 0
@@ -158,7 +163,7 @@ class Rotary:
                 q_out = out[0]
                 oq = _rows(q_out, "q_out", dtype, index, shape)
         if k is not None:
-            hk = k.shape[1]
+            hk = _shape(k, "k")[1]
             shape = (n, hk, d)
             rk = _rows(k, "k", dtype, index, shape)
             if out is None:
@@ -305,17 +310,15 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     - 1``; ``window``: a query sees that many positions at most (0: all).
     ``error``: an int32 tensor of one element that gets device error bits.
     Returns ``[tokens, H_q, head_dim]``; rows in no sequence stay unwritten."""
-    if q.dim() != 3 or k.dim() != 3 or not q.is_cuda:
-        raise ValueError("q, k and v must be CUDA tensors [tokens, heads, head_dim]")
-    n, hq, d = q.shape
+    n, hq, d = _shape(q, "q")
     index, dtype = q.get_device(), q.dtype
-    kv = (n, k.shape[1], d)
+    kv = (n, _shape(k, "k")[1], d)
     rq = _rows(q, "q", dtype, index, q.shape)
     rk, rv = _rows(k, "k", dtype, index, kv), _rows(v, "v", dtype, index, kv)
     out = _out_like(out, q, stream)
-    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+    B = cu_seqlens.numel() - 1
+    if B < 0:
         raise ValueError("cu_seqlens must be [sequences + 1]")
-    B = cu_seqlens.shape[0] - 1
     _call(index, stream, load().kvk_prompt_attention, rq, rk, rv, n, hq, kv[1], d, _code(q),
           _ints(cu_seqlens, "cu_seqlens", (B + 1,), index), B, scale, window, out.data_ptr(),
           0 if error is None else _ints(error, "error", (1,), index))
