@@ -23,7 +23,8 @@
 //
 // Jobs in order of their distance from their sequence's end, all sequences
 // side by side: the longest first where lengths are equal, the short ones last
-// in any case; dealt to the CTAs back and forth.  Chunks over pages that make
+// in any case; dealt to the CTAs back and forth.  (More than 128 sequences go one
+// behind another: there are jobs enough to even out.)  Chunks over pages that make
 // few jobs go in equal runs of tiles instead, one per CTA: jobs that a run cuts
 // leave their pieces (result, reference and sum of each row) in the workspace,
 // and a second kernel joins them.
@@ -70,6 +71,7 @@ struct Job {
 // and sums
 constexpr int tc_part(int D) { return kTcT * (D + 2); }
 constexpr int kTcMinShare = 4;  // tiles of a run at least
+constexpr int kTcOrdered = 128;  // sequences whose jobs are put in order
 
 template <int D>
 struct Smem {
@@ -290,7 +292,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       }
       return true;
     };
-    // blocks of sequence b; those of the first 128 stay in registers, four a lane
     auto read_blocks = [&](int b) {
       int q0;
       return b < pv.B ? (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P) : 0;
@@ -384,25 +385,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           j = describe(b, h, blk, q0, n);
         }
       }
-    } else {
+    } else if (pv.B <= kTcOrdered) {
+      // blocks of the batch's sequences, four a lane
       int nb[4], total = 0, most = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) nb[i] = read_blocks(lane + 32 * i);
-      auto each = [&](auto &&f) {  // of this lane's sequences
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f(nb[i]);
-        for (int b = lane + 128; b < pv.B; b += 32) f(read_blocks(b));
-      };
-      each([&](int x) {
-        total += x;
-        most = max(most, x);
-      });
+      for (int i = 0; i < 4; ++i) {
+        nb[i] = read_blocks(lane + 32 * i);
+        total += nb[i];
+        most = max(most, nb[i]);
+      }
       total = (int)__reduce_add_sync(kAll, (unsigned)total);
       most = (int)__reduce_max_sync(kAll, (unsigned)most);
       // jobs at most `d` blocks from their sequence's end
       auto upto = [&](int d) {
         unsigned sum = 0;
-        each([&](int x) { sum += min(x, d); });
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += min(nb[i], d);
         return (int)__reduce_add_sync(kAll, sum);
       };
       const int n_jobs = total * pv.Hkv, step = gridDim.x;
@@ -419,19 +417,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             d1 = mid;
         }
         int rem = r - f0, b = 0;
-        for (int b0 = 0;; b0 += 32) {
-          const int x = b0 == 0 ? nb[0] : b0 == 32 ? nb[1] : b0 == 64 ? nb[2] : b0 == 96 ? nb[3] : read_blocks(b0 + lane);
-          const uint32_t in = __ballot_sync(kAll, x > d0);
-          const int c = __popc(in);
-          if (rem < c) {
-            b = b0 + (int)__fns(in, 0, rem + 1);
-            break;
-          }
-          rem -= c;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const uint32_t in = __ballot_sync(kAll, nb[c] > d0);
+          const int n = __popc(in);
+          if (rem >= 0 && rem < n) b = 32 * c + (int)__fns(in, 0, rem + 1);
+          rem -= n;
         }
         int q0;
         const int n = seq_tokens(pv, b, q0);
         ok = emit(describe(b, idx - r * pv.Hkv, (n + 2 * P - 1) / (2 * P) - 1 - d0, q0, n));
+      }
+    } else {
+      // sequence by sequence, the search going on from where the last job was
+      int b0 = 0, before = 0, x = 0, sum = 0;  // blocks of this lane's sequence; up to and with it
+      auto chunk = [&]() {
+        x = sum = read_blocks(b0 + lane);
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(kAll, sum, o);
+          if (lane >= o) sum += y;
+        }
+      };
+      chunk();
+      for (int64_t idx = blockIdx.x; ok; idx += gridDim.x) {
+        const int r = (int)(idx / pv.Hkv);
+        while (b0 < pv.B && before + __shfl_sync(kAll, sum, 31) <= r) {
+          before += __shfl_sync(kAll, sum, 31);
+          b0 += 32;
+          chunk();
+        }
+        if (b0 >= pv.B) break;
+        const int f = __ffs(__ballot_sync(kAll, before + sum > r)) - 1;
+        const int from_end = r - (before + __shfl_sync(kAll, sum - x, f));
+        int q0;
+        const int n = seq_tokens(pv, b0 + f, q0);
+        ok = emit(describe(b0 + f, (int)(idx - (int64_t)r * pv.Hkv), (n + 2 * P - 1) / (2 * P) - 1 - from_end, q0, n));
       }
     }
     if (ok) emit(end);

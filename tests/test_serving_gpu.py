@@ -474,9 +474,20 @@ def test_prompt_strides():
     prompt_case([130, 5, 260], 8, 2, 64, F16, seed=24, strided=True)
 
 
-def test_prompts_many_sequences():
+@pytest.mark.parametrize("count,longest", [(90, 40), (128, 60), (129, 60), (400, 30)])
+def test_prompts_many_sequences(count, longest):
     rng = np.random.default_rng(25)
-    prompt_case([int(x) for x in rng.integers(0, 40, 90)], 4, 2, 64, BF16, seed=25)
+    prompt_case([int(x) for x in rng.integers(0, longest, count)], 4, 2, 64, BF16, seed=25)
+    prompt_case([0] * (count - 2) + [300, 1], 2, 1, 128, F16, seed=26)
+
+
+@pytest.mark.parametrize("count", [33, 130])
+@pytest.mark.parametrize("most", [1, 3, 40])
+def test_many_sequences_over_pages(count, most):
+    rng = np.random.default_rng(27)
+    news = [int(x) for x in rng.integers(0, most + 1, count)]
+    lens = [int(x) for x in rng.integers(0, 70, count)]
+    Batch(news, lens, 10, 2, 64, BF16, 16, seed=28).fill().check(25)
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("-inf")])
