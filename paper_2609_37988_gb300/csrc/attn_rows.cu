@@ -79,7 +79,7 @@ __device__ __forceinline__ Seq load_seq(const PagedView &v, int b, int max_new) 
   s.q0 = c0;
   s.len = max(len, 0);
   const int64_t cap = (int64_t)v.max_pages << v.page_shift;
-  if (s.n > max_new || s.len > cap) {
+  if (s.n > 0 && (s.n > max_new || s.len > cap)) {
     set_err(v.err, kErrCount);
     s.n = min(s.n, max_new);
     s.len = (int)min((int64_t)s.len, cap);
@@ -156,7 +156,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a) {
   const int tid = threadIdx.x, v = tid % V, grp = tid / V;
   const int rows = a.hc * a.rows;
   pdl_wait();
-  const int n = *reinterpret_cast<volatile int *>(&a.list->n) * rows;
+  const int n = min(*reinterpret_cast<volatile int *>(&a.list->n), kRowsMaxCtas) * rows;
   const bool wide = n <= (int)gridDim.x;
   const int step = wide ? groups : 1;
   for (int item = wide ? blockIdx.x : blockIdx.x * groups + grp; item < n; item += gridDim.x * (wide ? 1 : groups)) {
@@ -636,7 +636,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     if (!whole && t_begin == 0 && tid == 0) {
       const int at_list = atomicAdd(&a.list->n, 1);  // a CTA adds one at most
       const int last = (int)blockIdx.x + (w_begin + at.nt - 1) / s_share;
-      a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, row0, R};
+      if ((unsigned)at_list < (unsigned)kRowsMaxCtas) a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, row0, R};
     }
     if (w < mine) {
       fence_proxy_async();
@@ -658,19 +658,14 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   memcpy(&ra.mv, a.whole ? a.ov : a.wv, sizeof ra.mv);
   ra.a = a;
   ra.a.rows = std::min(8 * NB, a.max_new * a.G);
-  static std::atomic<bool> ready{false};
-  if (!ready.load(std::memory_order_relaxed)) {
-    const cudaError_t e =
-        cudaFuncSetAttribute(attn_rows_kernel<D, NB, BF16>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != cudaSuccess) return e;
-    ready.store(true, std::memory_order_relaxed);
-  }
+  cudaError_t e = allow_smem<&attn_rows_kernel<D, NB, BF16>>(smem, a.device);
+  if (e != cudaSuccess) return e;
   // two CTAs per SM, no more of them than runs that there can be
   const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / (kT / a.hc) + 2;
   const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * ((a.max_new * a.G + 8 * NB - 1) / (8 * NB)) * cap;
   const int64_t runs = a.whole ? tiles / cap : (tiles + kMinShare - 1) / kMinShare;
   const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), runs);
-  const cudaError_t e = launch_pdl(attn_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
+  e = launch_pdl(attn_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
   if (e != cudaSuccess || a.whole) return e;
   // a unit cut in pieces starts in a CTA of its own; eight of the joining CTAs
   // fit an SM

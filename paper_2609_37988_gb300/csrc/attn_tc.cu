@@ -358,7 +358,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             if (t == 0 && lane == 0) {
               const int at = atomicAdd(&a.tc_list->n, 1);  // a CTA adds one at most
               const int before = (int)(share - left);
-              a.tc_list->unit[at] =
+              if ((unsigned)at < (unsigned)kTcMaxCtas)
+                a.tc_list->unit[at] =
                   TcSplit{(int)blockIdx.x, (int)blockIdx.x + (before + nt - 1) / (int)share, j.q0, j.n, j.p0, j.tok0, j.h};
             }
             j.lo += t * kTcT;
@@ -830,7 +831,7 @@ __global__ void __launch_bounds__(kTcT) attn_tc_join_kernel(const AttnArgs a, in
   const int row = threadIdx.x, tok_row = row / a.G;
   constexpr int C = D / 16;
   pdl_wait();
-  const int n = *reinterpret_cast<volatile int *>(&a.tc_list->n) * 2 * C;
+  const int n = min(*reinterpret_cast<volatile int *>(&a.tc_list->n), kTcMaxCtas) * 2 * C;
   for (int item = blockIdx.x; item < n; item += gridDim.x) {
     const TcSplit u = a.tc_list->unit[item / (2 * C)];
     const int i = item / C & 1, c = item % C;
@@ -887,13 +888,8 @@ cudaError_t rows_map(CUtensorMap *m, bool bf, void *p, int D, int64_t n1, int64_
 }
 template <int D, bool BF16, bool PAGED>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
-  static std::atomic<bool> ready{false};
-  cudaError_t e = cudaSuccess;
-  if (!ready.load(std::memory_order_relaxed)) {
-    e = cudaFuncSetAttribute(attn_tc_kernel<D, BF16, PAGED>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D>::kBytes);
-    if (e != cudaSuccess) return e;
-    ready.store(true, std::memory_order_relaxed);
-  }
+  cudaError_t e = allow_smem<&attn_tc_kernel<D, BF16, PAGED>>(Smem<D>::kBytes, a.device);
+  if (e != cudaSuccess) return e;
   TcArgs t;
   t.a = a;
   t.P = kTcT / a.G;

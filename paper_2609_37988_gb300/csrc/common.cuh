@@ -57,6 +57,19 @@ inline cudaError_t check_reg_split(const RegSplit &split) {
   return cudaSuccess;
 }
 
+// Lets kernel K use `smem` bytes of dynamic shared memory on device `dev`; the
+// runtime is asked once per kernel and device.
+template <auto K>
+inline cudaError_t allow_smem(int smem, int dev) {
+  static std::atomic<uint64_t> done{0};
+  const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+  if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+  const cudaError_t e =
+      cudaFuncSetAttribute(reinterpret_cast<const void *>(K), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 __device__ __forceinline__ void set_err(int32_t *err, int code) {
   if (err) atomicOr(err, code);
 }

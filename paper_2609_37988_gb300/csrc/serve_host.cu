@@ -63,7 +63,7 @@ kvk_status take_rows(const kvk_rows *r, const char *name, int n_tokens, int head
   return KVK_OK;
 }
 
-bool scale_ok(float s) { return std::isfinite(s) && s > 0.f; }
+bool scale_ok(float s) { return std::isfinite(s * 1.4426950408889634f) && s > 0.f; }
 
 // heads and widths that the attention kernels take
 kvk_status check_heads(int Hq, int Hkv, int D, int dtype) {
@@ -371,6 +371,7 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.tc_list = reinterpret_cast<TcList *>(p->ws + w.tc_list);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
+  a.device = p->device;
   const PageMap *maps = &p->maps[(size_t)layer * 6];
   a.mk = maps[0].bytes;
   a.mv = maps[1].bytes;
@@ -419,6 +420,7 @@ kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&a.sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "querying the device");
+  a.device = dev;
   a.pv.cu = cu_seqlens;
   a.pv.B = batch;
   a.pv.Hkv = n_kv_heads;

@@ -229,6 +229,7 @@ class PagedCache:
                                             ctypes.byref(h)))
             self.handle = h
             check(self.lib.kvk_paged_reset(h, _stream()))
+            torch.cuda.current_stream().synchronize()  # calls on any stream may follow
         self._index = dev.index
         self._append, self._attend = self.lib.kvk_paged_append, self.lib.kvk_paged_attention
 

@@ -313,6 +313,58 @@ def test_device_errors_and_recovery():
     assert torch.equal(keep, b.attend(0.125)) and b.cache.device_error() == 0
 
 
+def test_lengths_of_sequences_without_new_tokens_do_not_matter():
+    b = Batch([1, 0, 2], [70, 40, 90], 8, 2, 64, BF16, 16, seed=31).fill()
+    keep = b.attend(0.125)
+    for other in (10 ** 9, -5):
+        got = b.cache.attend(0, b.q.cuda(), b.cu, ints([70, other, 90]), b.table_d, 0.125, max_new=2)
+        assert torch.equal(keep, got) and b.cache.device_error() == 0
+        got = b.cache.attend(0, b.q.cuda(), b.cu, ints([70, other, 90]), b.table_d, 0.125, max_new=40)
+        assert b.cache.device_error() == 0
+
+
+@pytest.mark.parametrize("news", [[1, 2], [40, 70]])
+def test_pools_past_two_to_the_31_elements(news):
+    """Pages at both ends of pools of 2^31 + elements."""
+    from paper_2609_37988_gb300.serving import PagedCache
+    hq, hkv, d, page = 8, 8, 128, 128
+    n_pages = 2 ** 31 // (hkv * page * d) + 4
+    cache = PagedCache(n_q_heads=hq, n_kv_heads=hkv, n_layers=1, head_dim=d, n_pages=n_pages, page_size=page, dtype=BF16)
+    lens = [300, 200]
+    table = np.array([[n_pages - 1, 0, n_pages - 3], [n_pages - 2, 1, 0]])
+    g = gen(32)
+    k, v = [torch.randn((l, hkv, d), generator=g).to(BF16) for l in lens], [torch.randn((l, hkv, d), generator=g).to(BF16) for l in lens]
+    q = torch.randn((sum(news), hq, d), generator=g).to(BF16)
+    cache.append(0, torch.cat(k).cuda(), torch.cat(v).cuda(), offsets(lens), ints(lens), ints(table.tolist()))
+    got = cache.attend(0, q.cuda(), offsets(news), ints(lens), ints(table.tolist()), 0.088, max_new=max(news))
+    at = 0
+    for b, n in enumerate(news):
+        r = osv.attend(f64(q[at:at + n]), *(np.transpose(f64(x[b]), (1, 0, 2)) for x in (k, v)), 0.088)
+        close(got[at:at + n], r[0], osv.attend_bound(*r, d, lens[b], U[BF16], 0.0))
+        at += n
+    assert cache.device_error() == 0
+
+
+def test_two_caches_over_the_same_pools_at_once():
+    """Workspaces are a cache object's own: two of them run side by side."""
+    from paper_2609_37988_gb300.serving import PagedCache
+    a = Batch([1, 2, 1], [900, 300, 5], 10, 2, 128, BF16, 16, seed=33).fill()
+    b = Batch([30, 80], [700, 900], 10, 2, 128, BF16, 16, seed=34).fill()
+    twin = PagedCache(n_q_heads=10, k_pages=b.cache.k_pages, v_pages=b.cache.v_pages)
+    keep_a, keep_b = a.attend(0.088), b.attend(0.088)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    qa, qb = a.q.cuda(), b.q.cuda()
+    torch.cuda.synchronize()
+    outs = []
+    for _ in range(10):
+        outs.append((keep_a, a.attend(0.088, q=qa, stream=streams[0])))
+        outs.append((keep_b, b.attend(0.088, q=qb, stream=streams[1])))
+        outs.append((keep_b, twin.attend(0, qb, b.cu, b.lengths, b.table_d, 0.088, max_new=80, stream=streams[2])))
+    torch.cuda.synchronize()
+    assert all(torch.equal(x, y) for x, y in outs)
+
+
 def test_empty_batches():
     b = Batch([0, 0], [0, 40], 8, 2, 64, BF16, 16).fill()
     assert b.attend(0.125).shape == (0, 8, 64)
