@@ -728,8 +728,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           ++tiles;
         }
         if (!ok) break;
-        const bool sees = real && pos >= 0;
-        const float inv = sees ? 1.f / l : 0.f;
+        const float inv = real && pos >= 0 ? 1.f / l : 0.f;
         uint32_t nan[D / 32] = {};  // channels of which the row sees a value that is not finite
         if (je > js) {
           if (!wait(&odone[i], (tiles - 1) & 1)) break;
@@ -781,28 +780,31 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = 0.f;
           }
+          if (nan[c]) {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = nan[c] >> y & 1 ? NAN : o[y];
+          }
           if (slot_out >= 0 && real) {
 #pragma unroll
-            for (int y = 0; y < 8; ++y) {
-              float4 x = make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]);
-              if (nan[c] >> (4 * y) & 1) x.x = NAN;
-              if (nan[c] >> (4 * y) & 2) x.y = NAN;
-              if (nan[c] >> (4 * y) & 4) x.z = NAN;
-              if (nan[c] >> (4 * y) & 8) x.w = NAN;
-              __stcg(reinterpret_cast<float4 *>(part + (8 * c + y) * (4 * kTcT)), x);
-            }
+            for (int y = 0; y < 8; ++y)
+              __stcg(reinterpret_cast<float4 *>(part + (8 * c + y) * (4 * kTcT)),
+                     make_float4(o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]));
           } else if (real) {
+            // rows before position 0 have zeros here, and 0 as their factor
             uint32_t w[16];
 #pragma unroll
-            for (int y = 0; y < 16; ++y) {
-              float u = sees ? o[2 * y] * inv : 0.f, v = sees ? o[2 * y + 1] * inv : 0.f;
-              if (nan[c] >> (2 * y) & 1) u = NAN;
-              if (nan[c] >> (2 * y + 1) & 1) v = NAN;
-              w[y] = pack2<BF16>(u, v);
-            }
+            for (int y = 0; y < 16; ++y) w[y] = pack2<BF16>(o[2 * y] * inv, o[2 * y + 1] * inv);
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              reinterpret_cast<uint4 *>(dst)[4 * c + y] = make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+            for (int y = 0; y < 4; y += 2) {
+              const uint4 u = make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+              const uint4 v = make_uint4(w[4 * y + 4], w[4 * y + 5], w[4 * y + 6], w[4 * y + 7]);
+              if (a.out_sector) {
+                st_sector(dst + 64 * c + 16 * y, u, v);
+              } else {
+                reinterpret_cast<uint4 *>(dst)[4 * c + y] = u;
+                reinterpret_cast<uint4 *>(dst)[4 * c + y + 1] = v;
+              }
+            }
           }
         }
         if (je > js) {
@@ -893,6 +895,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   TcArgs t;
   t.a = a;
   t.P = kTcT / a.G;
+  t.a.out_sector = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   const int N = a.pv.n_tokens;
   e = rows_map(&t.mq, BF16, a.q.p, D, a.Hq, a.q.hs, N, a.q.ts, a.G, t.P);
   if (PAGED) {

@@ -72,6 +72,7 @@ struct AttnArgs {
   PagedView pv;
   Rows q, k, v;
   void *out;              // [n_tokens, Hq, D]
+  int out_sector;         // on 32 bytes
   int Hq, G, window, max_new;
   int hc, rows, whole;    // few-token form: KV heads of a unit, its rows at most, units never cut
   int part_shift, pt_shift;  // positions of one copy, of a tile (log2)
