@@ -526,11 +526,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       umma_commit_if(leader, &free_[s]);
       if (nt == 1) umma_commit_if(leader, qfree);
       if (++s == NS) s = 0, ph ^= 1;
+      // tiles [steady, steady_end): seen in full by every row, as a tile of both
+      // query tiles that is neither one's first, the next one theirs too and not
+      // the job's last: nothing to ask between the products
+      const int steady = max(max(js0, js1) + 1, (low - lo + kTcT - 1) / kTcT);
+      const int steady_end = min(min(min(je0, je1), nt - 1) - 1, first - lo >= kTcT - 1 ? (first - lo + 1) / kTcT : 0);
       for (int jt = 0; jt < nt; ++jt) {
         // V of this tile at s, K of the next at sk
         int sk = s + 1;
         uint32_t phk = ph;
         if (sk == NS) sk = 0, phk ^= 1;
+        if (jt >= steady && jt < steady_end) {
+          if (!(ok = wait(&full[s], ph))) break;
+          if (!(ok = values(i0, s, true))) break;
+          if (!(ok = wait(&full[sk], phk))) break;
+          tc_fence_after();
+          scores(i0, sk);
+          if (!(ok = values(i1, s, true))) break;
+          umma_commit_if(leader, &free_[s]);
+          s = sk + 1, ph = phk;
+          if (s == NS) s = 0, ph ^= 1;
+          scores(i1, sk);
+          umma_commit_if(leader, &free_[sk]);
+          continue;
+        }
         const bool more = jt + 1 < nt;
         const int t0 = lo + jt * kTcT;
         if (!(ok = wait(&full[s], ph))) break;
