@@ -721,7 +721,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           }
           const float ref = (m == -INFINITY ? 0.f : m) - kShift;
           const uint64_t sg2 = pair_f32(sg, sg), ref2 = pair_f32(-ref, -ref);
-          uint64_t sum[2] = {0, 0};
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
             uint32_t w[8];
@@ -729,9 +728,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             for (int y = 0; y < 8; ++y) {
               float u, v;
               unpair_f32(fma_f32x2(pair_f32(x[16 * c + 2 * y], x[16 * c + 2 * y + 1]), sg2, ref2), u, v);
-              u = fast_exp2(u);
-              v = fast_exp2(v);
-              sum[y & 1] = add_f32x2(sum[y & 1], pair_f32(u, v));
+              u = x[16 * c + 2 * y] = fast_exp2(u);
+              v = x[16 * c + 2 * y + 1] = fast_exp2(v);
               w[y] = pack2<BF16>(u, v);
             }
             tmem_st8_nw(ts + 8 * c, w);
@@ -740,6 +738,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
               tc_fence_before();
               arrive(&pfull[2 * i + (c >> 2)]);
             }
+          }
+          // the row's sum, of the weights before their rounding: behind the hand-over,
+          // which the products wait for
+          uint64_t sum[2] = {0, 0};
+#pragma unroll
+          for (int c = 0; c < 128; c += 4) {
+            sum[0] = add_f32x2(sum[0], pair_f32(x[c], x[c + 1]));
+            sum[1] = add_f32x2(sum[1], pair_f32(x[c + 2], x[c + 3]));
           }
           float u, v;
           unpair_f32(add_f32x2(sum[0], sum[1]), u, v);
