@@ -24,6 +24,8 @@ cache      whole-plan reference: builds every anchor's stored state from a
            per-layer plan (GQA anchors, and MLA anchors whose kept latent
            and positional key are stored as quantised vectors) and computes
            every layer's decode output.
+serving    rotary positions with several axes, page tables, causal attention
+           with a window, and the error bounds of the serving tests.
 
 Parity status: every function here is pinned by a ``-m "not gpu"`` test
 (``tests/test_oracle_*.py``) against closed forms, the paper's printed

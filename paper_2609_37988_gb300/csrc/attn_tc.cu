@@ -21,14 +21,15 @@
 // NaN, so those enter as zeros, and a row that sees one gets NaN in that
 // channel when it is written.
 //
-// Jobs in order of their distance from their sequence's end, all sequences
-// side by side: the longest first where lengths are equal, the short ones last
-// in any case; dealt to the CTAs back and forth.  (More than 128 sequences go one
-// behind another: there are jobs enough to even out.)  Chunks over pages that make
+// Jobs in order of the positions that they see, the most first (with the order
+// of their distance from their own sequence's end, prompts of 560 to 9000 tokens
+// took 528 us), dealt to the CTAs back and forth.  (More than 128 sequences go
+// one behind another: there are jobs enough to even out.)  Chunks over pages that make
 // few jobs go in equal runs of tiles instead, one per CTA: jobs that a run cuts
 // leave their pieces (result, reference and sum of each row) in the workspace,
 // and a second kernel joins them.
 #include <cuda.h>
+#include <limits.h>
 #include <math.h>
 #include <string.h>
 
@@ -387,21 +388,31 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         }
       }
     } else if (pv.B <= kTcOrdered) {
-      // blocks of the batch's sequences, four a lane
-      int nb[4], total = 0, most = 0;
+      // The batch's sequences, four a lane: a sequence's blocks are [from, to), in
+      // blocks from its position 0 on, so that a block's number says how many
+      // positions its rows see.
+      int from[4], to[4], total = 0, top = 0, low = INT_MAX;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        nb[i] = read_blocks(lane + 32 * i);
-        total += nb[i];
-        most = max(most, nb[i]);
+        const int b = lane + 32 * i, n = read_blocks(b);
+        from[i] = 0;
+        if (PAGED && n > 0) {
+          int q0;
+          const int held = (int)min((int64_t)max(pv.lens[b], 0), (int64_t)pv.max_pages << pv.page_shift);
+          from[i] = max(held - seq_tokens(pv, b, q0), 0) / (2 * P);
+        }
+        to[i] = from[i] + n;
+        total += n;
+        if (n > 0) top = max(top, to[i]), low = min(low, from[i]);
       }
       total = (int)__reduce_add_sync(kAll, (unsigned)total);
-      most = (int)__reduce_max_sync(kAll, (unsigned)most);
-      // jobs at most `d` blocks from their sequence's end
+      top = (int)__reduce_max_sync(kAll, (unsigned)top);
+      low = (int)__reduce_min_sync(kAll, (unsigned)low);
+      // jobs with one of the `d` largest numbers
       auto upto = [&](int d) {
         unsigned sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sum += min(nb[i], d);
+        for (int i = 0; i < 4; ++i) sum += min(max(to[i] - (top - d), 0), to[i] - from[i]);
         return (int)__reduce_add_sync(kAll, sum);
       };
       const int n_jobs = total * pv.Hkv, step = gridDim.x;
@@ -409,25 +420,30 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         const int idx = i * step + (i & 1 ? step - 1 - (int)blockIdx.x : (int)blockIdx.x);
         if (idx >= n_jobs) break;
         const int r = idx / pv.Hkv;
-        int d0 = 0, d1 = most, f0 = 0;  // upto(d0) <= r < upto(d1)
+        int d0 = 0, d1 = top - low, f0 = 0;  // upto(d0) <= r < upto(d1)
         while (d1 - d0 > 1) {
-          const int mid = (d0 + d1) / 2, f = upto(mid);
+          const int mid = d0 + (d1 - d0) / 2, f = upto(mid);
           if (f <= r)
             d0 = mid, f0 = f;
           else
             d1 = mid;
         }
-        int rem = r - f0, b = 0;
+        const int number = top - 1 - d0;
+        int rem = r - f0, b = 0, blk = 0;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          const uint32_t in = __ballot_sync(kAll, nb[c] > d0);
-          const int n = __popc(in);
-          if (rem >= 0 && rem < n) b = 32 * c + (int)__fns(in, 0, rem + 1);
-          rem -= n;
+          const uint32_t in = __ballot_sync(kAll, from[c] <= number && number < to[c]);
+          const int m = __popc(in);
+          if (rem >= 0 && rem < m) {
+            const int f = (int)__fns(in, 0, rem + 1);
+            b = 32 * c + f;
+            blk = number - __shfl_sync(kAll, from[c], f);
+          }
+          rem -= m;
         }
         int q0;
         const int n = seq_tokens(pv, b, q0);
-        ok = emit(describe(b, idx - r * pv.Hkv, (n + 2 * P - 1) / (2 * P) - 1 - d0, q0, n));
+        ok = emit(describe(b, idx - r * pv.Hkv, blk, q0, n));
       }
     } else {
       // sequence by sequence, the search going on from where the last job was
