@@ -3,10 +3,10 @@
 //
 // Query j of sequence b sits at position p = len_b - n_b + j and sees
 // positions max(0, p - window + 1) .. p; head h reads KV head h / G.  Rows
-// r = j G + (head in its group) of a (sequence, KV head) go in units of 8 or 16,
-// so that a key or value byte is read once for all of them; with small pages a
-// unit takes HC = 2 or 4 KV heads side by side, whose parts of a page adjoin,
-// so that a copy is 16 KB either way.  A unit's positions go in tiles of
+// r = j G + (head in its group), at most 8 or 16 of a (sequence, KV head), make a
+// unit, so that a key or value byte is read once for all of them; with small
+// pages a unit takes HC = 2 or 4 KV heads side by side, whose parts of a page
+// adjoin, so that a copy is 16 KB either way.  A unit's positions go in tiles of
 // 64 / HC; the tiles of all units, one behind another, are cut into equal runs,
 // one per CTA (two CTAs per SM are resident), whatever the sequences' lengths
 // are.  A unit that a run covers whole is written at once; the pieces of the
@@ -86,32 +86,12 @@ __device__ __forceinline__ Seq load_seq(const PagedView &v, int b, int max_new) 
   }
   return s;
 }
-// Positions from lo (a multiple of the tile) in nt tiles that the rows of unit
-// block rb (RU rows) see; at least one tile, so that rows that see nothing get
-// their zeros.
-template <int RU>
-__device__ __forceinline__ void block_range(const Seq &s, const AttnArgs &a, int rb, int &lo, int &nt) {
-  int first = s.len - s.n, last = s.len - 1;
-  if (s.n * a.G > RU) {
-    last = first + min(s.n * a.G - 1, rb * RU + RU - 1) / a.G;
-    first += rb * RU / a.G;
-  }
+// Positions from lo (a multiple of the tile) in nt tiles that the new tokens see;
+// at least one tile, so that rows that see nothing get their zeros.
+__device__ __forceinline__ void seq_range(const Seq &s, const AttnArgs &a, int &lo, int &nt) {
   const int sh = a.pt_shift;
-  lo = max(0, first - a.window + 1) >> sh << sh;
-  nt = max(1, (last + (1 << sh) - lo) >> sh);
-}
-template <int RU>
-__device__ __forceinline__ int row_blocks(const Seq &s, int G) { return (s.n * G + RU - 1) / RU; }
-// Tiles of a sequence, per unit of heads.
-template <int RU>
-__device__ __forceinline__ int seq_tiles(const Seq &s, const AttnArgs &a) {
-  int sum = 0;
-  for (int rb = 0; rb < row_blocks<RU>(s, a.G); ++rb) {
-    int lo, nt;
-    block_range<RU>(s, a, rb, lo, nt);
-    sum += nt;
-  }
-  return sum;
+  lo = max(0, s.len - s.n - a.window + 1) >> sh << sh;
+  nt = max(1, (s.len - 1 + (1 << sh) - lo) >> sh);
 }
 // x / y, in 32 bits where they do (a 64-bit division takes 500 cycles)
 __device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
@@ -121,7 +101,7 @@ __device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
 
 // A place in the list of tiles.
 struct At {
-  int b, h, rb, t;   // sequence, unit of KV heads, row block, tile of the unit
+  int b, h, t;       // sequence, unit of KV heads, tile of the unit
   int lo, nt;        // the unit's first position and tiles
   Seq s;
 };
@@ -188,7 +168,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(const AttnArgs a) {
 #pragma unroll
       for (int i = 1; i < groups; ++i) join(M, L, x, sl[tid + i * V].x, sl[tid + i * V].y, sx[tid + i * V]);
     }
-    store_row<D, BF16>(a, u.q0, u.p_base, u.head + hd, u.row0 + r, v, x, L);
+    store_row<D, BF16>(a, u.q0, u.p_base, u.head + hd, r, v, x, L);
   }
   pdl_trigger();
   // every CTA has read n before it counts itself
@@ -234,20 +214,15 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
   }
   pdl_wait();
 
-  auto settle = [&](At &x) { block_range<RU>(x.s, a, x.rb, x.lo, x.nt); };
   auto next_unit = [&](At &x) {
     x.t = 0;
-    if (++x.rb >= row_blocks<RU>(x.s, a.G)) {
-      x.rb = 0;
-      if (++x.h >= units) {
-        x.h = 0;
-        do {
-          if (++x.b >= pv.B) return;  // behind the last unit: not used again
-          x.s = load_seq(pv, x.b, a.max_new);
-        } while (x.s.n == 0);
-      }
-    }
-    settle(x);
+    if (++x.h < units) return;
+    x.h = 0;
+    do {
+      if (++x.b >= pv.B) return;  // behind the last unit: not used again
+      x.s = load_seq(pv, x.b, a.max_new);
+    } while (x.s.n == 0);
+    seq_range(x.s, a, x.lo, x.nt);
   };
 
   // the run of this CTA: `mine` tiles from s_at on
@@ -258,8 +233,10 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     auto chunk = [&](int b0) {
       const bool in = b0 + lane < pv.B;
       if (in) sq = load_seq(pv, b0 + lane, a.max_new);
-      per = !in ? 0 : a.whole ? row_blocks<RU>(sq, a.G) : seq_tiles<RU>(sq, a);
-      uint32_t x = per;  // 32 sequences of at most 2^22 tiles and 8 row blocks each
+      int lo = 0, nt = 0;
+      if (in && sq.n > 0) seq_range(sq, a, lo, nt);
+      per = a.whole && nt > 0 ? 1 : nt;
+      uint32_t x = per;  // 32 sequences of at most 2^22 tiles
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t y = __shfl_up_sync(kAll, x, o);
@@ -274,8 +251,10 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     }
     const int64_t share = max(div_pos(total + gridDim.x - 1, gridDim.x), (int64_t)(a.whole ? 1 : kMinShare));
     const int64_t w0 = share * blockIdx.x;
+    if (lane == 0) s_mine = 0;
+    __syncwarp();
     if (w0 < total) {
-      for (int b0 = 0;; b0 += 32) {
+      for (int b0 = 0; b0 < pv.B; b0 += 32) {
         if (pv.B > 32) upto = chunk(b0);
         const uint32_t past = __ballot_sync(kAll, before + upto > w0);
         if (past) {
@@ -285,15 +264,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
             x.s = sq;
             const int64_t off = w0 - (before + upto - (int64_t)units * per);
             x.h = (int)div_pos(off, per);
-            int r = (int)(off - (int64_t)x.h * per);
-            x.rb = a.whole ? r : 0;
-            settle(x);
-            while (!a.whole && r >= x.nt) {
-              r -= x.nt;
-              ++x.rb;
-              settle(x);
-            }
-            x.t = a.whole ? 0 : r;
+            x.t = (int)(off - (int64_t)x.h * per);
+            seq_range(x.s, a, x.lo, x.nt);
             s_at = x;
             s_mine = (int)min(share, total - w0);
             if (a.whole) {  // units to tiles
@@ -310,10 +282,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
         before += __shfl_sync(kAll, upto, 31);
       }
     }
-    if (lane == 0) {
-      if (w0 >= total) s_mine = 0;
-      s_share = (int)min(share, (int64_t)1 << 30);
-    }
+    if (lane == 0) s_share = (int)min(share, (int64_t)1 << 30);
   }
   __syncthreads();
   const int mine = s_mine;
@@ -406,7 +375,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
   for (int w = 0; w < mine;) {
     // a piece: tiles [t_begin, t_end) of one unit
     const int t_begin = at.t, t_end = min(at.nt, at.t + (mine - w)), w_begin = w;
-    const int row0 = at.rb * RU, R = min(RU, at.s.n * a.G - row0);
+    const int R = at.s.n * a.G;
     const int p_base = at.s.len - at.s.n;
     // Q^T as the B operand (row 8 nb + g), and the positions that rows
     // 8 nb + 2 c + e see
@@ -414,8 +383,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     int lim[2 * NB], low[2 * NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
-      const int r = row0 + 8 * nb + g, j = r / a.G;
-      const bool real = 8 * nb + g < R;
+      const int r = 8 * nb + g, j = r / a.G;
+      const bool real = r < R;
       const uint8_t *src = a.q.p + 2 * ((int64_t)(at.s.q0 + (real ? j : 0)) * a.q.ts +
                                         (int64_t)((at.h * HC + hh) * a.G + (real ? r - j * a.G : 0)) * a.q.hs);
 #pragma unroll
@@ -426,12 +395,11 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int rr = 8 * nb + 2 * c + e;
-        lim[2 * nb + e] = rr < R ? p_base + (row0 + rr) / a.G : -1;
+        lim[2 * nb + e] = rr < R ? p_base + rr / a.G : -1;
         low[2 * nb + e] = lim[2 * nb + e] - a.window + 1;
       }
     }
-    const int lim_min = p_base + row0 / a.G;                          // of the first row
-    const int low_max = p_base + (row0 + R - 1) / a.G - a.window + 1;  // of the last
+    const int lim_min = p_base, low_max = at.s.len - a.window;  // of the first and the last token
     float o[NB][KS][4];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb)
@@ -599,8 +567,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
         const float2 ml = s_ml[hh * per_head + i][lane];
         L += ml.y * (ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - M));
       }
-      const int rr = row0 + lane, j = rr / a.G;
-      row_off = (uint32_t)((at.s.q0 + j) * a.Hq + (at.h * HC + hh) * a.G + (rr - j * a.G));
+      const int j = lane / a.G;
+      row_off = (uint32_t)((at.s.q0 + j) * a.Hq + (at.h * HC + hh) * a.G + (lane - j * a.G));
       // a row before position 0 sees nothing and gives zeros
       inv = p_base + j >= 0 ? 1.f / L : -1.f;
       if (!whole && sub == 0) {
@@ -636,7 +604,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     if (!whole && t_begin == 0 && tid == 0) {
       const int at_list = atomicAdd(&a.list->n, 1);  // a CTA adds one at most
       const int last = (int)blockIdx.x + (w_begin + at.nt - 1) / s_share;
-      if ((unsigned)at_list < (unsigned)kRowsMaxCtas) a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, row0, R};
+      if ((unsigned)at_list < (unsigned)kRowsMaxCtas) a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, R};
     }
     if (w < mine) {
       fence_proxy_async();
@@ -662,7 +630,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   // two CTAs per SM, no more of them than runs that there can be
   const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / (kT / a.hc) + 2;
-  const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * ((a.max_new * a.G + 8 * NB - 1) / (8 * NB)) * cap;
+  const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * cap;
   const int64_t runs = a.whole ? tiles / cap : (tiles + kMinShare - 1) / kMinShare;
   const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), runs);
   e = launch_pdl(attn_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);

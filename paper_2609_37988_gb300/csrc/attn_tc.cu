@@ -326,7 +326,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         int b = 0, h = 0, blk = 0, t = 0;
         int64_t off = 0;
         int per = 0;  // of the sequence found
-        for (int b0 = 0;; b0 += 32) {
+        for (int b0 = 0; b0 < pv.B; b0 += 32) {
           const int tl = b0 == 0 ? tiles0 : b0 + lane < pv.B ? head_tiles(b0 + lane) : 0;
           const int64_t x = (int64_t)pv.Hkv * tl;
           int64_t sum = x;
@@ -344,11 +344,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           }
           off += __shfl_sync(kAll, sum, 31);
         }
+        ok = per > 0;  // a sequence was found: the lengths are as they were
         int q0, n = seq_tokens(pv, b, q0);
-        h = (int)div_pos(off, per);
+        h = ok ? (int)div_pos(off, per) : 0;
         t = (int)(off - (int64_t)h * per);
         Job j = describe(b, h, 0, q0, n);
-        while (t >= max(1, j.nt)) {
+        while (ok && t >= max(1, j.nt) && (blk + 1) * 2 * P < n) {
           t -= max(1, j.nt);
           j = describe(b, h, ++blk, q0, n);
         }
@@ -380,8 +381,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             if (++h >= pv.Hkv) {
               h = 0;
               do {
-                n = seq_tokens(pv, ++b, q0);
+                n = ++b < pv.B ? seq_tokens(pv, b, q0) : -1;
               } while (n == 0);
+              if (n < 0) break;
             }
           }
           j = describe(b, h, blk, q0, n);
@@ -472,7 +474,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         ok = emit(describe(b0 + f, (int)(idx - (int64_t)r * pv.Hkv), (n + 2 * P - 1) / (2 * P) - 1 - from_end, q0, n));
       }
     }
-    if (ok) emit(end);
+    if (!__any_sync(kAll, *abort_flag)) emit(end);
     // after a wait that gave up: the copies in flight land before the CTA ends
     if (*abort_flag && lane == 0) {
       if (loads > 0) mbar_wait(qfull, (loads - 1) & 1, kWaits);

@@ -47,7 +47,7 @@ cudaError_t launch_rotary(const RotArgs &a, int dtype, cudaStream_t st);
 constexpr int kRowsMaxCtas = 320;
 struct RowsSplit {
   int32_t first, last;    // the CTAs where it starts and ends
-  int32_t q0, p_base, head, row0, rows;
+  int32_t q0, p_base, head, rows;
 };
 struct RowsList {         // n and done are zero between calls
   int32_t n;
