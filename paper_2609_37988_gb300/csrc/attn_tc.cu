@@ -869,49 +869,82 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   pdl_trigger();
 }
 
-// Joins the pieces of the jobs that runs cut: a CTA takes 16 channels of a
-// query tile, a thread a row.
-template <int D, bool BF16>
-__global__ void __launch_bounds__(kTcT) attn_tc_join_kernel(const AttnArgs a, int P) {
-  const int row = threadIdx.x, tok_row = row / a.G;
-  constexpr int C = D / 16;
+// Joins the pieces of the jobs that runs cut: a CTA takes CH channels of a query
+// tile, a thread a row and every HALVES-th piece, U pieces' loads in flight; the
+// halves meet in shared memory.  The last CTA clears the list for the next call.
+// Two forms: 16 channels and 2 pieces at a time where many jobs were cut into a few
+// pieces each; 8 channels, two halves and 8 at a time where a few were cut into
+// dozens (one sequence of 65000 positions, 37 pieces a job: 55 -> 39 us; 512 new
+// tokens of one over 8192, 88 jobs: 68 us, with the other form 80).
+template <int D, bool BF16, int CH, int HALVES, int U>
+__global__ void __launch_bounds__(HALVES *kTcT) attn_tc_join_kernel(const AttnArgs a, int P) {
+  constexpr int C = D / CH;
+  __shared__ float s_x[CH + 2][kTcT];
+  const int row = threadIdx.x % kTcT, hf = threadIdx.x / kTcT, tok_row = row / a.G;
   pdl_wait();
   const int n = min(*reinterpret_cast<volatile int *>(&a.tc_list->n), kTcMaxCtas) * 2 * C;
   for (int item = blockIdx.x; item < n; item += gridDim.x) {
     const TcSplit u = a.tc_list->unit[item / (2 * C)];
     const int i = item / C & 1, c = item % C;
     const int tok = u.tok0 + i * P + tok_row;
-    if (tok_row >= P || tok >= u.n) continue;
-    float M = -INFINITY, L = 0.f, x[16];
+    const bool real = tok_row < P && tok < u.n;
+    float M = -INFINITY, L = 0.f, x[CH];
 #pragma unroll
-    for (int y = 0; y < 16; ++y) x[y] = 0.f;
-    for (int p = u.first; p <= u.last; ++p) {
-      const float *part = a.part + (int64_t)(2 * (2 * p + (p == u.first)) + i) * tc_part(D);
-      const float pm = __ldcg(part + kTcT * D + row), pl = __ldcg(part + kTcT * (D + 1) + row);
-      float4 z[4];
+    for (int y = 0; y < CH; ++y) x[y] = 0.f;
+    auto join = [&](float m, float l, const float *z) {
+      if (m == -INFINITY && l == 0.f) return;  // saw nothing
+      const float t = fmaxf(M, m), f = M == -INFINITY ? 0.f : fast_exp2(M - t), h = m == -INFINITY ? 0.f : fast_exp2(m - t);
+      M = t;
+      L = L * f + l * h;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) z[y] = __ldcg(reinterpret_cast<const float4 *>(part + (4 * c + y) * (4 * kTcT) + 4 * row));
-      if (pm == -INFINITY && pl == 0.f) continue;  // saw nothing
-      const float m = fmaxf(M, pm), f = M == -INFINITY ? 0.f : fast_exp2(M - m), h = pm == -INFINITY ? 0.f : fast_exp2(pm - m);
-      M = m;
-      L = L * f + pl * h;
+      for (int y = 0; y < CH; ++y) x[y] = x[y] * f + z[y] * h;
+    };
+    for (int p0 = u.first + hf; real && p0 <= u.last; p0 += U * HALVES) {
+      float pm[U], pl[U], z[U][CH];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        x[4 * y] = x[4 * y] * f + z[y].x * h;
-        x[4 * y + 1] = x[4 * y + 1] * f + z[y].y * h;
-        x[4 * y + 2] = x[4 * y + 2] * f + z[y].z * h;
-        x[4 * y + 3] = x[4 * y + 3] * f + z[y].w * h;
+      for (int k = 0; k < U; ++k) {
+        const int p = p0 + k * HALVES;
+        const bool in = p <= u.last;
+        const float *part = a.part + (int64_t)(2 * (2 * p + (p == u.first)) + i) * tc_part(D);
+        pm[k] = in ? __ldcg(part + kTcT * D + row) : -INFINITY;
+        pl[k] = in ? __ldcg(part + kTcT * (D + 1) + row) : 0.f;
+#pragma unroll
+        for (int y = 0; y < CH / 4; ++y)
+          *reinterpret_cast<float4 *>(&z[k][4 * y]) =
+              in ? __ldcg(reinterpret_cast<const float4 *>(part + (CH / 4 * c + y) * (4 * kTcT) + 4 * row))
+                 : make_float4(0.f, 0.f, 0.f, 0.f);
       }
-    }
-    const bool sees = u.p0 + tok >= 0;
-    const float inv = sees ? 1.f / L : 0.f;
-    uint32_t w[8];
 #pragma unroll
-    for (int y = 0; y < 8; ++y) w[y] = sees ? pack2<BF16>(x[2 * y] * inv, x[2 * y + 1] * inv) : 0u;
-    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) +
-                                           2 * (((int64_t)(u.q0 + tok) * a.Hq + u.h * a.G + (row - tok_row * a.G)) * D + 16 * c));
-    dst[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    dst[1] = make_uint4(w[4], w[5], w[6], w[7]);
+      for (int k = 0; k < U; ++k) join(pm[k], pl[k], z[k]);
+    }
+    if constexpr (HALVES == 2) {
+      if (hf == 1) {
+#pragma unroll
+        for (int y = 0; y < CH; ++y) s_x[y][row] = x[y];
+        s_x[CH][row] = M;
+        s_x[CH + 1][row] = L;
+      }
+      __syncthreads();
+      if (hf == 0) {
+        float z[CH];
+#pragma unroll
+        for (int y = 0; y < CH; ++y) z[y] = s_x[y][row];
+        join(s_x[CH][row], s_x[CH + 1][row], z);
+      }
+      __syncthreads();
+    }
+    if (hf == 0 && real) {
+      // a row before position 0 sees nothing and gives zeros
+      const bool sees = u.p0 + tok >= 0;
+      const float inv = sees ? 1.f / L : 0.f;
+      uint32_t w[CH / 2];
+#pragma unroll
+      for (int y = 0; y < CH / 2; ++y) w[y] = sees ? pack2<BF16>(x[2 * y] * inv, x[2 * y + 1] * inv) : 0u;
+      uint4 *dst = reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) +
+                                             2 * (((int64_t)(u.q0 + tok) * a.Hq + u.h * a.G + (row - tok_row * a.G)) * D + CH * c));
+#pragma unroll
+      for (int y = 0; y < CH / 8; ++y) dst[y] = make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+    }
   }
   pdl_trigger();
   __syncthreads();
@@ -960,7 +993,12 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   const int grid = std::min(a.sms, kTcMaxCtas);
   e = launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3(grid), dim3(kTcThreads), Smem<D>::kBytes, st, t);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attn_tc_join_kernel<D, BF16>, dim3(std::min(grid * 2 * D / 16, 8 * a.sms)), dim3(kTcT), 0, st, t.a, t.P);
+  // a CTA's run cuts off the start of one job at most
+  const int64_t cut = std::min<int64_t>(jobs, grid);
+  if (cut * 2 * (D / 8) <= 4 * a.sms)
+    return launch_pdl(attn_tc_join_kernel<D, BF16, 8, 2, 8>, dim3((int)cut * 2 * (D / 8)), dim3(2 * kTcT), 0, st, t.a, t.P);
+  return launch_pdl(attn_tc_join_kernel<D, BF16, 16, 1, 2>, dim3((int)std::min<int64_t>(cut * 2 * (D / 16), 8 * a.sms)), dim3(kTcT),
+                    0, st, t.a, t.P);
 }
 
 template <int D, bool BF16>
