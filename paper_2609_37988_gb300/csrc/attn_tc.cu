@@ -278,14 +278,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           if (!wait0(&free_[s], ph ^ 1)) return false;
           if (lane == 0) mbar_expect_tx(&full[s], SM::kTile);
           __syncwarp();
-          uint8_t *dst = sm + SM::kRing + s * SM::kTile + half * kBox;
+          uint8_t *dst = sm + SM::kRing + s * SM::kTile;
           const CUtensorMap *m = kv ? &t.mv : &t.mk;
-          if (lane < parts * NB) {
+          if (PAGED && kv) {
+            // values of a page in one copy, its halves one behind the other
+            const int pg = __shfl_sync(kAll, page, lane < parts ? lane * NB : 0);
+            if (lane < parts)
+              tma_load_5d(dst + (lane << shift) * (2 * D), m, 0, (lane << shift) & ((1 << pv.page_shift) - 1), 0, j.h, pg, &full[s]);
+          } else if (lane < parts * NB) {
+            // keys: their halves apart, 128 rows each, as the products' rows have to be
             if (PAGED)
-              tma_load_4d(dst + (part << shift) * 128, m, 64 * half, (part << shift) & ((1 << pv.page_shift) - 1), j.h, page,
-                          &full[s]);
+              tma_load_4d(dst + half * kBox + (part << shift) * 128, m, 64 * half, (part << shift) & ((1 << pv.page_shift) - 1),
+                          j.h, page, &full[s]);
             else
-              tma_load_3d(dst, m, 64 * half, j.q0 + j.lo + jt * kTcT, j.h, &full[s]);
+              tma_load_3d(dst + half * kBox, m, 64 * half, j.q0 + j.lo + jt * kTcT, j.h, &full[s]);
           }
           if (++s == NS) s = 0, ph ^= 1;
         }
@@ -493,6 +499,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     constexpr uint32_t hi = umma_desc_hi_sw128(1024);
     const uint32_t ring = smem_u32(sm + SM::kRing), q_at = umma_desc_lo(smem_u32(sm + SM::kQ), 16);
     const bool leader = elect_one();
+    // values: rows of a copy (log2), and where 16 of them start (in 16 bytes)
+    const int v_shift = PAGED ? min(pv.page_shift, 6) : 7;
+    auto v_step = [&](int x) {
+      if (!PAGED) return 128 * x;
+      return ((x >> (v_shift - 4)) << v_shift) * (2 * D / 16) + (x & ((1 << (v_shift - 4)) - 1)) * 128;
+    };
     int s = 0;
     uint32_t ph = 0, loads = 0, cleans = 0;   // cleans: parity of either stage's vclean
     uint32_t tiles[2] = {0, 0}, done[2] = {0, 0};  // of either query tile: parity of its tiles, jobs with any
@@ -508,14 +520,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     };
     auto values = [&](auto I, int at, bool acc) {
       constexpr int i = decltype(I)::value;
-      const uint32_t vv = umma_desc_lo(ring + at * SM::kTile, kBox);
+      const uint32_t vv = umma_desc_lo(ring + at * SM::kTile, 128 << v_shift);
 #pragma unroll
       for (int hf = 0; hf < 2; ++hf) {
         if (!wait(&pfull[2 * i + hf], tiles[i])) return false;
         tc_fence_after();
 #pragma unroll
         for (int x = 4 * hf; x < 4 * hf + 4; ++x)
-          umma_f16_ts_if(leader, tO + D * i, tS + 128 * i + 8 * x, vv + 128 * x, hi, id_v, acc || x > 0);
+          umma_f16_ts_if(leader, tO + D * i, tS + 128 * i + 8 * x, vv + v_step(x), hi, id_v, acc || x > 0);
       }
       umma_commit_if(leader, &odone[i]);
       tiles[i] ^= 1;
@@ -976,7 +988,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   e = rows_map(&t.mq, BF16, a.q.p, D, a.Hq, a.q.hs, N, a.q.ts, a.G, t.P);
   if (PAGED) {
     memcpy(&t.mk, a.mk, sizeof t.mk);
-    memcpy(&t.mv, a.mv, sizeof t.mv);
+    memcpy(&t.mv, a.ov, sizeof t.mv);
   } else {
     if (e == cudaSuccess) e = rows_map(&t.mk, BF16, a.k.p, D, N, a.k.ts, a.pv.Hkv, a.k.hs, kTcT, 1);
     if (e == cudaSuccess) e = rows_map(&t.mv, BF16, a.v.p, D, N, a.v.ts, a.pv.Hkv, a.v.hs, kTcT, 1);

@@ -77,9 +77,9 @@ struct AttnArgs {
   int hc, rows, whole;    // few-token form: KV heads of a unit, its rows at most, units never cut
   int part_shift, pt_shift;  // positions of one copy, of a tile (log2)
   float sig_log2;
-  // the pages' tensor maps (host memory, 128 bytes each): boxes of 64 channels,
-  // of whole rows of rows_heads() KV heads, of whole rows of one
-  const void *mk, *mv, *wk, *wv, *ok, *ov;
+  // the pages' tensor maps (host memory, 128 bytes each): keys in boxes of 64
+  // channels; keys and values in whole rows of rows_heads() KV heads, and of one
+  const void *mk, *wk, *wv, *ok, *ov;
   float *part;            // partial results
   RowsList *list;
   TcList *tc_list;

@@ -25,6 +25,7 @@ struct kvk_rotary {
   int head_dim;
 };
 
+constexpr int kMaps = 5;
 struct PageMap {
   alignas(64) uint8_t bytes[128];
 };
@@ -32,7 +33,7 @@ struct PageMap {
 struct kvk_paged {
   kvk_paged_desc d;
   std::vector<uint8_t *> k, v;
-  std::vector<PageMap> maps;  // tensor maps of a layer's pools: keys and values, three times
+  std::vector<PageMap> maps;  // kMaps tensor maps of a layer's pools, as AttnArgs has them
   uint8_t *ws;
   int device, sms, page_shift;
 };
@@ -273,7 +274,7 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
       p->k.push_back(static_cast<uint8_t *>(k_pages[l]));
       p->v.push_back(static_cast<uint8_t *>(v_pages[l]));
     }
-    p->maps.resize((size_t)desc->n_layers * 6);
+    p->maps.resize((size_t)desc->n_layers * kMaps);
   } catch (const std::bad_alloc &) {
     delete p;
     return fail(KVK_ERR_INVALID_ARG, "out of host memory");
@@ -287,10 +288,13 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
     return kvk_internal_cuda_error(e, "querying the device");
   }
   const bool bf = desc->dtype == KVK_DTYPE_BF16;
-  const int heads[3] = {0, rows_heads(desc->page_size, desc->n_kv_heads), 1};
-  for (int i = 0; i < desc->n_layers * 6 && e == cudaSuccess; ++i)
-    e = make_pages_map(p->maps[i].bytes, bf, i & 1 ? p->v[i / 6] : p->k[i / 6], desc->head_dim, desc->page_size, desc->n_kv_heads,
-                       desc->n_pages, heads[i % 6 / 2]);
+  const int hc = rows_heads(desc->page_size, desc->n_kv_heads), heads[kMaps] = {0, hc, hc, 1, 1};
+  for (int i = 0; i < desc->n_layers * kMaps && e == cudaSuccess; ++i) {
+    const int l = i / kMaps, m = i % kMaps;
+    const bool values = m == 2 || m == 4;
+    e = make_pages_map(p->maps[i].bytes, bf, values ? p->v[l] : p->k[l], desc->head_dim, desc->page_size, desc->n_kv_heads,
+                       desc->n_pages, heads[m]);
+  }
   if (e != cudaSuccess) {
     delete p;
     return kvk_internal_cuda_error(e, "encoding the pages' tensor maps");
@@ -372,13 +376,12 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
   a.device = p->device;
-  const PageMap *maps = &p->maps[(size_t)layer * 6];
+  const PageMap *maps = &p->maps[(size_t)layer * kMaps];
   a.mk = maps[0].bytes;
-  a.mv = maps[1].bytes;
-  a.wk = maps[2].bytes;
-  a.wv = maps[3].bytes;
-  a.ok = maps[4].bytes;
-  a.ov = maps[5].bytes;
+  a.wk = maps[1].bytes;
+  a.wv = maps[2].bytes;
+  a.ok = maps[3].bytes;
+  a.ov = maps[4].bytes;
   const cudaError_t e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;
