@@ -552,7 +552,8 @@ typedef struct kvk_paged kvk_paged;
  * the new tokens: token j of sequence b's n_b new ones sits at position
  * lengths[b] - n_b + j.  table [batch, max_pages]: sequence b's position t is
  * slot t % page_size of page table[b][t / page_size]; entries behind its last
- * page are not read.  max_pages * page_size: at most 2^26. */
+ * page, and for an attention with a window those wholly before the first new
+ * token's window, may hold anything.  max_pages * page_size: at most 2^26. */
 typedef struct {
   const int32_t *cu_new;   /* [batch + 1], not decreasing, within [0, n_tokens] */
   const int32_t *lengths;  /* [batch] */
@@ -595,7 +596,8 @@ kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_bat
  * a page outside the pool sets KVK_DEVERR_PAGE and reads as zeros.
  * What the slots behind a sequence's last position hold does not matter, and a
  * key or value that a query does not see does not change its result, not even
- * one that is not finite.
+ * one that is not finite.  An infinite value that it does see makes its channel
+ * infinite or NaN.  softmax_scale: a positive, finite, normal number.
  * Calls that use the same cache object share its workspace and have to be
  * ordered (one stream, or graphs that do not overlap). */
 kvk_status kvk_paged_attention(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *q,

