@@ -49,9 +49,12 @@ kvk_status fail(kvk_status s, const char *fmt, ...) {
   return kvk_internal_fail(s, buf);
 }
 
-// A row view of the caller's as the kernels take it.  The stride of a
-// dimension of size one says nothing and is replaced.
-kvk_status take_rows(const kvk_rows *r, const char *name, int n_tokens, int heads, int D, int align, Rows &out) {
+bool aligned(const void *p, int bytes) { return !(reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)); }
+
+// A row view of the caller's as the kernels take it: elements of `elem` bytes,
+// rows on `align` bytes.  The stride of a dimension of size one says nothing
+// and is replaced.
+kvk_status take_rows(const kvk_rows *r, const char *name, int n_tokens, int heads, int D, int elem, int align, Rows &out) {
   if (!r || !r->data) return fail(KVK_ERR_INVALID_ARG, "%s is null", name);
   out.p = static_cast<uint8_t *>(r->data);
   out.hs = heads == 1 ? D : r->head_stride;
@@ -59,12 +62,13 @@ kvk_status take_rows(const kvk_rows *r, const char *name, int n_tokens, int head
   if (out.hs < D || out.ts < D)
     return fail(KVK_ERR_INVALID_ARG, "%s: strides must be at least head_dim (no broadcast rows)", name);
   if (out.hs >= (1LL << 38) || out.ts >= (1LL << 38)) return fail(KVK_ERR_INVALID_ARG, "%s: stride too large", name);
-  if (align > 1 && ((reinterpret_cast<uintptr_t>(out.p) & 15u) || out.hs % align || out.ts % align))
-    return fail(KVK_ERR_INVALID_ARG, "%s: rows must start on 16 bytes", name);
+  if (!aligned(out.p, align) || out.hs * elem % align || out.ts * elem % align)
+    return fail(KVK_ERR_INVALID_ARG, "%s: rows must start on %d bytes", name, align);
   return KVK_OK;
 }
 
-bool scale_ok(float s) { return std::isfinite(s * 1.4426950408889634f) && s > 0.f; }
+// (a subnormal scale would be zero on the way, and zero times a masked score NaN)
+bool scale_ok(float s) { return std::isfinite(s * 1.4426950408889634f) && std::isnormal(s) && s > 0.f; }
 
 // heads and widths that the attention kernels take
 kvk_status check_heads(int Hq, int Hkv, int D, int dtype) {
@@ -125,6 +129,8 @@ kvk_status check_call(const kvk_paged *p, int layer, const kvk_paged_batch *b, b
   if (empty) return KVK_OK;
   if (!b->cu_new || !b->lengths || (!b->table && b->max_pages))
     return fail(KVK_ERR_INVALID_ARG, "null offsets, lengths or table");
+  if (!aligned(b->cu_new, 4) || !aligned(b->lengths, 4) || !aligned(b->table, 4))
+    return fail(KVK_ERR_INVALID_ARG, "misaligned offsets, lengths or table");
   return KVK_OK;
 }
 
@@ -219,7 +225,7 @@ kvk_status kvk_rotary_apply(const kvk_rotary *r, const kvk_rows *q, const kvk_ro
   if (n_tokens < 0 || q_heads < 0 || k_heads < 0 || q_heads > 65535 || k_heads > 65535)
     return fail(KVK_ERR_INVALID_ARG, "tokens or heads out of range");
   if (n_tokens == 0 || q_heads + k_heads == 0) return KVK_OK;
-  if (!positions) return fail(KVK_ERR_INVALID_ARG, "null positions");
+  if (!positions || !aligned(positions, 4)) return fail(KVK_ERR_INVALID_ARG, "null or misaligned positions");
   RotArgs a = {};
   a.t = r->t;
   a.D = r->head_dim;
@@ -228,13 +234,14 @@ kvk_status kvk_rotary_apply(const kvk_rotary *r, const kvk_rows *q, const kvk_ro
   a.n_tokens = n_tokens;
   a.pos = positions;
   kvk_status s = KVK_OK;
+  const int elem = dtype == KVK_DTYPE_F32 ? 4 : 2;
   if (q_heads) {
-    s = take_rows(q, "q", n_tokens, q_heads, a.D, 1, a.q);
-    if (!s) s = take_rows(q_out, "q_out", n_tokens, q_heads, a.D, 1, a.qo);
+    s = take_rows(q, "q", n_tokens, q_heads, a.D, elem, elem, a.q);
+    if (!s) s = take_rows(q_out, "q_out", n_tokens, q_heads, a.D, elem, elem, a.qo);
   }
   if (!s && k_heads) {
-    s = take_rows(k, "k", n_tokens, k_heads, a.D, 1, a.k);
-    if (!s) s = take_rows(k_out, "k_out", n_tokens, k_heads, a.D, 1, a.ko);
+    s = take_rows(k, "k", n_tokens, k_heads, a.D, elem, elem, a.k);
+    if (!s) s = take_rows(k_out, "k_out", n_tokens, k_heads, a.D, elem, elem, a.ko);
   }
   if (s) return s;
   const cudaError_t e = launch_rotary(a, dtype, reinterpret_cast<cudaStream_t>(stream));
@@ -328,14 +335,15 @@ kvk_status kvk_paged_append(kvk_paged *p, int32_t layer, const kvk_paged_batch *
     return fail(KVK_ERR_INVALID_ARG, "a rotary of %d axes needs positions", rotary->t.n_axes);
   if (positions && !rotary) return fail(KVK_ERR_INVALID_ARG, "positions without a rotary");
   if (q && !rotary) return fail(KVK_ERR_INVALID_ARG, "queries are taken to be rotated: no rotary given");
+  if (!aligned(positions, 4)) return fail(KVK_ERR_INVALID_ARG, "misaligned positions");
   if (empty) return KVK_OK;
   RotArgs a = {};
   const int N = batch->n_tokens, D = p->d.head_dim, Hkv = p->d.n_kv_heads;
-  s = take_rows(k, "k", N, Hkv, D, 1, a.k);
-  if (!s) s = take_rows(v, "v", N, Hkv, D, 1, a.v);
+  s = take_rows(k, "k", N, Hkv, D, 2, 2, a.k);
+  if (!s) s = take_rows(v, "v", N, Hkv, D, 2, 2, a.v);
   if (!s && q) {
-    s = take_rows(q, "q", N, p->d.n_q_heads, D, 1, a.q);
-    if (!s) s = take_rows(q_out, "q_out", N, p->d.n_q_heads, D, 1, a.qo);
+    s = take_rows(q, "q", N, p->d.n_q_heads, D, 2, 2, a.q);
+    if (!s) s = take_rows(q_out, "q_out", N, p->d.n_q_heads, D, 2, 2, a.qo);
   }
   if (s) return s;
   if (rotary) a.t = rotary->t;
@@ -360,7 +368,7 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   if (empty) return KVK_OK;
   if (max_new < 1) return fail(KVK_ERR_INVALID_ARG, "max_new must be positive");
   AttnArgs a = {};
-  s = take_rows(q, "q", batch->n_tokens, p->d.n_q_heads, p->d.head_dim, 8, a.q);
+  s = take_rows(q, "q", batch->n_tokens, p->d.n_q_heads, p->d.head_dim, 2, 16, a.q);
   if (s) return s;
   if (!out || (reinterpret_cast<uintptr_t>(out) & 15u)) return fail(KVK_ERR_INVALID_ARG, "null or misaligned out");
   a.pv = view_of(p, layer, batch);
@@ -412,12 +420,13 @@ kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_
   if (batch < 0 || n_tokens < 0 || (int64_t)n_tokens * n_q_heads > (1 << 30))
     return fail(KVK_ERR_INVALID_ARG, "batch or n_tokens out of range");
   if (batch == 0 || n_tokens == 0) return KVK_OK;
-  if (!cu_seqlens) return fail(KVK_ERR_INVALID_ARG, "null offsets");
+  if (!cu_seqlens || !aligned(cu_seqlens, 4) || !aligned(error, 4))
+    return fail(KVK_ERR_INVALID_ARG, "null or misaligned offsets or error word");
   if (!out || (reinterpret_cast<uintptr_t>(out) & 15u)) return fail(KVK_ERR_INVALID_ARG, "null or misaligned out");
   AttnArgs a = {};
-  s = take_rows(q, "q", n_tokens, n_q_heads, head_dim, 8, a.q);
-  if (!s) s = take_rows(k, "k", n_tokens, n_kv_heads, head_dim, 8, a.k);
-  if (!s) s = take_rows(v, "v", n_tokens, n_kv_heads, head_dim, 8, a.v);
+  s = take_rows(q, "q", n_tokens, n_q_heads, head_dim, 2, 16, a.q);
+  if (!s) s = take_rows(k, "k", n_tokens, n_kv_heads, head_dim, 2, 16, a.k);
+  if (!s) s = take_rows(v, "v", n_tokens, n_kv_heads, head_dim, 2, 16, a.v);
   if (s) return s;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);

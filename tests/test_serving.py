@@ -101,6 +101,24 @@ def test_rotary_create(lib):
     assert so.kvk_rotary_destroy(h) == 0
 
 
+def test_rotary_refuses_misaligned_pointers(lib):
+    _, h = _rotary(lib)
+    so = lib.load()
+    rows = lambda *a: ctypes.byref(lib.Rows(*a))  # noqa: E731
+    ok = rows(256, 64, 64)
+    for q, q_out, dtype, pos in ((rows(257, 64, 64), ok, 1, 256), (ok, rows(257, 64, 64), 1, 256), (rows(258, 64, 64), ok, 0, 256),
+                                 (ok, ok, 1, 258)):
+        assert so.kvk_rotary_apply(h, q, q_out, 1, None, None, 0, dtype, 4, pos, None) == INVALID
+    assert so.kvk_rotary_destroy(h) == 0
+
+
+def test_prompt_attention_refuses_subnormal_scales_and_misaligned_words(lib):
+    so = lib.load()
+    ok = ctypes.byref(lib.Rows(256, 1024, 128))
+    for cu, scale, error in ((256, 1e-40, None), (258, 1.0, None), (256, 1.0, 257)):
+        assert so.kvk_prompt_attention(ok, ok, ok, 4, 8, 8, 128, lib.DTYPE_BF16, cu, 1, scale, 0, 256, error, None) == INVALID
+
+
 def test_prompt_attention_refusals(lib):
     so = lib.load()
     rows = lambda *a: ctypes.byref(lib.Rows(*a))  # noqa: E731
