@@ -229,6 +229,18 @@ def test_pages_that_the_window_has_left_need_no_entry(news, lens, page):
         b.check(window)
 
 
+@pytest.mark.parametrize("hq,hkv,d", [(64, 1, 128), (128, 2, 64), (33, 1, 128), (51, 3, 64), (65, 65, 64)])
+def test_head_groups_of_every_width(hq, hkv, d):
+    """The widest group, groups that fill no tile, many heads of their own; single
+    tokens of wide groups go with the chunks."""
+    b = Batch([1, 1, 1], [70, 1, 300], hq, hkv, d, BF16, 16, seed=41).fill()
+    b.check()
+    b = Batch([9, 0, 66], [9, 5, 200], hq, hkv, d, F16, 32, seed=42).fill()
+    for window in (0, 50):
+        b.check(window)
+    prompt_case([1, 77, 140], hq, hkv, d, BF16, windows=(0, 33), seed=43)
+
+
 def test_rows_in_no_sequence_stay():
     b = Batch([3, 2], [70, 9], 8, 2, 64, BF16, 16, rows_behind=4).fill()
     out = torch.full((b.n, 8, 64), 7.0, dtype=BF16, device="cuda")
