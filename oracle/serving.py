@@ -71,4 +71,5 @@ def attend_bound(out, mass, plain, span, d, t, u, smallest):
     type (u, half a step; below its normal range `smallest`, half its last step
     there), products summed over t positions, the result rounded (u)."""
     soft = 2 * (d + 4) * 2.0 ** -23 * span[..., None] + 2.0 ** -20 + 2 * (t + 8) * 2.0 ** -23
-    return u * np.abs(out) * (1 + u) + (1 + 2 * u) * (u + soft) * mass + smallest * plain + 2.0 ** -126
+    with np.errstate(invalid="ignore"):  # infinite results
+        return u * np.abs(out) * (1 + u) + (1 + 2 * u) * (u + soft) * mass + smallest * plain + 2.0 ** -126
