@@ -25,8 +25,8 @@
 // of their distance from their own sequence's end, prompts of 560 to 9000 tokens
 // took 528 us, with this one 473), dealt to the CTAs back and forth.  (More than
 // 128 sequences go one behind another: there are jobs enough to even out.)
-// Chunks over pages that make few jobs go in equal runs of tiles instead, one per
-// CTA: jobs that a run cuts leave their pieces (result, reference and sum of each
+// Chunks over pages that would fill a last round of jobs badly go in equal runs of
+// tiles instead, one per CTA: jobs that a run cuts leave their pieces (result, reference and sum of each
 // row) in the workspace, and a second kernel joins them.
 //
 // Measured: four prompts of 8192 tokens, 40 / 8 heads of 128, bf16: 1.82-1.92 ms,
@@ -38,6 +38,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <cmath>
 #include <type_traits>
 
 #include <algorithm>
@@ -998,9 +999,21 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   // at most so many jobs: every sequence's last one may be a partial one
   const int64_t jobs = (int64_t)a.pv.Hkv * (N / (2 * t.P) + std::min(a.pv.B, N));
-  // Runs where there are fewer than four jobs per SM at least (every token in
-  // one sequence).
-  t.a.runs = PAGED && (int64_t)a.pv.Hkv * ((N + 2 * t.P - 1) / (2 * t.P)) < 4 * a.sms;
+  // Runs where whole jobs would leave SMs idle for longer than the pieces take on
+  // their way through memory: the part of the last round of jobs that is not
+  // filled, against 5 tiles for a second kernel and up to 18 for the pieces of as
+  // many cut jobs (tiles by the table's width or the window, sequences taken to be
+  // of equal shares).  Measured (us, whole / runs, 40 / 8 heads of 128; new tokens
+  // over positions): 400 over 2000 27.7 / 32.2, over 4000 47 / 39; 1000 over 2000
+  // 35 / 48, over 4000 73 / 66; 512 over 8192 86 / 70; 600 over 600 15 / 28; 4 x 33
+  // over 2000 27 / 18; 32 x 4 over 1900 54 / 55, over 8192 182 / 174.  Up to four
+  // rounds: of 2048 tokens over 32768, 1 (2.2 rounds) 971 / 916, 4 (8.6) 3473 / 3894.
+  const int64_t seqs = std::min(a.pv.B, N), share = (N + seqs - 1) / seqs, blocks = (share + 2 * t.P - 1) / (2 * t.P);
+  const int64_t seen = std::min((int64_t)a.pv.max_pages << a.pv.page_shift, (int64_t)a.window + 2 * t.P + kTcT);
+  const double full = (double)a.pv.Hkv * seqs * blocks, waves = full / a.sms;
+  const double idle = (std::ceil(waves) - waves) * (double)((seen + kTcT - 1) / kTcT);
+  const double rows = (double)std::min<int64_t>(2 * t.P, share) * a.G / (2 * kTcT);
+  t.a.runs = PAGED && waves < 4 && idle > 5 + 0.12 * std::min(full, (double)a.sms) * rows;
   if (!t.a.runs)
     return launch_pdl(attn_tc_kernel<D, BF16, PAGED>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(kTcThreads),
                       Smem<D>::kBytes, st, t);

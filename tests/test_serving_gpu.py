@@ -241,6 +241,64 @@ def test_head_groups_of_every_width(hq, hkv, d):
     prompt_case([1, 77, 140], hq, hkv, d, BF16, windows=(0, 33), seed=43)
 
 
+RUNS = [([9], [3000]), ([300, 7], [2500, 2100]), ([24, 1, 0, 33], [4000, 10, 70, 1500]), ([600], [2600])]
+
+
+@pytest.mark.parametrize("news,lens", RUNS)
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 128, BF16, 16), (7, 1, 128, F16, 64), (8, 2, 64, BF16, 128)])
+def test_chunks_over_long_contexts(news, lens, hq, hkv, d, dtype, page):
+    """Few jobs of many tiles: cut into pieces and joined, in either form of the join."""
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=51).fill()
+    for window in (0, 1300):
+        b.check(window)
+    first = b.attend(0.1)
+    for _ in range(3):
+        assert torch.equal(b.attend(0.1)[: sum(news)], first[: sum(news)])
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_values_that_are_not_finite_in_pieces_of_jobs(bad):
+    news, lens = [80, 150], [2000, 1900]
+    b = Batch(news, lens, 10, 2, 128, BF16, 16, seed=52)
+    for s, t, ch in [(0, 1999, 3), (1, 1898, 77), (1, 1820, 5), (0, 1950, 127)]:
+        b.v[s][t, 1, ch] = bad
+    b.k[1][1899, 0, 9] = float("nan")
+    b.fill()
+    for window in (0, 1200):
+        scale = 1.0 / math.sqrt(128)
+        got = f64(b.attend(scale, window)[: sum(news)])
+        ref, tol = b.expected(scale, window)
+        fine = np.isfinite(ref)
+        assert (np.isfinite(got) == fine).all()
+        assert (np.abs(got[fine] - ref[fine]) <= tol[fine]).all()
+
+
+def test_chunks_over_long_contexts_captured():
+    """A graph of calls whose jobs are cut, replayed as the lengths grow."""
+    b = Batch([40, 20], [3000, 2200], 10, 2, 128, BF16, 16, seed=53).fill()
+    lens = [2000, 2200]
+    b.lengths.copy_(ints(lens))
+    q, scale = b.q.cuda(), 1.0 / math.sqrt(128)
+    out = torch.empty_like(q)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=stream):
+        for _ in range(2):
+            b.attend(scale, q=q, out=out)
+    full_k, full_v = b.k, b.v
+    for lens in ([2000, 2200], [3000, 100], [60, 2200]):
+        b.lengths.copy_(ints(lens))
+        out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        b.k, b.v, b.lens = [x[:m] for x, m in zip(full_k, lens)], [x[:m] for x, m in zip(full_v, lens)], lens
+        ref, tol = b.expected(scale, 0)
+        close(out, ref, tol, f"lengths {lens}")
+    assert b.cache.device_error() == 0
+
+
 def test_rows_in_no_sequence_stay():
     b = Batch([3, 2], [70, 9], 8, 2, 64, BF16, 16, rows_behind=4).fill()
     out = torch.full((b.n, 8, 64), 7.0, dtype=BF16, device="cuda")
