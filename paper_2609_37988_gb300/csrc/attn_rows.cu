@@ -22,9 +22,10 @@
 // and results are computed transposed, S^T = K Q^T and O^T += V^T P^T on
 // mma.m16n8k16 (positions and channels in the 16, query rows in the 8: few rows
 // waste little), fp32 accumulation, the softmax online in base 2, each warp with
-// its own maxima and sums; P enters as hi + lo halves.  Measured: a 14B-shaped
-// step over 32 x 8192 positions in pages of 16, 165 us (6.5 TB/s, 96 % of the copy
-// bandwidth); 8 x 8192 51 us, 1 x 8192 15 us, of which 10 are start and joining.
+// its own maxima and sums; P enters as hi + lo halves (f16: 2^14 times as large, so
+// that small weights stay normal).  Measured: a 14B-shaped step over 32 x 8192
+// positions in pages of 16, 165 us (6.5 TB/s, 96 % of the copy bandwidth); 8 x 8192
+// 51 us, 1 x 8192 15 us, of which 10 are start and joining.
 //
 // Non-finite values: weight 0 times an infinite value would be NaN, so tiles
 // that some row does not see in full are looked through first, and a warp whose
@@ -185,6 +186,11 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
   constexpr int RB = D * 2;            // bytes of a row
   constexpr int kTile = kT * RB;       // bytes of a key (or value) tile
   constexpr int KS = D / 16, NS = rows_stages<D>(), RU = 8 * NB;
+  // Weights are at most 1: the reference is the largest score so far.  In f16 those
+  // below 2^-14 would lose bits to the type's subnormals and those below 2^-25 all of
+  // them, while the row's sum has them whole.  Kept 2^14 times as large (the sum too:
+  // the quotient is the same) they are off by 2^-39 of the largest at most.
+  constexpr float kShift = BF16 ? 0.f : 14.f;
   const AttnArgs &a = ra.a;
   extern __shared__ uint8_t sm_raw[];
   uint8_t *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
@@ -470,7 +476,7 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float ref = m[2 * nb + (e & 1)];
-          s[nb][e] = fast_exp2(s[nb][e] - (ref == -INFINITY ? 0.f : ref));
+          s[nb][e] = fast_exp2(s[nb][e] - (ref == -INFINITY ? 0.f : ref) + kShift);
           l[2 * nb + (e & 1)] += s[nb][e];
         }
 #pragma unroll

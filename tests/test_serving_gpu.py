@@ -725,3 +725,24 @@ def test_prompts_then_chunks_then_steps(hq, hkv, d, dtype, page):
                 close(own[rows], r[0], tol, "prompt")
             at += m
     assert cache.device_error() == 0
+
+
+@pytest.mark.parametrize("gap", [12.0, 15.0, 17.5, 20.0])
+@pytest.mark.parametrize("d,page,positions", [(128, 16, 4096), (64, 128, 4096), (128, 32, 400)])
+def test_f16_weights_far_below_the_largest(gap, d, page, positions):
+    """One key `gap` above all the others, its value zero: the result is what the
+    others' small weights bring.  They enter the product 2^14 times (few tokens) or
+    2^8 times (chunks) as large as the row's largest one is 1, so that half the last
+    step below f16's normal range is 2^-39 or 2^-33 of it."""
+    b = Batch([1], [positions], 2, 1, d, F16, page, seed=61, rows_behind=20)
+    b.q.zero_()
+    b.q[..., 0] = 1.0
+    b.k[0].zero_()
+    b.k[0][positions // 3, 0, 0] = gap
+    b.v[0][:] = 1024.0 + 4 * torch.arange(d)
+    b.v[0][positions // 3] = 0.0
+    b.fill()
+    r = osv.attend(f64(b.q[:1]), *(np.transpose(f64(x[0]), (1, 0, 2)) for x in (b.k, b.v)), 1.0)
+    for max_new, small in ((1, 2.0 ** -39), (b.n, 2.0 ** -33)):
+        got = b.attend(1.0, max_new=max_new)[:1]
+        close(got, r[0], osv.attend_bound(*r, d, positions, U[F16], small), f"max_new {max_new}")
