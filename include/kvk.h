@@ -521,8 +521,10 @@ typedef struct {
  * or (2 i, 2 i + 1) where `adjacent` is 1, becomes
  *   (x c - y s, y c + x s),  (c, s) = factor (cos, sin)(pos[axis[i]] inv_freq[i]);
  * the channels from rotary_dim on stay.  Text has one axis; images and video
- * have a time, a height and a width.  Angles are exact to 2^-32 of a turn plus
- * the position times inv_freq's own rounding, at any position.
+ * have a time, a height and a width.  The angle of the inv_freq given is kept to
+ * 2^-32 of a turn plus the position times 2^-63 of a turn, at any position and for
+ * either sign; its cosine and sine are taken of it rounded to binary32, 2^-26 of a
+ * turn at most.
  * inv_freq (rotary_dim / 2 doubles) and axis (as many) are host arrays, copied.
  * head_dim: even, at most 256; rotary_dim: even, at most head_dim; n_axes: 1..8.
  * Errors: INVALID_ARG. */

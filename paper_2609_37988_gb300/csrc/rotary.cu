@@ -3,11 +3,12 @@
 //
 // Frequency i (of R/2) turns with the position on its axis a(i): its pair of
 // channels (x, y) becomes (x c - y s, y c + x s) with (c, s) = factor *
-// (cos, sin)(pos[a(i)] f_i).  Angles are exact to 2^-32 of a turn at any
-// position: f_i / (2 pi) is kept as a 64-bit binary fraction of a turn, its
-// product with the position wraps modulo 2^64, which drops whole turns and
-// nothing else, and cospi/sinpi of the leading 32 bits follow.  (The angle in
-// binary32 would be off by 0.06 at position 10^6.)
+// (cos, sin)(pos[a(i)] f_i).  The angle is right to 2^-32 of a turn at any
+// position: f_i / (2 pi) is kept as a 64-bit binary fraction of a turn (2^-64 off),
+// its product with the position wraps modulo 2^64, which drops whole turns and
+// nothing else, and cospi/sinpi of the leading 32 bits follow, rounded to binary32
+// (2^-26 of a turn where the angle is near half of one, less in proportion below).
+// (The angle in binary32 would be off by 0.06 at position 10^6.)
 //
 // Memory-bound: every channel is read once and written once.  A thread keeps one
 // place in the rows of one token, 2 * VEC channels (two 16-byte pieces), with

@@ -194,17 +194,18 @@ kvk_status kvk_rotary_create(int32_t head_dim, int32_t rotary_dim, int32_t n_axe
   r->t.n_axes = n_axes;
   r->t.adjacent = adjacent;
   r->t.factor = factor;
-  // 1 / (2 pi) in two doubles: the turn's fraction keeps more bits than one
-  // double of it has
+  // f / (2 pi) as a 64-bit fraction of a turn, 1 / (2 pi) in two doubles: of
+  // |f| (whole turns of a number that is not negative drop out exactly), a signed
+  // remainder added, the sign put back last; all modulo 2^64.
   constexpr double hi = 0.15915494309189535, lo = -9.839338337591243e-18;
   for (int i = 0; i < n; ++i) {
-    const double f = inv_freq[i], t = f * hi, rest = std::fma(f, hi, -t) + f * lo;
-    const double whole = std::floor(t);
-    const double frac = t - whole;  // exact, in [0, 1]
-    uint64_t s = frac >= 1.0 ? 0 : (uint64_t)std::ldexp(frac, 64);
-    const double add = std::ldexp(rest - std::floor(rest), 64);  // [0, 2^64]
-    s += add >= 18446744073709551616.0 ? 0 : (uint64_t)add;
-    r->t.step[i] = s;
+    const double f = std::fabs(inv_freq[i]), t = f * hi;
+    const double frac = t - std::floor(t);  // exact, in [0, 1)
+    double rest = std::fma(f, hi, -t) + f * lo;
+    rest -= std::nearbyint(rest);  // exact, in [-1/2, 1/2]
+    if (rest == 0.5) rest = -0.5;
+    const uint64_t s = (uint64_t)std::nearbyint(std::ldexp(frac, 64)) + (uint64_t)(int64_t)std::nearbyint(std::ldexp(rest, 64));
+    r->t.step[i] = inv_freq[i] < 0 ? 0 - s : s;
     r->t.axis[i] = (uint8_t)axis[i];
   }
   *out = r;

@@ -3,6 +3,7 @@ the paged cache's append and attention, attention over whole prompts, and a run
 of them together.  Every tolerance is oracle.serving.attend_bound's (or, for
 the rotary, the bound beside it), derived from the roundings each path makes."""
 import math
+from fractions import Fraction
 
 import numpy as np
 import pytest
@@ -13,6 +14,7 @@ from oracle import serving as osv
 pytestmark = pytest.mark.gpu
 
 BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+PI = Fraction(314159265358979323846264338327950288419716939937510, 10 ** 50)
 U = {BF16: 2.0 ** -8, F16: 2.0 ** -11, F32: 2.0 ** -24}
 # half the last step below the type's normal range, relative to a row's largest weight
 SMALL = {BF16: 0.0, F16: 2.0 ** -25}
@@ -746,3 +748,43 @@ def test_f16_weights_far_below_the_largest(gap, d, page, positions):
     for max_new, small in ((1, 2.0 ** -39), (b.n, 2.0 ** -33)):
         got = b.attend(1.0, max_new=max_new)[:1]
         close(got, r[0], osv.attend_bound(*r, d, positions, U[F16], small), f"max_new {max_new}")
+
+
+def turn_of(f, p):
+    """p * f / (2 pi) as a fraction of a turn in [-1/2, 1/2), from f's own binary value."""
+    x = Fraction(f) * p / (2 * PI)
+    return x - math.floor(x + Fraction(1, 2))
+
+
+@pytest.mark.parametrize("positive", [True, False])
+@pytest.mark.parametrize("freqs", [[1.0, -1.0, 1e-3, -1e-3, 0.75, -0.5, 3.0, 40.0],
+                                   [10000.0 ** (-i / 64) for i in range(0, 32, 4)],
+                                   [-(1000000.0 ** (-i / 64)) for i in range(3, 35, 4)]])
+def test_rotary_angles_at_far_positions(freqs, positive):
+    """Angles near whole turns at positions near 2^31, where the angle's 32 bits are
+    exact in binary32 and its sine is small: what is left is the 2^-32 of a turn cut
+    off, the position times 2^-63 of a turn (the step's own rounding) and 2 ulp of a
+    sine below 2^-5 (2^-28)."""
+    from paper_2609_37988_gb300.serving import Rotary
+    n, tokens = len(freqs), 12
+    pos = np.zeros((n, tokens), np.int64)
+    for i, f in enumerate(freqs):
+        found, p, per = [], 2 ** 31 - 1, Fraction(abs(f)) / (2 * PI)
+        while len(found) < tokens:
+            p = min(p - 1, math.floor(math.floor(p * per) / per) + 1)  # about a turn back
+            for c in (p, p - 1):
+                if len(found) < tokens and abs(turn_of(f, c)) < Fraction(1, 300):
+                    found.append(c)
+            p -= 1
+        pos[i] = found
+    if not positive:
+        pos = -pos
+    rot = Rotary(head_dim=2 * n, inv_freq=freqs, axes=list(range(n)))
+    x = torch.zeros((tokens, 1, 2 * n), device="cuda")
+    x[..., :n] = 1.0
+    got = f64(rot.apply(x, None, ints(pos.tolist()))[0])[:, 0]
+    tol = 2 * math.pi * (2.0 ** -32 + 2.0 ** 31 * 2.0 ** -63) + 2.0 ** -28
+    for i, f in enumerate(freqs):
+        for t in range(tokens):
+            want = math.sin(2 * math.pi * float(turn_of(f, int(pos[i, t]))))
+            assert abs(got[t, n + i] - want) <= tol, (f, int(pos[i, t]), got[t, n + i] - want)
