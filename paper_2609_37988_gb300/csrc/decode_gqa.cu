@@ -2,6 +2,8 @@
 // the tensor maps its kept-list gather reads.
 #include <cuda.h>  // CUtensorMap and its enums (the encoder is reached through the runtime)
 
+#include <atomic>
+
 #include "kernels.h"
 #include "layout.h"
 
@@ -49,7 +51,8 @@ cudaError_t encode_tensor_map_tiled(void *map, int dtype, int rank, void *base,
                               const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                               const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
                               CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-  static Encode encode = nullptr;
+  static std::atomic<Encode> known{nullptr};
+  Encode encode = known.load(std::memory_order_relaxed);
   if (!encode) {
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
@@ -58,14 +61,24 @@ cudaError_t encode_tensor_map_tiled(void *map, int dtype, int rank, void *base,
     if (e != cudaSuccess) return e;
     if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
     encode = reinterpret_cast<Encode>(fn);
+    known.store(encode, std::memory_order_relaxed);
   }
-  const CUresult r = encode(static_cast<CUtensorMap *>(map), (CUtensorMapDataType)dtype,
-                            (cuuint32_t)rank, base, reinterpret_cast<const cuuint64_t *>(dims),
-                            reinterpret_cast<const cuuint64_t *>(strides),
-                            reinterpret_cast<const cuuint32_t *>(box),
-                            reinterpret_cast<const cuuint32_t *>(elem_strides),
-                            (CUtensorMapInterleave)interleave, (CUtensorMapSwizzle)swizzle,
-                            (CUtensorMapL2promotion)l2_promotion, (CUtensorMapFloatOOBfill)oob_fill);
+  auto call = [&] {
+    return encode(static_cast<CUtensorMap *>(map), (CUtensorMapDataType)dtype, (cuuint32_t)rank, base,
+                  reinterpret_cast<const cuuint64_t *>(dims), reinterpret_cast<const cuuint64_t *>(strides),
+                  reinterpret_cast<const cuuint32_t *>(box), reinterpret_cast<const cuuint32_t *>(elem_strides),
+                  (CUtensorMapInterleave)interleave, (CUtensorMapSwizzle)swizzle, (CUtensorMapL2promotion)l2_promotion,
+                  (CUtensorMapFloatOOBfill)oob_fill);
+  };
+  CUresult r = call();
+  if (r == CUDA_ERROR_INVALID_CONTEXT) {
+    // a thread that has made no runtime call yet: its device's context becomes current
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaSetDevice(dev);
+    if (e != cudaSuccess) return e;
+    r = call();
+  }
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 

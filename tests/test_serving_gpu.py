@@ -788,3 +788,32 @@ def test_rotary_angles_at_far_positions(freqs, positive):
         for t in range(tokens):
             want = math.sin(2 * math.pi * float(turn_of(f, int(pos[i, t]))))
             assert abs(got[t, n + i] - want) <= tol, (f, int(pos[i, t]), got[t, n + i] - want)
+
+
+@pytest.mark.parametrize("what", ["prompt", "chunk", "few"])
+def test_first_call_of_a_thread(what):
+    """Tensor maps of a call's queries are encoded by the driver, which wants a
+    current context; a thread that has made no call yet has none."""
+    import threading
+    from paper_2609_37988_gb300.serving import prompt_attention
+    b = Batch([70, 33] if what == "chunk" else [1, 1], [700, 500], 10, 2, 128, BF16, 16, seed=76).fill()
+    q, k, v = (randn(gen(77), (200, h, 128), BF16) for h in (10, 2, 2))
+    cu, bq = offsets([150, 50]), b.q.cuda()
+    out = torch.empty_like(q if what == "prompt" else bq)
+    call = {"prompt": lambda: prompt_attention(q, k, v, cu, 0.088, out=out)}.get(what, lambda: b.attend(0.088, q=bq, out=out))
+    keep = call().clone()
+    out.zero_()
+    torch.cuda.synchronize()
+    failed = []
+
+    def work():
+        try:
+            call()
+        except Exception as e:
+            failed.append(e)
+
+    t = threading.Thread(target=work)
+    t.start()
+    t.join()
+    torch.cuda.synchronize()
+    assert not failed and torch.equal(out, keep)
