@@ -603,7 +603,8 @@ kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_bat
  * one that is not finite.  An infinite value that it does see makes its channel
  * infinite or NaN.  softmax_scale: a positive, finite, normal number.
  * Calls that use the same cache object share its workspace and have to be
- * ordered (one stream, or graphs that do not overlap). */
+ * ordered on the GPU (one stream, or graphs that do not overlap); threads may
+ * make them at the same time. */
 kvk_status kvk_paged_attention(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *q,
                                float softmax_scale, int32_t max_new, int32_t window, void *out, kvk_stream stream);
 /* As kvk_get_device_error, for the paged cache's own error word. */

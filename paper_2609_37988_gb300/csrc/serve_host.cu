@@ -7,6 +7,7 @@
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
+#include <mutex>
 #include <new>
 #include <vector>
 
@@ -36,6 +37,7 @@ struct kvk_paged {
   std::vector<PageMap> maps;  // kMaps tensor maps of a layer's pools, as AttnArgs has them
   uint8_t *ws;
   int device, sms, page_shift;
+  std::mutex calls;  // an attention's launches follow one another
 };
 
 namespace {
@@ -391,7 +393,13 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.wv = maps[2].bytes;
   a.ok = maps[3].bytes;
   a.ov = maps[4].bytes;
-  const cudaError_t e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+  // Two launches around the workspace's list of cut units: another thread's must
+  // not come between them, its units would be joined into this call's output.
+  cudaError_t e;
+  {
+    std::lock_guard<std::mutex> one(p->calls);
+    e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+  }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;
 }

@@ -184,7 +184,8 @@ class PagedCache:
     Calls take the batch as device int32 tensors: ``cu [B + 1]`` offsets of the
     new tokens, ``lengths [B]`` positions held with the new tokens, ``table
     [B, max_pages]`` each sequence's pages.  Calls on one object share its
-    workspace: order them."""
+    workspace: order them on the GPU (one stream, say; threads may call at the
+    same time)."""
 
     def __init__(self, *, n_q_heads: int, n_layers: int = None, n_kv_heads: int = None, head_dim: int = None,
                  n_pages: int = None, page_size: int = 16, dtype=torch.bfloat16, device=None, k_pages=None, v_pages=None):

@@ -817,3 +817,39 @@ def test_first_call_of_a_thread(what):
     t.join()
     torch.cuda.synchronize()
     assert not failed and torch.equal(out, keep)
+
+
+def test_calls_of_several_threads_on_one_stream():
+    """An attention that cuts its work is two launches around one list in the
+    cache's workspace: threads that share the cache and a stream may call at the
+    same time all the same."""
+    import threading
+    b = Batch([1, 2, 1, 33], [3000, 900, 50, 2000], 10, 2, 128, BF16, 16, seed=62).fill()
+    q, scale = b.q.cuda(), 0.088
+    # few tokens of three sequences and of one, a chunk, all of them
+    calls = []
+    for s in ([0, 1, 2], [0], [3], [0, 1, 2, 3]):
+        at = np.concatenate([[0], np.cumsum(b.news)])
+        rows = torch.cat([torch.arange(at[i], at[i + 1]) for i in s]).cuda()
+        calls.append((q[rows].contiguous(), offsets([b.news[i] for i in s]), b.lengths[s].contiguous(),
+                      b.table_d[s].contiguous(), max(b.news[i] for i in s)))
+    run = lambda c, **kw: b.cache.attend(0, *c[:4], scale, max_new=c[4], **kw)  # noqa: E731
+    want = [run(c) for c in calls]
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got, start = [[] for _ in calls], threading.Barrier(len(calls))
+
+    def work(i):
+        start.wait()
+        for _ in range(100):
+            got[i].append(run(calls[i], stream=stream))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(calls))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    stream.synchronize()
+    assert b.cache.device_error(stream) == 0
+    for x, w in zip(got, want):
+        assert len(x) == 100 and all(torch.equal(y, w) for y in x)
