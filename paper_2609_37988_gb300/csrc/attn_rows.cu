@@ -476,7 +476,9 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float ref = m[2 * nb + (e & 1)];
-          s[nb][e] = fast_exp2(s[nb][e] - (ref == -INFINITY ? 0.f : ref) + kShift);
+          s[nb][e] -= ref == -INFINITY ? 0.f : ref;
+          if constexpr (kShift != 0.f) s[nb][e] += kShift;  // (adding 0 would cost 1 %)
+          s[nb][e] = fast_exp2(s[nb][e]);
           l[2 * nb + (e & 1)] += s[nb][e];
         }
 #pragma unroll
