@@ -607,6 +607,13 @@ kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_bat
  * make them at the same time. */
 kvk_status kvk_paged_attention(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *q,
                                float softmax_scale, int32_t max_new, int32_t window, void *out, kvk_stream stream);
+/* Waits of an attention are bounded (2^20 polls).  One that gives up ends its
+ * CTA's others, sets KVK_DEVERR_TIMEOUT and leaves the call's outputs unspecified;
+ * what is in flight lands first, and later calls are unaffected.  give_up 1: the
+ * calls enqueued from now on copy no tile, as if the wait for a place to copy to
+ * had run out, and give up in all that waits for one: a way to exercise that path
+ * without a fault.  0 (default): they work.  Errors: INVALID_ARG. */
+kvk_status kvk_paged_set_give_up(kvk_paged *cache, int32_t give_up);
 /* As kvk_get_device_error, for the paged cache's own error word. */
 kvk_status kvk_paged_get_device_error(kvk_paged *cache, kvk_stream stream, int32_t *code);
 

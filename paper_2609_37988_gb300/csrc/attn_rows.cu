@@ -325,7 +325,9 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
       return seen(x) ? pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)] : pv.n_pages;
     };
     int page = look_up(at);
-    bool ok = true;
+    // (asked once: a limit from the arguments in the loop's waits cost 1.3 %)
+    bool ok = !a.give_up;
+    if (!ok && lane == 0) *abort_flag = 1;
     for (int w = 0; w < mine && ok; ++w) {
       const int t = at.lo + at.t * pt + (lane << shift);
       const int y = t & ((1 << pv.page_shift) - 1), h = at.h * HC;
@@ -352,14 +354,16 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_rows_kernel(const __gri
         next_stage();
       }
     }
-    if (*abort_flag && lane == 0) {  // the copies in flight land before the CTA ends
+    pdl_trigger();
+    // the copies in flight land before the CTA ends, whoever waits for them: the
+    // other warps may give up after this one is through
+    if (lane == 0) {
       for (int i = 0; i < NS; ++i) {
         if (par == 0 && i >= stage) break;
         mbar_wait(&s_full[i], i < stage ? par : par ^ 1, kWaits);
       }
+      if (*abort_flag) set_err(pv.err, kErrTimeout);
     }
-    if (*abort_flag && lane == 0) set_err(pv.err, kErrTimeout);
-    pdl_trigger();
     return;
   }
 

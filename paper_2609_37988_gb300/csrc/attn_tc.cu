@@ -259,6 +259,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         const int i = lane / NB, half = lane % NB;
         tma_load_3d(sm + SM::kQ + i * SM::kTile + half * kBox, &t.mq, 64 * half, j.h * G, j.q0 + j.tok0 + i * P, qfull);
       }
+      // (asked once a job: a limit from the arguments in every wait cost 4 %)
+      if (PAGED && a.give_up) {
+        if (lane == 0) *abort_flag = 1;
+        return false;
+      }
       // page of this lane's part of a tile, one tile ahead
       const int shift = PAGED ? min(pv.page_shift, 6) : 7, parts = kTcT >> shift;
       const int part = lane / NB, half = lane % NB;
@@ -484,8 +489,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       }
     }
     if (!__any_sync(kAll, *abort_flag)) emit(end);
-    // after a wait that gave up: the copies in flight land before the CTA ends
-    if (*abort_flag && lane == 0) {
+    // the copies in flight land before the CTA ends, whoever waits for them: another
+    // warp may give up after this one is through
+    if (lane == 0) {
       if (loads > 0) mbar_wait(qfull, (loads - 1) & 1, kWaits);
       for (int i = 0; i < NS; ++i) {
         if (ph == 0 && i >= s) break;  // never used
@@ -619,11 +625,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         if (more && ++s == NS) s = 0, ph ^= 1;
       }
     }
-    // after a wait that gave up: the products in flight end before TMEM is freed
-    if (*abort_flag) {
-      umma_commit_if(leader, drain);
-      mbar_wait(drain, 0, kWaits);
-    }
+    // the products in flight end before TMEM is freed, likewise
+    umma_commit_if(leader, drain);
+    mbar_wait(drain, 0, kWaits);
     __syncwarp();
   } else if (warp >= 10) {
     // -- values of partly seen tiles ----------------------------------------------

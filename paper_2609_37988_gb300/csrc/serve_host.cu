@@ -4,6 +4,7 @@
 // stream; allocates no device memory.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -37,6 +38,7 @@ struct kvk_paged {
   std::vector<PageMap> maps;  // kMaps tensor maps of a layer's pools, as AttnArgs has them
   uint8_t *ws;
   int device, sms, page_shift;
+  std::atomic<int32_t> give_up{0};
   std::mutex calls;  // an attention's launches follow one another
 };
 
@@ -387,6 +389,7 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
   a.device = p->device;
+  a.give_up = p->give_up.load(std::memory_order_relaxed);
   const PageMap *maps = &p->maps[(size_t)layer * kMaps];
   a.mk = maps[0].bytes;
   a.wk = maps[1].bytes;
@@ -401,6 +404,13 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
     e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
+  return KVK_OK;
+}
+
+kvk_status kvk_paged_set_give_up(kvk_paged *p, int32_t give_up) {
+  if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
+  if (give_up != 0 && give_up != 1) return fail(KVK_ERR_INVALID_ARG, "give_up must be 0 or 1");
+  p->give_up.store(give_up, std::memory_order_relaxed);
   return KVK_OK;
 }
 

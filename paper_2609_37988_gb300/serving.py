@@ -294,6 +294,11 @@ class PagedCache:
               n if max_new is None else max_new, window, out.data_ptr())
         return out
 
+    def set_give_up(self, give_up: bool):
+        """Whether attentions give up before their first tile, as if a bounded wait
+        had run out (setting the timeout error): for tests of that path."""
+        check(self.lib.kvk_paged_set_give_up(self.handle, int(give_up)))
+
     def device_error(self, stream=None) -> int:
         """Synchronise, read and clear the device error word (0 = none)."""
         code = ctypes.c_int32()

@@ -163,3 +163,7 @@ def test_binding_checks_shapes():
         PagedCache(n_q_heads=2, k_pages=[torch.zeros((1, 1, 16, 64))], v_pages=[torch.zeros((1, 1, 16, 64))])
     with pytest.raises(TypeError):
         PagedCache(n_q_heads=2, n_layers=1, n_kv_heads=1, head_dim=64, n_pages=1, dtype=torch.float64, device="cuda:0")
+
+
+def test_give_up_of_no_cache(lib):
+    assert lib.load().kvk_paged_set_give_up(None, 0) == INVALID

@@ -853,3 +853,24 @@ def test_calls_of_several_threads_on_one_stream():
     assert b.cache.device_error(stream) == 0
     for x, w in zip(got, want):
         assert len(x) == 100 and all(torch.equal(y, w) for y in x)
+
+
+# few tokens in whole units and in runs, chunks in whole jobs and in runs
+FORMS = [([1, 2, 1], [300, 2, 77], 0), ([1, 2, 1], [3000, 700, 5], 0), ([200, 70], [400, 500], 0), ([300, 7], [2500, 2100], 0),
+         ([24, 1, 0, 33], [4000, 10, 70, 1500], 1000)]
+
+
+@pytest.mark.parametrize("news,lens,window", FORMS)
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 128, BF16, 16), (8, 2, 64, F16, 64)])
+def test_attention_gives_up_and_recovers(news, lens, window, hq, hkv, d, dtype, page):
+    """No tile is copied, and every wait for one gives up: the call sets the timeout
+    error (and nothing else) and returns; the next one is as before."""
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=75).fill()
+    keep = b.check(window)
+    scale, n = 1.0 / math.sqrt(d), sum(news)
+    for _ in range(2):
+        b.cache.set_give_up(True)
+        b.attend(scale, window)
+        assert b.cache.device_error() == 8
+        b.cache.set_give_up(False)
+        assert torch.equal(keep[:n], b.attend(scale, window)[:n]) and b.cache.device_error() == 0
