@@ -624,12 +624,17 @@ kvk_status kvk_paged_get_device_error(kvk_paged *cache, kvk_stream stream, int32
  * out: device [n_tokens, n_q_heads, head_dim] of `dtype` (BF16 or F16),
  * 16-byte aligned.  Offsets out of order or range are clamped.  head_dim 64 or
  * 128, at most 64 query heads per KV head.  error: device int32 that gets
- * KVK_DEVERR bits, or NULL.  Non-finite keys and values as above.
+ * KVK_DEVERR bits; NULL: a word of the library's, one a device, which
+ * kvk_prompt_get_device_error reads.  Non-finite keys and values as above.
  * Errors: INVALID_ARG, UNSUPPORTED. */
 kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_rows *v, int32_t n_tokens,
                                 int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                                 const int32_t *cu_seqlens, int32_t batch, float softmax_scale, int32_t window, void *out,
                                 int32_t *error, kvk_stream stream);
+/* As kvk_get_device_error, for the current device's prompts that were given no
+ * error word; as kvk_paged_set_give_up, for all prompts. */
+kvk_status kvk_prompt_get_device_error(kvk_stream stream, int32_t *code);
+kvk_status kvk_prompt_set_give_up(int32_t give_up);
 
 const char *kvk_status_string(kvk_status s);
 const char *kvk_last_error(void);

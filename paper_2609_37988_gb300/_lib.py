@@ -114,6 +114,8 @@ _SIGS = {
     "kvk_paged_set_give_up": [_P, _I],
     "kvk_paged_get_device_error": [_P, _P, ctypes.POINTER(_I)],
     "kvk_prompt_attention": [_R, _R, _R, _I, _I, _I, _I, _I, _P, _I, _F, _I, _P, _P, _P],
+    "kvk_prompt_get_device_error": [_P, ctypes.POINTER(_I)],
+    "kvk_prompt_set_give_up": [_I],
     "kvk_status_string": [_I],
     "kvk_last_error": [],
     "kvk_version": [],

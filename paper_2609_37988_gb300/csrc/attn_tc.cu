@@ -260,7 +260,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         tma_load_3d(sm + SM::kQ + i * SM::kTile + half * kBox, &t.mq, 64 * half, j.h * G, j.q0 + j.tok0 + i * P, qfull);
       }
       // (asked once a job: a limit from the arguments in every wait cost 4 %)
-      if (PAGED && a.give_up) {
+      if (a.give_up) {
         if (lane == 0) *abort_flag = 1;
         return false;
       }

@@ -91,7 +91,7 @@ struct AttnArgs {
   TcList *tc_list;
   int runs;               // tensor-core form: equal runs of tiles
   int sms, device;
-  int give_up;            // over pages: a CTA's copying warp gives up before its first tile
+  int give_up;            // a CTA's copying warp gives up before its first tile
 };
 cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads);
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);

@@ -165,6 +165,41 @@ cudaError_t launch_attn(const AttnArgs &a, int dtype, cudaStream_t st) {
   return launch_attn_tc(a, dtype, st);
 }
 
+// The error word of prompts whose caller gives none, one a device.
+__device__ int32_t g_prompt_err;
+constexpr int kMaxDevices = 64;
+std::mutex g_prompt_mu;
+int32_t *g_prompt_word[kMaxDevices] = {};
+std::atomic<int32_t> g_prompt_give_up{0};
+
+// its address on the current device (looked up once)
+cudaError_t prompt_word(int dev, int32_t **word) {
+  if (dev < 0 || dev >= kMaxDevices) return cudaErrorInvalidDevice;
+  std::lock_guard<std::mutex> lock(g_prompt_mu);
+  if (!g_prompt_word[dev]) {
+    void *p = nullptr;
+    const cudaError_t e = cudaGetSymbolAddress(&p, g_prompt_err);
+    if (e != cudaSuccess) return e;
+    g_prompt_word[dev] = static_cast<int32_t *>(p);
+  }
+  *word = g_prompt_word[dev];
+  return cudaSuccess;
+}
+
+// reads an error word and clears it
+kvk_status take_error(int32_t *word, kvk_stream stream, int32_t *code) {
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+  int32_t h = 0;
+  cudaError_t e = cudaMemcpyAsync(&h, word, 4, cudaMemcpyDeviceToHost, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e == cudaSuccess) e = cudaMemsetAsync(word, 0, 4, st);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "reading the device error word");
+  *code = h;
+  if (h) return fail(KVK_ERR_DEVICE, "device error word 0x%x", h);
+  return KVK_OK;
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kNoWindow = 1 << 30;
 
@@ -416,16 +451,23 @@ kvk_status kvk_paged_set_give_up(kvk_paged *p, int32_t give_up) {
 
 kvk_status kvk_paged_get_device_error(kvk_paged *p, kvk_stream stream, int32_t *code) {
   if (!p || !code) return fail(KVK_ERR_INVALID_ARG, "null paged cache or output");
-  cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
-  int32_t h = 0;
-  cudaError_t e = cudaMemcpyAsync(&h, p->ws, 4, cudaMemcpyDeviceToHost, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e == cudaSuccess) e = cudaMemsetAsync(p->ws, 0, 4, st);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(st);
-  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "reading the device error word");
-  *code = h;
-  if (h) return fail(KVK_ERR_DEVICE, "device error word 0x%x", h);
+  return take_error(reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim).err), stream, code);
+}
+
+kvk_status kvk_prompt_set_give_up(int32_t give_up) {
+  if (give_up != 0 && give_up != 1) return fail(KVK_ERR_INVALID_ARG, "give_up must be 0 or 1");
+  g_prompt_give_up.store(give_up, std::memory_order_relaxed);
   return KVK_OK;
+}
+
+kvk_status kvk_prompt_get_device_error(kvk_stream stream, int32_t *code) {
+  if (!code) return fail(KVK_ERR_INVALID_ARG, "null output");
+  int dev = 0;
+  int32_t *word = nullptr;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = prompt_word(dev, &word);
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "looking up the prompts' error word");
+  return take_error(word, stream, code);
 }
 
 kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_rows *v, int32_t n_tokens,
@@ -450,8 +492,10 @@ kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&a.sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e == cudaSuccess && !error) e = prompt_word(dev, &error);
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "querying the device");
   a.device = dev;
+  a.give_up = g_prompt_give_up.load(std::memory_order_relaxed);
   a.pv.cu = cu_seqlens;
   a.pv.B = batch;
   a.pv.Hkv = n_kv_heads;

@@ -26,7 +26,7 @@ from . import _lib
 from ._lib import DTYPE_BF16, DTYPE_F16, DTYPE_F32, KVKError, PagedBatch, PagedDesc, Rows, check, load
 from .cache import _ptr, _stream
 
-__all__ = ["Rotary", "PagedCache", "prompt_attention", "KVKError"]
+__all__ = ["Rotary", "PagedCache", "prompt_attention", "prompt_error", "prompt_give_up", "KVKError"]
 
 _CODES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16}
 
@@ -315,7 +315,8 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     head_dim]``, ``k`` and ``v`` ``[tokens, H_kv, head_dim]`` (bf16 or fp16,
     post-RoPE), sequence ``b``'s tokens ``cu_seqlens[b]`` .. ``cu_seqlens[b + 1]
     - 1``; ``window``: a query sees that many positions at most (0: all).
-    ``error``: an int32 tensor of one element that gets device error bits.
+    ``error``: an int32 tensor of one element that gets device error bits
+    (without one, ``prompt_error`` tells).
     Returns ``[tokens, H_q, head_dim]``; rows in no sequence stay unwritten."""
     n, hq, d = _shape(q, "q")
     index, dtype = q.get_device(), q.dtype
@@ -330,3 +331,19 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
           _ints(cu_seqlens, "cu_seqlens", (B + 1,), index), B, scale, window, out.data_ptr(),
           0 if error is None else _ints(error, "error", (1,), index))
     return out
+
+
+def prompt_error(device=None, stream=None) -> int:
+    """Synchronise, read and clear the device error word of the prompts on
+    ``device`` (default: the current one) that were given no word (0 = none)."""
+    code = ctypes.c_int32()
+    with torch.cuda.device(device):
+        st = load().kvk_prompt_get_device_error(_stream(stream), ctypes.byref(code))
+    if st not in (0, 7):
+        check(st)
+    return code.value
+
+
+def prompt_give_up(give_up: bool):
+    """As ``PagedCache.set_give_up``, for all prompts."""
+    check(load().kvk_prompt_set_give_up(int(give_up)))

@@ -167,3 +167,8 @@ def test_binding_checks_shapes():
 
 def test_give_up_of_no_cache(lib):
     assert lib.load().kvk_paged_set_give_up(None, 0) == INVALID
+
+
+def test_prompt_errors_need_a_place_and_give_up_a_truth_value(lib):
+    assert lib.load().kvk_prompt_get_device_error(None, None) == INVALID
+    assert lib.load().kvk_prompt_set_give_up(2) == INVALID

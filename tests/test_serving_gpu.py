@@ -874,3 +874,43 @@ def test_attention_gives_up_and_recovers(news, lens, window, hq, hkv, d, dtype, 
         assert b.cache.device_error() == 8
         b.cache.set_give_up(False)
         assert torch.equal(keep[:n], b.attend(scale, window)[:n]) and b.cache.device_error() == 0
+
+
+@pytest.mark.parametrize("d,dtype", [(128, BF16), (64, F16)])
+def test_prompts_that_give_up_leave_a_sign(d, dtype):
+    """In the caller's word, or in the library's where the caller gives none."""
+    from paper_2609_37988_gb300.serving import prompt_attention, prompt_error, prompt_give_up
+    q, k, v = (randn(gen(78), (700, h, d), dtype) for h in (10, 2, 2))
+    cu, error = offsets([300, 1, 33, 366]), ints([0])
+    keep = prompt_attention(q, k, v, cu, 0.088)
+    assert prompt_error() == 0
+    try:
+        prompt_give_up(True)
+        prompt_attention(q, k, v, cu, 0.088)
+        assert prompt_error() == 8 and prompt_error() == 0
+        prompt_attention(q, k, v, cu, 0.088, error=error)
+        assert int(error) == 8 and prompt_error(q.device) == 0
+    finally:
+        prompt_give_up(False)
+    error.zero_()
+    assert torch.equal(keep, prompt_attention(q, k, v, cu, 0.088)) and prompt_error() == 0
+    assert torch.equal(keep, prompt_attention(q, k, v, cu, 0.088, error=error)) and int(error) == 0
+
+
+def test_prompts_whose_first_call_is_captured():
+    """The library's error word is looked up within the capture."""
+    import subprocess
+    import sys
+    program = """
+import torch
+from paper_2609_37988_gb300.serving import prompt_attention, prompt_error
+q, k, v = (torch.randn((200, h, 64), device="cuda").bfloat16() for h in (4, 2, 2))
+cu = torch.tensor([0, 150, 200], dtype=torch.int32, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    out = prompt_attention(q, k, v, cu, 0.125)
+graph.replay()
+assert prompt_error() == 0 and torch.equal(out, prompt_attention(q, k, v, cu, 0.125))
+"""
+    subprocess.run([sys.executable, "-c", program], check=True, timeout=120)
