@@ -914,3 +914,44 @@ graph.replay()
 assert prompt_error() == 0 and torch.equal(out, prompt_attention(q, k, v, cu, 0.125))
 """
     subprocess.run([sys.executable, "-c", program], check=True, timeout=120)
+
+
+def ragged_batch(count, most, longest, seed):
+    """News and lengths with empty sequences, short ones and, past the 32nd, long ones."""
+    rng = np.random.default_rng(seed)
+    news = [int(x) for x in rng.integers(0, most + 1, count)]
+    lens = [int(x) for x in rng.integers(0, 80, count)]
+    for b in list(rng.integers(0, count, 6)) + [count - 1]:
+        news[b], lens[b] = most, int(rng.integers(longest // 2, longest))
+    news[5] = news[31] = 0
+    return news, lens
+
+
+@pytest.mark.parametrize("count", [33, 64, 130])
+@pytest.mark.parametrize("most", [1, 3])
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 64, BF16, 16), (4, 4, 128, F16, 32)])
+def test_few_tokens_of_many_sequences_in_runs(count, most, hq, hkv, d, dtype, page):
+    """Over tables of more than 512 positions units are cut into equal runs, whose
+    starts are searched 32 sequences at a time."""
+    news, lens = ragged_batch(count, most, 900, 63)
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=63).fill()
+    assert b.table.shape[1] * page > 512
+    for window in (0, 100):
+        first = b.check(window)
+        for _ in range(3):
+            assert torch.equal(first[: sum(news)], b.attend(1.0 / math.sqrt(d), window)[: sum(news)])
+
+
+@pytest.mark.parametrize("count", [33, 64, 130])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(5, 1, 128, BF16), (8, 1, 64, F16)])
+def test_chunks_of_many_sequences_in_runs(count, hq, hkv, d, dtype):
+    """The same for chunks.  One block of tokens a sequence and one KV head are 33 to
+    130 jobs of 152 places; behind a table of 2^16 positions the idle ones weigh
+    0.14 x 512 tiles and more, and runs are taken."""
+    news, lens = ragged_batch(count, 20, 1500, 64)
+    page = 16
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=64, slack=2 ** 16 // page).fill()
+    for window in (0, 100):  # (a window bounds the tiles that a place can idle: whole jobs)
+        first = b.check(window)
+        for _ in range(3):
+            assert torch.equal(first[: sum(news)], b.attend(1.0 / math.sqrt(d), window)[: sum(news)])
