@@ -955,3 +955,55 @@ def test_chunks_of_many_sequences_in_runs(count, hq, hkv, d, dtype):
         first = b.check(window)
         for _ in range(3):
             assert torch.equal(first[: sum(news)], b.attend(1.0 / math.sqrt(d), window)[: sum(news)])
+
+
+@pytest.mark.parametrize("tokens", [5003, 9613])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rotary_many_tokens_a_block(tokens, dtype):
+    """Narrow rows of many tokens: 8 and 16 tokens of a block."""
+    rotary_case(dtype, 64, 64, 3, False, tokens, 8, 2, 4096, seed=65)
+    rotary_case(dtype, 64, 32, 1, True, tokens, 3, 1, 4096, seed=66, inplace=True)
+
+
+@pytest.mark.parametrize("tokens", [5003, 9613])
+@pytest.mark.parametrize("own", [True, False])
+def test_append_many_tokens_a_block(tokens, own):
+    """8 and 16 tokens of a block, sequences that begin and end inside one, a few
+    tokens in none."""
+    from paper_2609_37988_gb300.serving import Rotary
+    news = [3, 0, 1, 40, 2, 700, 5]
+    news.append(tokens - sum(news) - 4)
+    lens = [n + x for n, x in zip(news, [0, 9, 300, -5, 13, 77, 100, 1])]
+    hq, hkv, d, page = 8, 2, 64, 32
+    b = Batch(news, lens, hq, hkv, d, BF16, page, seed=67, rows_behind=4)
+    assert b.n == tokens
+    g = gen(68)
+    q, k, v = (randn(g, (tokens, h, d), BF16) for h in (hq, hkv, hkv))
+    axis = [0] * (d // 2) if own else [i % 3 for i in range(d // 2)]
+    rot = Rotary(head_dim=d, axes=axis)
+    inv_freq = [10000.0 ** (-2.0 * i / d) for i in range(d // 2)]
+    at = np.concatenate([[0], np.cumsum(news)])
+    place = np.concatenate([np.arange(l - n, l) for n, l in zip(news, lens)])
+    pos = torch.randint(0, 4096, (3, tokens), generator=g, dtype=torch.int32)
+    p = np.concatenate([place, np.zeros(4, np.int64)])[None] if own else pos.numpy()
+    q_out = torch.full((tokens, hq, d), 7.0, dtype=BF16, device="cuda")
+    b.cache.append(0, k, v, b.cu, b.lengths, b.table_d, rotary=rot, positions=None if own else pos.cuda(), q=q, q_out=q_out)
+    assert b.cache.device_error() == 0
+    m = sum(news)
+    ref = osv.rotary(f64(q), p, inv_freq, axis)
+    close(q_out[:m], ref[:m], rotary_bound(f64(q), ref, inv_freq, p, BF16, 1.0, False, d // 2)[:m])
+    assert (q_out[m:] == 7.0).all()
+    rk = osv.rotary(f64(k), p, inv_freq, axis)
+    tol = rotary_bound(f64(k), rk, inv_freq, p, BF16, 1.0, False, d // 2)
+    kp, vp = f64(b.cache.k_pages[0]), f64(b.cache.v_pages[0])
+    written = np.zeros(kp.shape[:1] + kp.shape[2:3], bool)
+    for s in range(len(news)):
+        t = place[at[s]:at[s + 1]]
+        rows = np.arange(at[s], at[s + 1])[t >= 0]
+        t = t[t >= 0]
+        pages, slots = b.table[s][t // page], t % page
+        close(kp[pages, :, slots], rk[rows], tol[rows])
+        np.testing.assert_array_equal(vp[pages, :, slots], f64(v)[rows])
+        written[pages, slots] = True
+    for pool in (kp, vp):  # nothing else was written
+        assert np.isnan(np.transpose(pool, (0, 2, 1, 3))[~written]).all()
