@@ -1007,3 +1007,25 @@ def test_append_many_tokens_a_block(tokens, own):
         written[pages, slots] = True
     for pool in (kp, vp):  # nothing else was written
         assert np.isnan(np.transpose(pool, (0, 2, 1, 3))[~written]).all()
+
+
+def test_lengths_of_sequences_without_new_tokens_do_not_matter_to_chunks():
+    b = Batch([40, 0, 25], [70, 40, 90], 8, 2, 64, BF16, 16, seed=69).fill()
+    keep = b.check()
+    for other in (10 ** 9, -5):
+        b.lengths.copy_(ints([70, other, 90]))
+        assert torch.equal(keep, b.attend(0.125)) and b.cache.device_error() == 0
+
+
+def test_prompt_offsets_out_of_order_give_each_sequence_its_own_rows():
+    """Offsets 0, 20, 10, 10^6, -3 of 50 tokens are clamped to sequences of tokens
+    0 .. 19, none, 10 .. 49 and none; 10 .. 19 belong to two and hold either's rows."""
+    from paper_2609_37988_gb300.serving import prompt_attention
+    d = 64
+    q, k, v = (randn(gen(28), (50, h, d), BF16) for h in (2, 1, 1))
+    out = torch.full((50, 2, d), 7.0, dtype=BF16, device="cuda")
+    prompt_attention(q, k, v, ints([0, 20, 10, 10 ** 6, -3]), 0.125, out=out)
+    for first, last, seen in ((0, 20, slice(0, 10)), (10, 50, slice(10, 40))):
+        r = osv.attend(f64(q[first:last]), *(np.transpose(f64(x[first:last]), (1, 0, 2)) for x in (k, v)), 0.125)
+        tol = osv.attend_bound(*r, d, last - first, U[BF16], 0.0)
+        close(out[first:last][seen], r[0][seen], tol[seen], f"tokens {first} to {last}")
