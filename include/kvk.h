@@ -593,11 +593,15 @@ kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_bat
  * max(0, p - window + 1) .. p (window 0: from 0), query head h reading KV head
  * h / (n_q_heads / n_kv_heads).  A query before position 0 sees nothing and
  * gives zeros.  q: post-RoPE, rows on 16 bytes; out: device
- * [n_tokens, n_q_heads, head_dim] of the cache's dtype, 16-byte aligned.
- * max_new: no sequence has more new tokens (n_tokens always serves; single
- * tokens run a form of their own).  A sequence that has more, or more positions
- * than its table holds, sets KVK_DEVERR_COUNT, and its outputs are unspecified;
- * a page outside the pool sets KVK_DEVERR_PAGE and reads as zeros.
+ * [n_tokens, n_q_heads, head_dim] of the cache's dtype, 16-byte aligned; it may
+ * be q itself, and may not overlap it otherwise.
+ * max_new: no sequence has more new tokens (n_tokens always serves).  Up to 16
+ * rows of a KV head (max_new times the query heads that read it) run a form of
+ * their own.  How the work is cut goes by the table's width, as the lengths are
+ * on the device: one that is no wider than the contexts serves short ones best.
+ * A sequence that has more new tokens, or more positions than its table holds,
+ * sets KVK_DEVERR_COUNT, and its outputs are unspecified; a page outside the pool
+ * sets KVK_DEVERR_PAGE and reads as zeros.
  * What the slots behind a sequence's last position hold does not matter, and a
  * key or value that a query does not see does not change its result, not even
  * one that is not finite.  An infinite value that it does see makes its channel
@@ -622,7 +626,7 @@ kvk_status kvk_paged_get_device_error(kvk_paged *cache, kvk_stream stream, int32
  * to its sequence's tokens max(0, i - window + 1) .. i (window 0: from 0).  q:
  * n_q_heads, k and v: n_kv_heads rows per token (post-RoPE, rows on 16 bytes);
  * out: device [n_tokens, n_q_heads, head_dim] of `dtype` (BF16 or F16),
- * 16-byte aligned.  Offsets out of order or range are clamped.  head_dim 64 or
+ * 16-byte aligned; it may be q itself.  Offsets out of order or range are clamped.  head_dim 64 or
  * 128, at most 64 query heads per KV head.  error: device int32 that gets
  * KVK_DEVERR bits; NULL: a word of the library's, one a device, which
  * kvk_prompt_get_device_error reads.  Non-finite keys and values as above.

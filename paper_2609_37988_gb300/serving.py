@@ -284,7 +284,9 @@ class PagedCache:
         """Causal attention of the new tokens' queries over the layer's pages
         (appended first); ``window``: a query sees that many positions at most
         (0: all).  ``max_new``: no sequence has more new tokens (default: all of
-        them); a tight one lets decode steps run the form for few tokens.
+        them); a tight one lets decode steps run the form for few tokens, and a
+        ``table`` no wider than the contexts the quickest cut of the work.
+        ``out`` may be ``q``.
         Returns ``[tokens, n_q_heads, head_dim]``; rows in no sequence stay
         unwritten."""
         n = q.shape[0]
@@ -315,7 +317,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     head_dim]``, ``k`` and ``v`` ``[tokens, H_kv, head_dim]`` (bf16 or fp16,
     post-RoPE), sequence ``b``'s tokens ``cu_seqlens[b]`` .. ``cu_seqlens[b + 1]
     - 1``; ``window``: a query sees that many positions at most (0: all).
-    ``error``: an int32 tensor of one element that gets device error bits
+    ``out`` may be ``q``.  ``error``: an int32 tensor of one element that gets device error bits
     (without one, ``prompt_error`` tells).
     Returns ``[tokens, H_q, head_dim]``; rows in no sequence stay unwritten."""
     n, hq, d = _shape(q, "q")

@@ -1029,3 +1029,53 @@ def test_prompt_offsets_out_of_order_give_each_sequence_its_own_rows():
         r = osv.attend(f64(q[first:last]), *(np.transpose(f64(x[first:last]), (1, 0, 2)) for x in (k, v)), 0.125)
         tol = osv.attend_bound(*r, d, last - first, U[BF16], 0.0)
         close(out[first:last][seen], r[0][seen], tol[seen], f"tokens {first} to {last}")
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1], [65001, 300]), ([2, 3], [64, 65536]), ([33], [65500]), ([1, 17, 0], [40001, 9, 70])])
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(4, 1, 128, BF16, 16), (6, 2, 64, F16, 64)])
+def test_contexts_of_65536_positions(news, lens, hq, hkv, d, dtype, page):
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=71).fill()
+    for window in (0, 5000):
+        b.check(window)
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1, 1], [300, 1, 512]), ([1], [512]), ([3, 0, 2], [70, 5, 2]), ([100], [100]), ([600], [600]),
+                                       ([64, 1, 30], [64, 400, 31])])
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(10, 2, 128, BF16, 16), (8, 2, 64, F16, 128)])
+def test_tables_much_wider_than_the_contexts(news, lens, hq, hkv, d, dtype, page):
+    """As a serving program keeps them: a table of 32768 positions, whatever is held.
+    Its unused entries lie far outside the pool."""
+    b = Batch(news, lens, hq, hkv, d, dtype, page, seed=72, slack=32768 // page).fill()
+    for window in (0, 50):
+        first = b.check(window)
+        assert torch.equal(first, b.attend(1.0 / math.sqrt(d), window))
+
+
+@pytest.mark.parametrize("news,lens", [([1, 1, 1], [300, 1, 400]), ([1, 2], [3000, 700]), ([70, 33], [70, 500]), ([24, 1, 0, 33], [4000, 10, 70, 1500])])
+def test_results_may_replace_the_queries(news, lens):
+    b = Batch(news, lens, 10, 2, 128, BF16, 16, seed=73).fill()
+    keep, q = b.attend(0.088), b.q.cuda()
+    assert b.attend(0.088, q=q, out=q) is q and torch.equal(q, keep)
+
+
+def test_prompt_results_may_replace_the_queries():
+    from paper_2609_37988_gb300.serving import prompt_attention
+    q, k, v = (randn(gen(74), (700, h, 128), BF16) for h in (10, 2, 2))
+    cu = offsets([300, 1, 33, 366])
+    keep = prompt_attention(q, k, v, cu, 0.088)
+    assert prompt_attention(q, k, v, cu, 0.088, out=q) is q and torch.equal(q, keep)
+
+
+@pytest.mark.parametrize("news,lens", [([1, 2, 1], [300, 1, 400]), ([1, 3], [3000, 700]), ([70, 33], [70, 500]), ([24, 1, 0, 33], [4000, 10, 70, 1500])])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_queries_that_are_not_finite_reach_only_their_own_rows(news, lens, bad):
+    b = Batch(news, lens, 10, 2, 128, BF16, 16, seed=79).fill()
+    keep = b.attend(0.088)
+    hit = [(0, 3), (sum(news) - 1, 0), (sum(news) // 2, 9)]
+    for token, head in hit:
+        b.q[token, head, 17] = bad
+    got = b.attend(0.088)
+    for token, head in hit:
+        assert torch.isnan(got[token, head]).all()
+        keep[token, head] = got[token, head] = 0
+    assert torch.equal(got, keep)
