@@ -72,6 +72,11 @@ def _shape(t: torch.Tensor, name: str):
     return shape
 
 
+def _int32(x: int) -> int:
+    """``x``, or the nearest number that an int32 holds (ctypes would drop bits)."""
+    return x if -2 ** 31 <= x < 2 ** 31 else 2 ** 31 - 1 if x > 0 else -2 ** 31
+
+
 def _call(index: int, stream, fn, *args):
     """The library's call on GPU ``index``, which it wants to be the current one."""
     if stream is not None and stream.device.index != index:
@@ -274,7 +279,7 @@ class PagedCache:
         if positions is not None and rotary is None:
             raise ValueError("positions without a rotary")
         pos = 0 if positions is None else rotary._positions(positions, n, index)
-        _call(index, stream, self._append, self.handle, layer, self._batch(n, cu, lengths, table), rk, rv,
+        _call(index, stream, self._append, self.handle, _int32(layer), self._batch(n, cu, lengths, table), rk, rv,
               rotary.handle if rotary is not None else None, pos, rq, ro)
         return q_out if q is not None else None
 
@@ -292,8 +297,8 @@ class PagedCache:
         n = q.shape[0]
         rq = _rows(q, "q", self.dtype, self._index, (n, self.n_q_heads, self.head_dim))
         out = _out_like(out, q, stream)
-        _call(self._index, stream, self._attend, self.handle, layer, self._batch(n, cu, lengths, table), rq, scale,
-              n if max_new is None else max_new, window, out.data_ptr())
+        _call(self._index, stream, self._attend, self.handle, _int32(layer), self._batch(n, cu, lengths, table), rq, scale,
+              n if max_new is None else _int32(max_new), _int32(window), out.data_ptr())
         return out
 
     def set_give_up(self, give_up: bool):
@@ -330,7 +335,7 @@ def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqle
     if B < 0:
         raise ValueError("cu_seqlens must be [sequences + 1]")
     _call(index, stream, load().kvk_prompt_attention, rq, rk, rv, n, hq, kv[1], d, _code(q),
-          _ints(cu_seqlens, "cu_seqlens", (B + 1,), index), B, scale, window, out.data_ptr(),
+          _ints(cu_seqlens, "cu_seqlens", (B + 1,), index), B, scale, _int32(window), out.data_ptr(),
           0 if error is None else _ints(error, "error", (1,), index))
     return out
 

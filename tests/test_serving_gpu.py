@@ -1079,3 +1079,27 @@ def test_queries_that_are_not_finite_reach_only_their_own_rows(news, lens, bad):
         assert torch.isnan(got[token, head]).all()
         keep[token, head] = got[token, head] = 0
     assert torch.equal(got, keep)
+
+
+@pytest.mark.parametrize("news,lens", [([1, 2], [300, 77]), ([40, 70], [200, 300])])
+def test_limits_past_32_bits_are_no_limits(news, lens):
+    from paper_2609_37988_gb300.serving import KVKError, prompt_attention
+    b = Batch(news, lens, 8, 2, 64, BF16, 16, seed=80).fill()
+    keep = b.attend(0.125)
+    for far in (2 ** 31 - 1, 2 ** 31, 2 ** 32 + 5, 2 ** 63 - 1):
+        assert torch.equal(keep, b.attend(0.125, window=far))
+        assert torch.equal(b.attend(0.125, max_new=b.n), b.attend(0.125, max_new=far))
+    q, k, v = (randn(gen(81), (90, h, 64), BF16) for h in (8, 2, 2))
+    own = prompt_attention(q, k, v, offsets([90]), 0.125)
+    assert torch.equal(own, prompt_attention(q, k, v, offsets([90]), 0.125, window=2 ** 32 + 5))
+    assert b.cache.device_error() == 0
+    for back in (-1, -2 ** 32):
+        with pytest.raises(KVKError):
+            b.attend(0.125, window=back)
+        with pytest.raises(KVKError):
+            prompt_attention(q, k, v, offsets([90]), 0.125, window=back)
+    for layer in (1, 2 ** 32):
+        with pytest.raises(KVKError):
+            b.cache.attend(layer, b.q.cuda(), b.cu, b.lengths, b.table_d, 0.125)
+        with pytest.raises(KVKError):
+            b.cache.append(layer, *(torch.zeros((b.n, 2, 64), dtype=BF16, device="cuda") for _ in range(2)), b.cu, b.lengths, b.table_d)
