@@ -570,7 +570,8 @@ kvk_status kvk_paged_plan(const kvk_paged_desc *desc, size_t *pool_bytes, size_t
 /* k_pages, v_pages: n_layers device pointers, 128-byte aligned; workspace:
  * device, 256-byte aligned.  The current device becomes the cache's; calls
  * with another current device are refused.  kvk_paged_reset clears the
- * workspace, and has to have run before the first attention. */
+ * workspace, and has to have run before the first attention (one that no
+ * reset was enqueued before is refused). */
 kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, void *workspace,
                             size_t ws_bytes, kvk_paged **out);
 kvk_status kvk_paged_destroy(kvk_paged *cache);

@@ -39,6 +39,7 @@ struct kvk_paged {
   uint8_t *ws;
   int device, sms, page_shift;
   std::atomic<int32_t> give_up{0};
+  std::atomic<bool> cleared{false};  // the workspace, by kvk_paged_reset
   std::mutex calls;  // an attention's launches follow one another
 };
 
@@ -360,6 +361,7 @@ kvk_status kvk_paged_reset(kvk_paged *p, kvk_stream stream) {
   const cudaError_t e =
       cudaMemsetAsync(p->ws, 0, paged_ws(p->d.head_dim).part, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "resetting the workspace");
+  p->cleared.store(true, std::memory_order_relaxed);
   return KVK_OK;
 }
 
@@ -405,6 +407,9 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   if (s) return s;
   if (!scale_ok(softmax_scale)) return fail(KVK_ERR_INVALID_ARG, "softmax scale must be finite and positive");
   if (window < 0) return fail(KVK_ERR_INVALID_ARG, "window must not be negative");
+  // (what an uncleared workspace holds would be taken for units to join)
+  if (!p->cleared.load(std::memory_order_relaxed))
+    return fail(KVK_ERR_INVALID_ARG, "kvk_paged_reset has to clear the workspace before the first attention");
   if (empty) return KVK_OK;
   if (max_new < 1) return fail(KVK_ERR_INVALID_ARG, "max_new must be positive");
   AttnArgs a = {};

@@ -1103,3 +1103,25 @@ def test_limits_past_32_bits_are_no_limits(news, lens):
             b.cache.attend(layer, b.q.cuda(), b.cu, b.lengths, b.table_d, 0.125)
         with pytest.raises(KVKError):
             b.cache.append(layer, *(torch.zeros((b.n, 2, 64), dtype=BF16, device="cuda") for _ in range(2)), b.cu, b.lengths, b.table_d)
+
+
+def test_attention_before_the_workspace_is_cleared_is_refused():
+    """Through the C ABI, whose caller owns the workspace and orders its clearing."""
+    import ctypes
+    from paper_2609_37988_gb300 import _lib
+    b = Batch([1, 2], [700, 300], 8, 2, 64, BF16, 16, seed=82).fill()
+    so, c = _lib.load(), b.cache
+    ws = torch.full_like(c.workspace, 0)  # as clear as a reset leaves it: the refusal is the host's
+    h, ptr = ctypes.c_void_p(), lambda t: ctypes.c_void_p(t.data_ptr())  # noqa: E731
+    pools = [(ctypes.c_void_p * 1)(t.data_ptr()) for t in (c.k_pages[0], c.v_pages[0])]
+    assert so.kvk_paged_create(ctypes.byref(c.desc), *pools, ptr(ws), ws.numel(), ctypes.byref(h)) == 0
+    q, out = b.q.cuda(), torch.zeros((3, 8, 64), dtype=BF16, device="cuda")
+    batch = _lib.PagedBatch(b.cu.data_ptr(), b.lengths.data_ptr(), b.table_d.data_ptr(), 2, b.table_d.shape[1], 3)
+    rows = _lib.Rows(q.data_ptr(), 8 * 64, 64)
+    call = lambda: so.kvk_paged_attention(h, 0, ctypes.byref(batch), ctypes.byref(rows), 0.125, 2, 0, ptr(out), None)  # noqa: E731
+    torch.cuda.synchronize()
+    assert call() == 1 and b"reset" in so.kvk_last_error()
+    assert so.kvk_paged_reset(h, None) == 0 and call() == 0
+    torch.cuda.synchronize()
+    assert torch.equal(out, b.attend(0.125))
+    assert so.kvk_paged_destroy(h) == 0
