@@ -627,10 +627,11 @@ kvk_status kvk_paged_get_device_error(kvk_paged *cache, kvk_stream stream, int32
  * to its sequence's tokens max(0, i - window + 1) .. i (window 0: from 0).  q:
  * n_q_heads, k and v: n_kv_heads rows per token (post-RoPE, rows on 16 bytes);
  * out: device [n_tokens, n_q_heads, head_dim] of `dtype` (BF16 or F16),
- * 16-byte aligned; it may be q itself.  Offsets out of order or range are clamped.  head_dim 64 or
- * 128, at most 64 query heads per KV head.  error: device int32 that gets
- * KVK_DEVERR bits; NULL: a word of the library's, one a device, which
- * kvk_prompt_get_device_error reads.  Non-finite keys and values as above.
+ * 16-byte aligned; it may be q itself, and may not overlap q, k or v otherwise.
+ * Offsets out of order or range are clamped.  head_dim 64 or 128, at most 64
+ * query heads per KV head.  error: device int32 that gets KVK_DEVERR bits; NULL:
+ * a word of the library's, one a device, which kvk_prompt_get_device_error reads.
+ * Non-finite keys and values as above.
  * Errors: INVALID_ARG, UNSUPPORTED. */
 kvk_status kvk_prompt_attention(const kvk_rows *q, const kvk_rows *k, const kvk_rows *v, int32_t n_tokens,
                                 int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
