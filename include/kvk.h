@@ -577,6 +577,28 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
 kvk_status kvk_paged_destroy(kvk_paged *cache);
 kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
 
+/* The same cache held in 8 bits: a pool's elements are e4m3 codes (a sign, 4 bits
+ * of exponent of bias 7, 3 of mantissa; 0x7f and 0xff: NaN), and for every page and
+ * KV head a power of two, [n_pages, n_kv_heads] of int8 for the keys and as many for
+ * the values: an element is code * 2^exponent.  Pools as above; exponents 4-byte
+ * aligned.  `dtype` is what queries, new keys and values and results are; exponents
+ * lie in [-110, 119] (BF16) or [-15, 7] (F16; others read as the nearest of these),
+ * so that every element is a number of the dtype and attention is that over the
+ * dtype's own pages, with weights in f16 either way.  The handle serves every
+ * kvk_paged_ call.
+ *
+ * An append sets a page and head's exponent to the least that holds the largest
+ * finite magnitude among its new numbers, max |x| <= 448 * 2^exponent, and the codes
+ * to the nearest of x * 2^-exponent (ties to even; at most 448 in magnitude, which
+ * cuts BF16 off at 2.98e38 and F16 at 57344).  Where positions of the page were held
+ * before the call's first, the exponent does not fall; where it rises, their codes
+ * are rounded again, to the nearest of code * 2^(old - new).  Numbers that are not
+ * finite are held as NaN.  No two sequences of an append may write to one page. */
+kvk_status kvk_paged_coded_plan(const kvk_paged_desc *desc, size_t *pool_bytes, size_t *exp_bytes, size_t *ws_bytes);
+kvk_status kvk_paged_coded_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages,
+                                  int8_t *const *k_exps, int8_t *const *v_exps, void *workspace, size_t ws_bytes,
+                                  kvk_paged **out);
+
 /* Writes the new tokens' keys and values into `layer`'s pages.  With a rotary
  * the keys are rotated on the way, and with q its queries are rotated to q_out
  * (which may be q) in the same pass; positions (device int32
@@ -612,6 +634,52 @@ kvk_status kvk_paged_append(kvk_paged *cache, int32_t layer, const kvk_paged_bat
  * make them at the same time. */
 kvk_status kvk_paged_attention(kvk_paged *cache, int32_t layer, const kvk_paged_batch *batch, const kvk_rows *q,
                                float softmax_scale, int32_t max_new, int32_t window, void *out, kvk_stream stream);
+/* ---- operators on pages ------------------------------------------------------
+ * refs [n_pages] (device int32) counts a page's holders: rows of the caller's
+ * tables, or whoever else keeps one.  A page that is counted 0 times is free.  The
+ * calls read the counts, the table and the lengths when they run; what they choose
+ * goes by the counts before the call and by the order of pages and rows alone.
+ * Pages are copied with the exponents of a cache in 8 bits, in all layers.  The calls
+ * use the object's workspace: ordered on the GPU as attentions are.
+ * A page of a row outside the pool sets KVK_DEVERR_PAGE and is not counted; a length
+ * that the table does not hold, or a page of a row that is counted 0 times, sets
+ * KVK_DEVERR_COUNT (the length is cut, the counts are then unspecified).
+ * Errors: INVALID_ARG. */
+
+/* Page src[i] (device int32, n of them) is copied to page dst[i].  An entry of -1 on
+ * either side copies nothing; another that is no page sets KVK_DEVERR_PAGE.  No page
+ * may be written twice, or be both read and written. */
+kvk_status kvk_paged_copy(kvk_paged *cache, const int32_t *src, const int32_t *dst, int32_t n, kvk_stream stream);
+
+/* The `batch` rows of table [batch, max_pages], lengths[b] positions each, give way
+ * to `rows` rows of table_out [rows, max_pages_out]: row i goes on from row
+ * parents[i] (-1: from nothing) and has room for after[i] positions (after NULL: as
+ * many as its parent holds).  It keeps its parent's pages up to the smaller of the
+ * two lengths, and gets free pages, the lowest first, rows in order, up to after[i].
+ * A kept page that is not full by then is one that the row will write to: it stays
+ * the row's own if its count is 1 and, of the rows that keep it, this is the first
+ * and none has it full; else the row gets a copy, on a free page of its own.  So
+ * beams fork and are reordered, sequences grow, are taken back to fewer positions,
+ * end (in no parents) and begin.
+ * refs_out [n_pages] (it may be refs): the counts, less the given rows' pages, more
+ * the new rows'.  What this frees is handed out by the next call.  Entries behind a
+ * row's pages are -1, as are those that no free page was left for, which sets
+ * KVK_DEVERR_CAPACITY.  A parent that is no row (taken for -1), a negative length or
+ * one past max_pages_out (cut) sets KVK_DEVERR_COUNT.  table_out may not overlap
+ * table.  rows: at most 16384; with 0 all pages of the given rows are let go of. */
+kvk_status kvk_paged_fork(kvk_paged *cache, const int32_t *refs, const int32_t *table, const int32_t *lengths,
+                          int32_t batch, int32_t max_pages, const int32_t *parents, const int32_t *after, int32_t rows,
+                          int32_t *refs_out, int32_t *table_out, int32_t max_pages_out, kvk_stream stream);
+
+/* Moves the used pages to the beginning of the pools: with U of them, the k-th used
+ * page from number U on goes to the k-th free one before it.  where [n_pages]: each
+ * page's new number, -1 for one that was free; table_out [batch, max_pages] (it may be
+ * table): the rows' new numbers, -1 behind their pages; refs_out (it may be refs): the
+ * counts; used (one int32, or NULL): U.  What stands behind U is free. */
+kvk_status kvk_paged_compact(kvk_paged *cache, const int32_t *refs, const int32_t *table, const int32_t *lengths,
+                             int32_t batch, int32_t max_pages, int32_t *refs_out, int32_t *table_out, int32_t *where,
+                             int32_t *used, kvk_stream stream);
+
 /* Waits of an attention are bounded (2^20 polls).  One that gives up ends its
  * CTA's others, sets KVK_DEVERR_TIMEOUT and leaves the call's outputs unspecified;
  * what is in flight lands first, and later calls are unaffected.  give_up 1: the

@@ -107,10 +107,16 @@ _SIGS = {
     "kvk_paged_plan": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)],
     "kvk_paged_create": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_P), ctypes.POINTER(_P), _P, _SZ,
                          ctypes.POINTER(_P)],
+    "kvk_paged_coded_plan": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_SZ), ctypes.POINTER(_SZ), ctypes.POINTER(_SZ)],
+    "kvk_paged_coded_create": [ctypes.POINTER(PagedDesc), ctypes.POINTER(_P), ctypes.POINTER(_P), ctypes.POINTER(_P),
+                               ctypes.POINTER(_P), _P, _SZ, ctypes.POINTER(_P)],
     "kvk_paged_destroy": [_P],
     "kvk_paged_reset": [_P, _P],
     "kvk_paged_append": [_P, _I, _PB, _R, _R, _P, _P, _R, _R, _P],
     "kvk_paged_attention": [_P, _I, _PB, _R, _F, _I, _I, _P, _P],
+    "kvk_paged_copy": [_P, _P, _P, _I, _P],
+    "kvk_paged_fork": [_P, _P, _P, _P, _I, _I, _P, _P, _I, _P, _P, _I, _P],
+    "kvk_paged_compact": [_P, _P, _P, _P, _I, _I, _P, _P, _P, _P, _P],
     "kvk_paged_set_give_up": [_P, _I],
     "kvk_paged_get_device_error": [_P, _P, ctypes.POINTER(_I)],
     "kvk_prompt_attention": [_R, _R, _R, _I, _I, _I, _I, _I, _P, _I, _F, _I, _P, _P, _P],

@@ -1,0 +1,391 @@
+// pages.cu -- copying, forking and compacting the pages of a paged cache.
+//
+// A page's holders are counted on the device (refs); one that nobody holds is free.
+// All choices go by the counts as they were before the call and by the order of
+// pages and rows, so that they do not depend on how the GPU runs them.
+//
+// Bound: the pages that are copied (HBM, read and written once), for calls that
+// copy few the launches.
+#include <algorithm>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "serve.h"
+
+namespace kvk {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPer = kPageChunk / kThreads;
+constexpr int kErrCapacity = 2, kErrCount = 4, kErrPage = 32;  // KVK_DEVERR_*
+constexpr uint32_t kAll = 0xffffffffu;
+
+// Sum of x over the CTA's threads before this one; `total`: over all of them.
+// Every thread calls it.
+__device__ int scan_cta(int x, int &total) {
+  __shared__ int s_sum[kThreads / 32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int sum = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(kAll, sum, o);
+    if (lane >= o) sum += y;
+  }
+  __syncthreads();  // the last call's readers are through
+  if (lane == 31) s_sum[warp] = sum;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kThreads / 32; ++w) {
+    before += w < warp ? s_sum[w] : 0;
+    total += s_sum[w];
+  }
+  return before + sum - x;
+}
+
+__device__ __forceinline__ int pages_of(const PagesArgs &a, int len) {
+  return (int)(((int64_t)len + (1 << a.page_shift) - 1) >> a.page_shift);
+}
+// Positions of a given row, within its table.
+__device__ __forceinline__ int held(const PagesArgs &a, int b) {
+  return (int)min((int64_t)max(a.lens[b], 0), (int64_t)a.max_pages << a.page_shift);
+}
+
+// This thread's pages of chunk c and how many of them are used; the chunk's holders
+// are kept as they are before the call (refs_out may be refs).
+__device__ int count_chunk(const PagesArgs &a, int c, int32_t *keep) {
+  int used = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int p = c * kPageChunk + i * kThreads + threadIdx.x;
+    if (p >= a.n_pages) continue;
+    const int r = a.refs[p];
+    used += r > 0;
+    a.before[p] = r;
+    if (keep) keep[p] = r;
+  }
+  return used;
+}
+
+// Row i of a fork from its parent's: what it keeps of it, ends with.
+__device__ void fork_row(const PagesArgs &a, int j, int &parent, int &old, int &want, bool &open) {
+  parent = a.parents[j];
+  if (parent < -1 || parent >= a.B) parent = -1;
+  const int len = parent < 0 ? 0 : held(a, parent);
+  const int64_t cap = (int64_t)a.width << a.page_shift;
+  const int after = (int)min((int64_t)(a.after ? max(a.after[j], 0) : len), cap);
+  const int kept = min(len, after);
+  old = pages_of(a, kept);
+  want = pages_of(a, after);
+  open = (kept & ((1 << a.page_shift) - 1)) != 0;
+}
+
+// Pages counted, a CTA per chunk; then rows, a warp each.
+__global__ void __launch_bounds__(kThreads) fork_count_kernel(const PagesArgs a, int chunks) {
+  const int lane = threadIdx.x & 31;
+  pdl_wait();
+  if ((int)blockIdx.x < chunks) {
+    int total;
+    scan_cta(count_chunk(a, blockIdx.x, a.refs_out), total);
+    if (threadIdx.x == 0)
+      a.chunk[blockIdx.x] = min(kPageChunk, a.n_pages - (int)blockIdx.x * kPageChunk) - total;  // free
+    pdl_trigger();
+    return;
+  }
+  const int i = ((int)blockIdx.x - chunks) * (kThreads / 32) + (threadIdx.x >> 5);
+  if (i < a.R) {
+    ForkRow r;
+    bool open;
+    fork_row(a, i, r.parent, r.old, r.want, open);
+    r.copy = -1;
+    if (open) {
+      // A page that is not full will be written to: it stays with the first row that
+      // has it so if nobody else holds it and no row has it full.
+      bool shared = false;
+      for (int j = lane; j < a.R; j += 32) {
+        int p, o, w;
+        bool op;
+        if (j == i) continue;
+        fork_row(a, j, p, o, w, op);
+        if (p == r.parent) shared = shared || o > r.old || (o == r.old && (!op || j < i));
+      }
+      shared = __any_sync(kAll, shared);
+      const int page = a.table[(int64_t)r.parent * a.max_pages + r.old - 1];
+      if ((unsigned)page < (unsigned)a.n_pages && (shared || a.refs[page] != 1)) r.copy = page;
+    }
+    if (lane == 0) {
+      a.rows[i] = r;
+      const int parent = a.parents[i];
+      const int64_t cap = (int64_t)a.width << a.page_shift;
+      const int64_t after = a.after ? a.after[i] : r.parent < 0 ? 0 : held(a, r.parent);
+      if (parent < -1 || parent >= a.B || after < 0 || after > cap) set_err(a.err, kErrCount);
+    }
+  }
+  pdl_trigger();
+}
+
+// A CTA per row: the given one lets go of its pages, the new one takes its own.
+__global__ void __launch_bounds__(kThreads) fork_rows_kernel(const PagesArgs a) {
+  __shared__ int s_chunk, s_before;
+  const int tid = threadIdx.x, lane = tid & 31, r = blockIdx.x;
+  pdl_wait();
+  if (r < a.B) {
+    const int n = pages_of(a, held(a, r));
+    if (tid == 0 && (int64_t)a.lens[r] > (int64_t)a.max_pages << a.page_shift) set_err(a.err, kErrCount);
+    for (int j = tid; j < n; j += kThreads) {
+      const int page = a.table[(int64_t)r * a.max_pages + j];
+      if ((unsigned)page >= (unsigned)a.n_pages) {
+        set_err(a.err, kErrPage);
+      } else if (a.before[page] <= 0) {
+        set_err(a.err, kErrCount);
+      } else {
+        atomicSub(&a.refs_out[page], 1);
+      }
+    }
+  }
+  if (r < a.R) {
+    const ForkRow row = a.rows[r];
+    const int copied = row.copy >= 0, fresh_from = row.old - copied, need = row.want - fresh_from;
+    int32_t *out = a.table_out + (int64_t)r * a.width;
+    for (int j = tid; j < a.width; j += kThreads) {
+      if (j < fresh_from) {
+        const int page = a.table[(int64_t)row.parent * a.max_pages + j];
+        if ((unsigned)page < (unsigned)a.n_pages) atomicAdd(&a.refs_out[page], 1);
+        out[j] = page;
+      } else if (j >= row.want) {
+        out[j] = -1;
+      }
+    }
+    if (tid == 0) {
+      a.src[r] = row.copy;
+      a.dst[r] = -1;
+    }
+    if (need > 0) {  // (the same for the CTA)
+      // free pages that the rows before take
+      int mine = 0, base;
+      for (int j = tid; j < r; j += kThreads) {
+        const ForkRow x = a.rows[j];
+        mine += x.want - x.old + (x.copy >= 0);
+      }
+      scan_cta(mine, base);
+      // the chunk with free page number `base`
+      const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
+      if (tid < 32) {
+        int before = 0, c0 = 0;
+        for (; c0 < chunks; c0 += 32) {
+          const int x = c0 + lane < chunks ? a.chunk[c0 + lane] : 0;
+          int sum = x;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const int y = __shfl_up_sync(kAll, sum, o);
+            if (lane >= o) sum += y;
+          }
+          const uint32_t past = __ballot_sync(kAll, before + sum > base);
+          if (past) {
+            const int f = __ffs(past) - 1;
+            before += __shfl_sync(kAll, sum - x, f);
+            c0 += f;
+            break;
+          }
+          before += __shfl_sync(kAll, sum, 31);
+        }
+        if (lane == 0) s_chunk = c0, s_before = before;
+      }
+      __syncthreads();
+      int c = s_chunk, before = s_before;
+      for (; c < chunks && before < base + need; ++c) {
+        bool is_free[kPer];
+        int n = 0, total;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          const int p = c * kPageChunk + kPer * tid + i;
+          is_free[i] = p < a.n_pages && a.before[p] <= 0;
+          n += is_free[i];
+        }
+        int k = before + scan_cta(n, total) - base;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (!is_free[i]) continue;
+          if (k >= 0 && k < need) {
+            const int p = c * kPageChunk + kPer * tid + i;
+            out[fresh_from + k] = p;
+            a.refs_out[p] = 1;
+            if (copied && k == 0) a.dst[r] = p;
+          }
+          ++k;
+        }
+        before += total;
+      }
+      // those that no page is left for
+      const int got = min(max(before - base, 0), need);
+      for (int j = fresh_from + got + tid; j < row.want; j += kThreads) out[j] = -1;
+      if (got < need && tid == 0) set_err(a.err, kErrCapacity);
+    }
+  }
+  pdl_trigger();
+}
+
+__global__ void __launch_bounds__(kThreads) compact_count_kernel(const PagesArgs a) {
+  int total;
+  pdl_wait();
+  scan_cta(count_chunk(a, blockIdx.x, nullptr), total);
+  if (threadIdx.x == 0) a.chunk[blockIdx.x] = total;
+  pdl_trigger();
+}
+
+// Which page goes where: used page number k at or behind the used count to free
+// page number k before it.
+__global__ void __launch_bounds__(kThreads) compact_moves_kernel(const PagesArgs a) {
+  const int tid = threadIdx.x, c = blockIdx.x, chunks = gridDim.x;
+  int mine = 0, all = 0, before, used, low_before, x;
+  pdl_wait();
+  for (int i = tid; i < chunks; i += kThreads) {
+    const int n = a.chunk[i];
+    all += n;
+    if (i < c) mine += n;
+  }
+  scan_cta(mine, before);
+  scan_cta(all, used);
+  // used pages before number `used`
+  const int edge = used / kPageChunk;
+  int low = 0;
+  for (int i = tid; i < edge; i += kThreads) low += a.chunk[i];
+  for (int p = edge * kPageChunk + tid; p < used; p += kThreads) low += a.before[p] > 0;
+  scan_cta(low, low_before);
+  bool in[kPer];
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int p = c * kPageChunk + kPer * tid + i;
+    in[i] = p < a.n_pages && a.before[p] > 0;
+    n += in[i];
+  }
+  int k = before + scan_cta(n, x);  // used pages before this one
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int p = c * kPageChunk + kPer * tid + i;
+    if (p >= a.n_pages) break;
+    if (p < used) {
+      a.where[p] = in[i] ? p : -1;
+      if (in[i])
+        a.refs_out[p] = a.before[p];
+      else
+        a.dst[p - k] = p;
+    } else {
+      a.refs_out[p] = 0;
+      if (in[i])
+        a.src[k - low_before] = p;
+      else
+        a.where[p] = -1;
+    }
+    k += in[i];
+  }
+  if (c == 0 && tid == 0) {
+    *a.n_moved = used - low_before;
+    if (a.used) *a.used = used;
+  }
+  pdl_trigger();
+}
+
+// The moved pages' numbers and holders, the table.
+__global__ void __launch_bounds__(kThreads) compact_apply_kernel(const PagesArgs a) {
+  pdl_wait();
+  const int n = *a.n_moved;
+  const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i = at; i < n; i += step) {
+    const int s = a.src[i], d = a.dst[i];
+    a.where[s] = d;
+    a.refs_out[d] = a.before[s];
+  }
+  for (int64_t e = at; e < (int64_t)a.B * a.width; e += step) {
+    const int b = (int)(e / a.width), j = (int)(e - (int64_t)b * a.width);
+    int to = -1;
+    if (j == 0 && (int64_t)a.lens[b] > (int64_t)a.max_pages << a.page_shift) set_err(a.err, kErrCount);
+    if (j < pages_of(a, held(a, b))) {
+      const int page = a.table[(int64_t)b * a.max_pages + j];
+      if ((unsigned)page >= (unsigned)a.n_pages) {
+        set_err(a.err, kErrPage);
+      } else if (a.before[page] <= 0) {
+        set_err(a.err, kErrCount);
+      } else {
+        // a page that moves stands in the list, which is in order
+        int lo = 0, hi = n;
+        while (lo < hi) {
+          const int mid = (lo + hi) >> 1;
+          if (a.src[mid] < page)
+            lo = mid + 1;
+          else
+            hi = mid;
+        }
+        to = lo < n && a.src[lo] == page ? a.dst[lo] : page;
+      }
+    }
+    a.table_out[e] = to;
+  }
+  pdl_trigger();
+}
+
+constexpr int kPiece = 8192;  // bytes
+
+// Pieces of pages: a CTA copies 32 bytes a thread at a time.
+template <bool CODED>
+__global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
+  const int tid = threadIdx.x;
+  pdl_wait();
+  const int n = a.n_dev ? *a.n_dev : a.n;
+  const int pieces = (int)((a.bytes + kPiece - 1) / kPiece), pools = 2 * a.layers;
+  const int64_t per = (int64_t)pools * pieces, total = per * n;
+  for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
+    const int i = (int)(w / per), rest = (int)(w - i * per), pool = rest / pieces, piece = rest - pool * pieces;
+    const int s = a.src[i], d = a.dst[i];
+    if (s == -1 || d == -1) continue;
+    if ((unsigned)s >= (unsigned)a.n_pages || (unsigned)d >= (unsigned)a.n_pages) {
+      if (tid == 0) set_err(a.err, kErrPage);
+      continue;
+    }
+    if (s == d) continue;
+    const int l = pool >> 1;
+    uint8_t *x = pool & 1 ? a.v[l] : a.k[l];
+    const int64_t off = (int64_t)piece * kPiece + 32 * tid;
+    if (off < a.bytes) {
+      const uint4 *from = reinterpret_cast<const uint4 *>(x + s * a.bytes + off);
+      const uint4 u = from[0], v = from[1];
+      st_sector(x + d * a.bytes + off, u, v);
+    }
+    if (CODED && piece == 0) {
+      int8_t *e = pool & 1 ? a.ve[l] : a.ke[l];
+      for (int h = tid; h < a.Hkv; h += kThreads) e[(int64_t)d * a.Hkv + h] = e[(int64_t)s * a.Hkv + h];
+    }
+  }
+  pdl_trigger();
+}
+
+}  // namespace
+
+cudaError_t launch_copy_pages(const CopyArgs &a, bool coded, int sms, cudaStream_t st) {
+  const int64_t pieces = (a.bytes + kPiece - 1) / kPiece * 2 * a.layers * a.n;
+  if (pieces == 0) return cudaSuccess;
+  const dim3 grid((unsigned)std::min<int64_t>(pieces, (int64_t)8 * sms));
+  return launch_pdl(coded ? copy_pages_kernel<true> : copy_pages_kernel<false>, grid, dim3(kThreads), 0, st, a);
+}
+
+cudaError_t launch_fork(const PagesArgs &a, cudaStream_t st) {
+  const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
+  cudaError_t e = launch_pdl(fork_count_kernel, dim3(chunks + (a.R + kThreads / 32 - 1) / (kThreads / 32)), dim3(kThreads), 0, st, a,
+                             chunks);
+  if (e != cudaSuccess || std::max(a.B, a.R) == 0) return e;
+  return launch_pdl(fork_rows_kernel, dim3(std::max(a.B, a.R)), dim3(kThreads), 0, st, a);
+}
+
+cudaError_t launch_compact(const PagesArgs &a, cudaStream_t st) {
+  const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
+  cudaError_t e = launch_pdl(compact_count_kernel, dim3(chunks), dim3(kThreads), 0, st, a);
+  if (e == cudaSuccess) e = launch_pdl(compact_moves_kernel, dim3(chunks), dim3(kThreads), 0, st, a);
+  if (e != cudaSuccess) return e;
+  const int64_t work = std::max<int64_t>((int64_t)a.B * a.width, a.n_pages / 2);
+  return launch_pdl(compact_apply_kernel, dim3((unsigned)std::min<int64_t>((work + kThreads - 1) / kThreads, 1024)), dim3(kThreads), 0,
+                    st, a);
+}
+
+}  // namespace kvk

@@ -38,6 +38,10 @@ struct PagedView {
   const int32_t *table;   // [B, max_pages]
   int B, max_pages, n_pages, page_shift, Hkv, D, n_tokens;
   int32_t *err;
+  // a cache in 8 bits: k and v hold e4m3 codes, of these powers of two (log2) of a
+  // page and KV head, [n_pages, Hkv], within [e_lo, e_hi]; null: values of the dtype
+  int8_t *ke, *ve;
+  int e_lo, e_hi;
 };
 
 struct RotArgs {
@@ -48,6 +52,17 @@ struct RotArgs {
   PagedView pv;
 };
 cudaError_t launch_rotary(const RotArgs &a, int dtype, cudaStream_t st);
+
+// New keys and values into the pages of a cache in 8 bits; keys rotated on the way
+// where `rotate` is set.
+struct CodeArgs {
+  RotTable t;
+  Rows k, v;
+  const int32_t *pos;     // [n_axes, n_tokens]; null: positions in the sequence
+  int rotate, wide;       // wide: rows start on 16 bytes
+  PagedView pv;
+};
+cudaError_t launch_append_codes(const CodeArgs &a, int dtype, cudaStream_t st);
 
 // Units of the few-token form whose tiles lie in several CTAs' runs.
 constexpr int kRowsMaxCtas = 320;
@@ -96,6 +111,46 @@ struct AttnArgs {
 cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads);
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
 cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st);
+cudaError_t launch_attn_codes(const AttnArgs &a, int dtype, cudaStream_t st);
+
+// ---- operators on pages -------------------------------------------------------
+constexpr int kForkRows = 16384;   // rows that a fork may leave
+constexpr int kPageChunk = 1024;   // pages that a CTA counts
+constexpr int kCopyLayers = 96;    // of one launch of the copy
+
+// A row that a fork leaves, from its parent's.
+struct ForkRow {
+  int32_t parent, old, want;  // pages that it keeps (its last may be a copy) and has
+  int32_t copy;               // page to copy, or -1
+};
+struct PagesArgs {
+  const int32_t *refs;        // [n_pages] holders
+  int32_t *refs_out;
+  const int32_t *table, *lens;  // [B, max_pages], [B]
+  const int32_t *parents, *after;  // fork: [R]
+  int32_t *table_out;         // [R (fork) or B, width]
+  int32_t *where, *used;      // compact: a page's new number; pages used
+  int B, R, max_pages, width, n_pages, page_shift;
+  int32_t *err;
+  // workspace: holders before the call, pages counted per chunk, rows, pages to copy
+  int32_t *before, *chunk;
+  ForkRow *rows;
+  int32_t *src, *dst, *n_moved;
+};
+struct CopyArgs {
+  uint8_t *k[kCopyLayers], *v[kCopyLayers];
+  int8_t *ke[kCopyLayers], *ve[kCopyLayers];
+  const int32_t *src, *dst;
+  const int32_t *n_dev;       // entries, where the device knows them
+  int n, layers, n_pages, Hkv;
+  int64_t bytes;              // of a page of a pool
+  int32_t *err;
+};
+cudaError_t launch_fork(const PagesArgs &a, cudaStream_t st);
+cudaError_t launch_compact(const PagesArgs &a, cudaStream_t st);
+// up to kCopyLayers layers; coded: their powers too
+cudaError_t launch_copy_pages(const CopyArgs &a, bool coded, int sms, cudaStream_t st);
+
 // CTAs that a split launch may use at most, and the partial slots of each
 constexpr int kRowsPerUnit = 16, kRowsMaxHeads = 4;
 // KV heads of a unit: as many as make a copy 64 rows of one page

@@ -34,7 +34,9 @@ struct PageMap {
 
 struct kvk_paged {
   kvk_paged_desc d;
+  bool coded = false;             // a cache in 8 bits
   std::vector<uint8_t *> k, v;
+  std::vector<int8_t *> ke, ve;   // its powers of two
   std::vector<PageMap> maps;  // kMaps tensor maps of a layer's pools, as AttnArgs has them
   uint8_t *ws;
   int device, sms, page_shift;
@@ -89,9 +91,17 @@ kvk_status check_heads(int Hq, int Hkv, int D, int dtype) {
 }
 
 struct PagedWs {
-  size_t err, list, tc_list, part, total;
+  size_t err, list, tc_list, part, pages, total;
 };
-PagedWs paged_ws(int D) {
+constexpr size_t kWsAlign = 256;
+size_t up(size_t x) { return (x + kWsAlign - 1) / kWsAlign * kWsAlign; }
+// what the operators on pages keep: holders, chunks' counts, rows, two lists
+size_t chunks_of(int n_pages) { return ((size_t)n_pages + kPageChunk - 1) / kPageChunk; }
+size_t list_of(int n_pages) { return (size_t)n_pages / 2 + 1 > (size_t)kForkRows ? (size_t)n_pages / 2 + 1 : (size_t)kForkRows; }
+size_t pages_ws(int n_pages) {
+  return up(4 * (size_t)n_pages) + up(4 * chunks_of(n_pages)) + up(sizeof(ForkRow) * kForkRows) + 2 * up(4 * list_of(n_pages)) + kWsAlign;
+}
+PagedWs paged_ws(int D, int n_pages) {
   PagedWs w;
   w.err = 0;
   w.list = 256;
@@ -99,7 +109,8 @@ PagedWs paged_ws(int D) {
   w.part = w.tc_list + ((sizeof(TcList) + 255) & ~(size_t)255);
   // two pieces per CTA of either form
   const size_t rows = (size_t)2 * kRowsMaxCtas * kRowsMaxHeads * rows_part(D), tc = (size_t)2 * kTcMaxCtas * 2 * 128 * (D + 2);
-  w.total = w.part + (rows > tc ? rows : tc) * sizeof(float);
+  w.pages = up(w.part + (rows > tc ? rows : tc) * sizeof(float));
+  w.total = w.pages + pages_ws(n_pages);
   return w;
 }
 
@@ -111,19 +122,29 @@ kvk_status check_paged_desc(const kvk_paged_desc *d) {
   return check_heads(d->n_q_heads, d->n_kv_heads, d->head_dim, d->dtype);
 }
 
-size_t pool_bytes(const kvk_paged_desc *d) {
-  return (size_t)d->n_pages * d->n_kv_heads * d->page_size * d->head_dim * 2;
+size_t pool_bytes(const kvk_paged_desc *d, bool coded) {
+  return (size_t)d->n_pages * d->n_kv_heads * d->page_size * d->head_dim * (coded ? 1 : 2);
+}
+// powers of two that a cache in 8 bits uses: 2^e times any e4m3 code is a number of
+// the dtype (f16: its subnormals' step is 2^-24; bf16: a margin to its ends)
+int exp_lo(int dtype) { return dtype == KVK_DTYPE_BF16 ? -110 : -15; }
+int exp_hi(int dtype) { return dtype == KVK_DTYPE_BF16 ? 119 : 7; }
+
+kvk_status check_device(const kvk_paged *p) {
+  int dev = -1;
+  const cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "querying the current device");
+  if (dev != p->device)
+    return fail(KVK_ERR_INVALID_ARG, "current device %d is not the paged cache's device %d", dev, p->device);
+  return KVK_OK;
 }
 
 kvk_status check_call(const kvk_paged *p, int layer, const kvk_paged_batch *b, bool &empty) {
   if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
   if (layer < 0 || layer >= p->d.n_layers)
     return fail(KVK_ERR_INVALID_ARG, "layer %d out of range [0, %d)", layer, p->d.n_layers);
-  int dev = -1;
-  const cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "querying the current device");
-  if (dev != p->device)
-    return fail(KVK_ERR_INVALID_ARG, "current device %d is not the paged cache's device %d", dev, p->device);
+  const kvk_status dev = check_device(p);
+  if (dev) return dev;
   if (!b) return fail(KVK_ERR_INVALID_ARG, "null batch");
   if (b->batch < 0 || b->n_tokens < 0 || b->max_pages < 0)
     return fail(KVK_ERR_INVALID_ARG, "batch, n_tokens and max_pages must not be negative");
@@ -153,8 +174,74 @@ PagedView view_of(const kvk_paged *p, int layer, const kvk_paged_batch *b) {
   v.Hkv = p->d.n_kv_heads;
   v.D = p->d.head_dim;
   v.n_tokens = b->n_tokens;
-  v.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(v.D).err);
+  v.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(v.D, p->d.n_pages).err);
+  v.ke = p->coded ? p->ke[layer] : nullptr;
+  v.ve = p->coded ? p->ve[layer] : nullptr;
+  v.e_lo = exp_lo(p->d.dtype);
+  v.e_hi = exp_hi(p->d.dtype);
   return v;
+}
+
+// The workspace of the operators on pages.
+PagesArgs pages_args(const kvk_paged *p) {
+  PagesArgs a = {};
+  const int n = p->d.n_pages;
+  uint8_t *at = p->ws + paged_ws(p->d.head_dim, n).pages;
+  auto take = [&](size_t bytes) {
+    uint8_t *x = at;
+    at += up(bytes);
+    return x;
+  };
+  a.before = reinterpret_cast<int32_t *>(take(4 * (size_t)n));
+  a.chunk = reinterpret_cast<int32_t *>(take(4 * chunks_of(n)));
+  a.rows = reinterpret_cast<ForkRow *>(take(sizeof(ForkRow) * kForkRows));
+  a.src = reinterpret_cast<int32_t *>(take(4 * list_of(n)));
+  a.dst = reinterpret_cast<int32_t *>(take(4 * list_of(n)));
+  a.n_moved = reinterpret_cast<int32_t *>(take(4));
+  a.n_pages = n;
+  a.page_shift = p->page_shift;
+  a.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim, n).err);
+  return a;
+}
+
+// Pages of all layers, `n` entries at most (n_dev: as many as it says).
+cudaError_t copy_layers(const kvk_paged *p, const int32_t *src, const int32_t *dst, int n, const int32_t *n_dev, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  for (int l0 = 0; l0 < p->d.n_layers && e == cudaSuccess; l0 += kCopyLayers) {
+    CopyArgs c = {};
+    c.layers = p->d.n_layers - l0 < kCopyLayers ? p->d.n_layers - l0 : kCopyLayers;
+    for (int l = 0; l < c.layers; ++l) {
+      c.k[l] = p->k[l0 + l];
+      c.v[l] = p->v[l0 + l];
+      if (p->coded) c.ke[l] = p->ke[l0 + l], c.ve[l] = p->ve[l0 + l];
+    }
+    c.src = src;
+    c.dst = dst;
+    c.n = n;
+    c.n_dev = n_dev;
+    c.n_pages = p->d.n_pages;
+    c.Hkv = p->d.n_kv_heads;
+    c.bytes = (int64_t)p->d.n_kv_heads * p->d.page_size * p->d.head_dim * (p->coded ? 1 : 2);
+    c.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim, p->d.n_pages).err);
+    e = launch_copy_pages(c, p->coded, p->sms, st);
+  }
+  return e;
+}
+
+// A call on pages: the rows that the table has.
+kvk_status check_pages(const kvk_paged *p, const int32_t *refs, const int32_t *refs_out, const int32_t *table, const int32_t *lengths,
+                       int batch, int max_pages) {
+  if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
+  const kvk_status s = check_device(p);
+  if (s) return s;
+  if (batch < 0 || max_pages < 0) return fail(KVK_ERR_INVALID_ARG, "batch and max_pages must not be negative");
+  if ((int64_t)max_pages * p->d.page_size > (1 << 26))
+    return fail(KVK_ERR_INVALID_ARG, "max_pages %d: more than 2^26 positions", max_pages);
+  if (!refs || !refs_out || (batch && (!lengths || (!table && max_pages))))
+    return fail(KVK_ERR_INVALID_ARG, "null holders, lengths or table");
+  if (!aligned(refs, 4) || !aligned(refs_out, 4) || !aligned(table, 4) || !aligned(lengths, 4))
+    return fail(KVK_ERR_INVALID_ARG, "misaligned holders, lengths or table");
+  return KVK_OK;
 }
 
 // Rows of a KV head up to which the form for few tokens is the faster one (us,
@@ -294,33 +381,41 @@ kvk_status kvk_paged_plan(const kvk_paged_desc *desc, size_t *pool, size_t *ws_b
   kvk_status s = check_paged_desc(desc);
   if (s) return s;
   if (!pool || !ws_bytes) return fail(KVK_ERR_INVALID_ARG, "null output");
-  *pool = pool_bytes(desc);
-  *ws_bytes = paged_ws(desc->head_dim).total;
+  *pool = pool_bytes(desc, false);
+  *ws_bytes = paged_ws(desc->head_dim, desc->n_pages).total;
   return KVK_OK;
 }
 
-kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, void *workspace,
-                            size_t ws_bytes, kvk_paged **out) {
+static kvk_status paged_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, int8_t *const *k_exps,
+                               int8_t *const *v_exps, bool coded, void *workspace, size_t ws_bytes, kvk_paged **out) {
   if (!out) return fail(KVK_ERR_INVALID_ARG, "null output handle");
   *out = nullptr;
   kvk_status s = check_paged_desc(desc);
   if (s) return s;
-  if (!k_pages || !v_pages) return fail(KVK_ERR_INVALID_ARG, "null page pools");
+  if (!k_pages || !v_pages || (coded && (!k_exps || !v_exps))) return fail(KVK_ERR_INVALID_ARG, "null page pools");
+  for (int l = 0; coded && l < desc->n_layers; ++l)
+    for (const int8_t *p : {k_exps[l], v_exps[l]})
+      if (!p || !aligned(p, 4)) return fail(KVK_ERR_INVALID_ARG, "exponents of layer %d are null or not 4-byte aligned", l);
   for (int l = 0; l < desc->n_layers; ++l)
     for (const void *p : {k_pages[l], v_pages[l]})
       if (!p || (reinterpret_cast<uintptr_t>(p) & 127u))
         return fail(KVK_ERR_INVALID_ARG, "pages of layer %d are null or not 128-byte aligned", l);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u))
     return fail(KVK_ERR_INVALID_ARG, "workspace null or not 256-byte aligned");
-  if (ws_bytes < paged_ws(desc->head_dim).total)
-    return fail(KVK_ERR_INVALID_ARG, "workspace too small: %zu < %zu", ws_bytes, paged_ws(desc->head_dim).total);
+  if (ws_bytes < paged_ws(desc->head_dim, desc->n_pages).total)
+    return fail(KVK_ERR_INVALID_ARG, "workspace too small: %zu < %zu", ws_bytes, paged_ws(desc->head_dim, desc->n_pages).total);
   kvk_paged *p = new (std::nothrow) kvk_paged();
   if (!p) return fail(KVK_ERR_INVALID_ARG, "out of host memory");
   p->d = *desc;
+  p->coded = coded;
   try {
     for (int l = 0; l < desc->n_layers; ++l) {
       p->k.push_back(static_cast<uint8_t *>(k_pages[l]));
       p->v.push_back(static_cast<uint8_t *>(v_pages[l]));
+      if (coded) {
+        p->ke.push_back(k_exps[l]);
+        p->ve.push_back(v_exps[l]);
+      }
     }
     p->maps.resize((size_t)desc->n_layers * kMaps);
   } catch (const std::bad_alloc &) {
@@ -337,7 +432,7 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
   }
   const bool bf = desc->dtype == KVK_DTYPE_BF16;
   const int hc = rows_heads(desc->page_size, desc->n_kv_heads), heads[kMaps] = {0, hc, hc, 1, 1};
-  for (int i = 0; i < desc->n_layers * kMaps && e == cudaSuccess; ++i) {
+  for (int i = 0; !coded && i < desc->n_layers * kMaps && e == cudaSuccess; ++i) {
     const int l = i / kMaps, m = i % kMaps;
     const bool values = m == 2 || m == 4;
     e = make_pages_map(p->maps[i].bytes, bf, values ? p->v[l] : p->k[l], desc->head_dim, desc->page_size, desc->n_kv_heads,
@@ -351,6 +446,26 @@ kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, vo
   return KVK_OK;
 }
 
+kvk_status kvk_paged_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, void *workspace,
+                            size_t ws_bytes, kvk_paged **out) {
+  return paged_create(desc, k_pages, v_pages, nullptr, nullptr, false, workspace, ws_bytes, out);
+}
+
+kvk_status kvk_paged_coded_plan(const kvk_paged_desc *desc, size_t *pool, size_t *exps, size_t *ws_bytes) {
+  kvk_status s = check_paged_desc(desc);
+  if (s) return s;
+  if (!pool || !exps || !ws_bytes) return fail(KVK_ERR_INVALID_ARG, "null output");
+  *pool = pool_bytes(desc, true);
+  *exps = (size_t)desc->n_pages * desc->n_kv_heads;
+  *ws_bytes = paged_ws(desc->head_dim, desc->n_pages).total;
+  return KVK_OK;
+}
+
+kvk_status kvk_paged_coded_create(const kvk_paged_desc *desc, void *const *k_pages, void *const *v_pages, int8_t *const *k_exps,
+                                  int8_t *const *v_exps, void *workspace, size_t ws_bytes, kvk_paged **out) {
+  return paged_create(desc, k_pages, v_pages, k_exps, v_exps, true, workspace, ws_bytes, out);
+}
+
 kvk_status kvk_paged_destroy(kvk_paged *p) {
   delete p;
   return KVK_OK;
@@ -359,7 +474,7 @@ kvk_status kvk_paged_destroy(kvk_paged *p) {
 kvk_status kvk_paged_reset(kvk_paged *p, kvk_stream stream) {
   if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
   const cudaError_t e =
-      cudaMemsetAsync(p->ws, 0, paged_ws(p->d.head_dim).part, reinterpret_cast<cudaStream_t>(stream));
+      cudaMemsetAsync(p->ws, 0, paged_ws(p->d.head_dim, p->d.n_pages).part, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "resetting the workspace");
   p->cleared.store(true, std::memory_order_relaxed);
   return KVK_OK;
@@ -391,11 +506,23 @@ kvk_status kvk_paged_append(kvk_paged *p, int32_t layer, const kvk_paged_batch *
   if (rotary) a.t = rotary->t;
   a.D = D;
   a.Hq = q ? p->d.n_q_heads : 0;
-  a.Hk = a.Hv = Hkv;
+  a.Hk = a.Hv = p->coded ? 0 : Hkv;
   a.n_tokens = N;
   a.pos = positions;
   a.pv = view_of(p, layer, batch);
-  const cudaError_t e = launch_rotary(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+  cudaError_t e = cudaSuccess;
+  if (p->coded) {
+    CodeArgs c = {};
+    c.t = a.t;
+    c.k = a.k;
+    c.v = a.v;
+    c.pos = positions;
+    c.rotate = rotary != nullptr;
+    c.wide = aligned(c.k.p, 16) && aligned(c.v.p, 16) && !((c.k.ts | c.k.hs | c.v.ts | c.v.hs) & 7);
+    c.pv = a.pv;
+    e = launch_append_codes(c, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+  }
+  if (e == cudaSuccess) e = launch_rotary(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged append launch");
   return KVK_OK;
 }
@@ -423,27 +550,110 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.window = window && window < kNoWindow ? window : kNoWindow;
   a.max_new = max_new < batch->n_tokens ? max_new : batch->n_tokens;
   a.sig_log2 = softmax_scale * kLog2e;
-  const PagedWs w = paged_ws(p->d.head_dim);
+  const PagedWs w = paged_ws(p->d.head_dim, p->d.n_pages);
   a.list = reinterpret_cast<RowsList *>(p->ws + w.list);
   a.tc_list = reinterpret_cast<TcList *>(p->ws + w.tc_list);
   a.part = reinterpret_cast<float *>(p->ws + w.part);
   a.sms = p->sms;
   a.device = p->device;
   a.give_up = p->give_up.load(std::memory_order_relaxed);
-  const PageMap *maps = &p->maps[(size_t)layer * kMaps];
-  a.mk = maps[0].bytes;
-  a.wk = maps[1].bytes;
-  a.wv = maps[2].bytes;
-  a.ok = maps[3].bytes;
-  a.ov = maps[4].bytes;
+  if (!p->coded) {
+    const PageMap *maps = &p->maps[(size_t)layer * kMaps];
+    a.mk = maps[0].bytes;
+    a.wk = maps[1].bytes;
+    a.wv = maps[2].bytes;
+    a.ok = maps[3].bytes;
+    a.ov = maps[4].bytes;
+  }
   // Two launches around the workspace's list of cut units: another thread's must
   // not come between them, its units would be joined into this call's output.
   cudaError_t e;
   {
     std::lock_guard<std::mutex> one(p->calls);
-    e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+    e = p->coded ? launch_attn_codes(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream))
+                 : launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
+  return KVK_OK;
+}
+
+kvk_status kvk_paged_copy(kvk_paged *p, const int32_t *src, const int32_t *dst, int32_t n, kvk_stream stream) {
+  if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
+  const kvk_status s = check_device(p);
+  if (s) return s;
+  if (n < 0) return fail(KVK_ERR_INVALID_ARG, "n must not be negative");
+  if (n == 0) return KVK_OK;
+  if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return fail(KVK_ERR_INVALID_ARG, "null or misaligned pages");
+  const cudaError_t e = copy_layers(p, src, dst, n, nullptr, reinterpret_cast<cudaStream_t>(stream));
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page copy launch");
+  return KVK_OK;
+}
+
+kvk_status kvk_paged_fork(kvk_paged *p, const int32_t *refs, const int32_t *table, const int32_t *lengths, int32_t batch,
+                          int32_t max_pages, const int32_t *parents, const int32_t *after, int32_t rows, int32_t *refs_out,
+                          int32_t *table_out, int32_t max_pages_out, kvk_stream stream) {
+  kvk_status s = check_pages(p, refs, refs_out, table, lengths, batch, max_pages);
+  if (s) return s;
+  if (rows < 0 || rows > kForkRows) return fail(KVK_ERR_INVALID_ARG, "rows must be in [0, %d]", kForkRows);
+  if (max_pages_out < 0 || (int64_t)max_pages_out * p->d.page_size > (1 << 26))
+    return fail(KVK_ERR_INVALID_ARG, "max_pages_out out of range");
+  if (rows && (!parents || (!table_out && max_pages_out))) return fail(KVK_ERR_INVALID_ARG, "null parents or table");
+  if (!aligned(parents, 4) || !aligned(after, 4) || !aligned(table_out, 4))
+    return fail(KVK_ERR_INVALID_ARG, "misaligned parents, lengths or table");
+  const int64_t in = (int64_t)batch * max_pages, out = (int64_t)rows * max_pages_out;
+  if (in && out && table_out < table + in && table < table_out + out)
+    return fail(KVK_ERR_INVALID_ARG, "a fork's table may not overlap the one it is made from");
+  PagesArgs a = pages_args(p);
+  a.refs = refs;
+  a.refs_out = refs_out;
+  a.table = table;
+  a.lens = lengths;
+  a.parents = parents;
+  a.after = after;
+  a.table_out = table_out;
+  a.B = batch;
+  a.R = rows;
+  a.max_pages = max_pages;
+  a.width = max_pages_out;
+  // launches that share the workspace follow one another
+  cudaError_t e;
+  {
+    std::lock_guard<std::mutex> one(p->calls);
+    e = launch_fork(a, reinterpret_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess && rows) e = copy_layers(p, a.src, a.dst, rows, nullptr, reinterpret_cast<cudaStream_t>(stream));
+  }
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page fork launch");
+  return KVK_OK;
+}
+
+kvk_status kvk_paged_compact(kvk_paged *p, const int32_t *refs, const int32_t *table, const int32_t *lengths, int32_t batch,
+                             int32_t max_pages, int32_t *refs_out, int32_t *table_out, int32_t *where, int32_t *used,
+                             kvk_stream stream) {
+  kvk_status s = check_pages(p, refs, refs_out, table, lengths, batch, max_pages);
+  if (s) return s;
+  if (!where || (batch && max_pages && !table_out)) return fail(KVK_ERR_INVALID_ARG, "null table or numbers");
+  if (!aligned(where, 4) || !aligned(used, 4) || !aligned(table_out, 4))
+    return fail(KVK_ERR_INVALID_ARG, "misaligned table or numbers");
+  const int64_t in = (int64_t)batch * max_pages;
+  if (in && table_out != table && table_out < table + in && table < table_out + in)
+    return fail(KVK_ERR_INVALID_ARG, "table_out may be the table, and may not overlap it otherwise");
+  PagesArgs a = pages_args(p);
+  a.refs = refs;
+  a.refs_out = refs_out;
+  a.table = table;
+  a.lens = lengths;
+  a.table_out = table_out;
+  a.where = where;
+  a.used = used;
+  a.B = batch;
+  a.max_pages = a.width = max_pages;
+  cudaError_t e;
+  {
+    std::lock_guard<std::mutex> one(p->calls);
+    e = launch_compact(a, reinterpret_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = copy_layers(p, a.src, a.dst, p->d.n_pages / 2, a.n_moved, reinterpret_cast<cudaStream_t>(stream));
+  }
+  if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page compaction launch");
   return KVK_OK;
 }
 
@@ -456,7 +666,7 @@ kvk_status kvk_paged_set_give_up(kvk_paged *p, int32_t give_up) {
 
 kvk_status kvk_paged_get_device_error(kvk_paged *p, kvk_stream stream, int32_t *code) {
   if (!p || !code) return fail(KVK_ERR_INVALID_ARG, "null paged cache or output");
-  return take_error(reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim).err), stream, code);
+  return take_error(reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim, p->d.n_pages).err), stream, code);
 }
 
 kvk_status kvk_prompt_set_give_up(int32_t give_up) {

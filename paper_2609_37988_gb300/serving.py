@@ -11,6 +11,7 @@ contiguous, any other strides (views of a fused projection, say).
     q = pages.append(layer, k, v, cu, lengths, table, rotary=rot, positions=pos, q=q)
     o = pages.attend(layer, q, cu, lengths, table, scale, max_new=1)
     o = prompt_attention(q, k, v, cu, scale)          # before anything is cached
+    refs, table = pages.fork(refs, table, lengths, parents, lengths + 1)  # beams go on, pages for their next tokens
 
 Calls run on the current stream, or on ``stream``: the caller then orders it with
 the streams its tensors belong to, and keeps them until it has run.
@@ -186,6 +187,11 @@ class PagedCache:
     ``v_pages``: one pool ``[n_pages, n_kv_heads, page_size, head_dim]`` per
     layer (bf16 or fp16); without them the pools are allocated.
 
+    ``bits=8``, or pools of ``float8_e4m3fn`` with ``k_exps`` and ``v_exps`` (int8
+    ``[n_pages, n_kv_heads]`` per layer): held as e4m3 codes with a power of two for
+    each page and KV head, an element is ``code * 2 ** exponent``.  ``dtype`` is then
+    what queries, new keys and values and results are.
+
     Calls take the batch as device int32 tensors: ``cu [B + 1]`` offsets of the
     new tokens, ``lengths [B]`` positions held with the new tokens, ``table
     [B, max_pages]`` each sequence's pages.  Calls on one object share its
@@ -193,11 +199,16 @@ class PagedCache:
     same time)."""
 
     def __init__(self, *, n_q_heads: int, n_layers: int = None, n_kv_heads: int = None, head_dim: int = None,
-                 n_pages: int = None, page_size: int = 16, dtype=torch.bfloat16, device=None, k_pages=None, v_pages=None):
+                 n_pages: int = None, page_size: int = 16, dtype=torch.bfloat16, device=None, k_pages=None, v_pages=None,
+                 bits: int = None, k_exps=None, v_exps=None):
         self.handle = None
         self.lib = load()
         if (k_pages is None) != (v_pages is None):
             raise ValueError("k_pages and v_pages go together")
+        if (k_exps is None) != (v_exps is None) or (k_exps is not None and k_pages is None):
+            raise ValueError("k_exps and v_exps go together, with the pools of codes")
+        if bits not in (None, 8, 16):
+            raise ValueError("bits must be 8 or 16")
         if k_pages is not None:
             k_pages, v_pages = list(k_pages), list(v_pages)
             if not k_pages or len(k_pages) != len(v_pages):
@@ -207,9 +218,24 @@ class PagedCache:
                 if not (t.is_cuda and t.is_contiguous()) or t.dim() != 4 or t.shape != x.shape or t.dtype != x.dtype or \
                         t.device != x.device:
                     raise ValueError("pools must be contiguous CUDA tensors [n_pages, n_kv_heads, page_size, head_dim], all alike")
-            n_layers, dtype, dev = len(k_pages), x.dtype, x.device
+            n_layers, dev = len(k_pages), x.device
             n_pages, n_kv_heads, page_size, head_dim = x.shape
+            coded = x.dtype is torch.float8_e4m3fn
+            if bits is not None and bits != (8 if coded else 16):
+                raise ValueError(f"pools of {x.dtype} in {bits} bits")
+            if not coded:
+                dtype = x.dtype
+            if coded != (k_exps is not None):
+                raise ValueError("float8_e4m3fn pools and exponents go together")
+            if coded:
+                k_exps, v_exps = list(k_exps), list(v_exps)
+                for t in k_exps + v_exps:
+                    if t.shape != (n_pages, n_kv_heads) or t.dtype is not torch.int8 or t.device != dev or not t.is_contiguous():
+                        raise ValueError("exponents must be contiguous int8 [n_pages, n_kv_heads] on the pools' device")
+                if len(k_exps) != n_layers or len(v_exps) != n_layers:
+                    raise ValueError("exponents of keys and of values per layer")
         else:
+            coded = bits == 8
             if None in (n_layers, n_kv_heads, head_dim, n_pages):
                 raise ValueError("n_layers, n_kv_heads, head_dim and n_pages, or the pools, must be given")
             dev = torch.device(device) if device is not None else torch.device("cuda")
@@ -220,19 +246,29 @@ class PagedCache:
         self.device, self.dtype = dev, dtype
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
         self.desc = PagedDesc(n_layers, n_q_heads, n_kv_heads, head_dim, page_size, n_pages, _CODES[dtype])
-        pool, ws = ctypes.c_size_t(), ctypes.c_size_t()
-        check(self.lib.kvk_paged_plan(ctypes.byref(self.desc), ctypes.byref(pool), ctypes.byref(ws)))
+        self.bits = 8 if coded else 16
+        pool, exps, ws = ctypes.c_size_t(), ctypes.c_size_t(), ctypes.c_size_t()
+        sizes = [ctypes.byref(pool), ctypes.byref(exps), ctypes.byref(ws)]
+        if coded:
+            check(self.lib.kvk_paged_coded_plan(ctypes.byref(self.desc), *sizes))
+        else:
+            check(self.lib.kvk_paged_plan(ctypes.byref(self.desc), sizes[0], sizes[2]))
         if k_pages is None:
             shape = (n_pages, n_kv_heads, page_size, head_dim)
-            k_pages = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(n_layers)]
-            v_pages = [torch.empty(shape, dtype=dtype, device=dev) for _ in range(n_layers)]
-        self.k_pages, self.v_pages = k_pages, v_pages
+            kind = torch.float8_e4m3fn if coded else dtype
+            k_pages = [torch.empty(shape, dtype=kind, device=dev) for _ in range(n_layers)]
+            v_pages = [torch.empty(shape, dtype=kind, device=dev) for _ in range(n_layers)]
+            if coded:
+                k_exps = [torch.zeros(shape[:2], dtype=torch.int8, device=dev) for _ in range(n_layers)]
+                v_exps = [torch.zeros(shape[:2], dtype=torch.int8, device=dev) for _ in range(n_layers)]
+        self.k_pages, self.v_pages, self.k_exps, self.v_exps = k_pages, v_pages, k_exps, v_exps
         self.workspace = torch.empty(ws.value, dtype=torch.uint8, device=dev)
         h = ctypes.c_void_p()
-        ptrs = [(ctypes.c_void_p * n_layers)(*[t.data_ptr() for t in p]) for p in (k_pages, v_pages)]
+        ptrs = [(ctypes.c_void_p * n_layers)(*[t.data_ptr() for t in p])
+                for p in (k_pages, v_pages) + ((k_exps, v_exps) if coded else ())]
         with torch.cuda.device(dev):
-            check(self.lib.kvk_paged_create(ctypes.byref(self.desc), ptrs[0], ptrs[1], _ptr(self.workspace), ws.value,
-                                            ctypes.byref(h)))
+            create = self.lib.kvk_paged_coded_create if coded else self.lib.kvk_paged_create
+            check(create(ctypes.byref(self.desc), *ptrs, _ptr(self.workspace), ws.value, ctypes.byref(h)))
             self.handle = h
             check(self.lib.kvk_paged_reset(h, _stream()))
             torch.cuda.current_stream().synchronize()  # calls on any stream may follow
@@ -300,6 +336,80 @@ class PagedCache:
         _call(self._index, stream, self._attend, self.handle, _int32(layer), self._batch(n, cu, lengths, table), rq, scale,
               n if max_new is None else _int32(max_new), _int32(window), out.data_ptr())
         return out
+
+    def copy(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
+        """Page ``src[i]`` to page ``dst[i]`` (int32) in all layers; -1 in either:
+        nothing.  No page may be written twice, or be both read and written."""
+        if src.dim() != 1:
+            raise ValueError("src must be [pages]")
+        n = src.shape[0]
+        _call(self._index, stream, self.lib.kvk_paged_copy, self.handle, _ints(src, "src", (n,), self._index),
+              _ints(dst, "dst", (n,), self._index), n)
+
+    def _counts(self, refs, table, lengths):
+        if lengths.dim() != 1 or table.dim() != 2:
+            raise ValueError("lengths must be [B], table [B, max_pages]")
+        B, width, index = lengths.shape[0], table.shape[1], self._index
+        return (_ints(refs, "refs", (self.desc.n_pages,), index), _ints(table, "table", (B, width), index),
+                _ints(lengths, "lengths", (B,), index), B, width)
+
+    def fork(self, refs: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
+             after: torch.Tensor = None, *, out=None, stream=None):
+        """Rows that go on from the table's: row ``i`` from row ``parents[i]`` (-1:
+        from nothing), with pages for ``after[i]`` positions (default: its parent's).
+        Pages are shared but for the one a row will write to next, which is its own
+        or a copy; new ones are the lowest that ``refs`` (int32 ``[n_pages]``, a
+        page's holders) counts 0 times.  ``out``: the pair (refs, table) to write,
+        refs perhaps the given one; returns it.  A page no longer held is free for the
+        next call; without free pages the table gets -1 and ``device_error`` tells."""
+        ptrs = self._counts(refs, table, lengths)
+        if parents.dim() != 1:
+            raise ValueError("parents must be [rows]")
+        R, index = parents.shape[0], self._index
+        if out is None:
+            refs_out = _new_like(refs, stream)
+            if R == table.shape[0]:
+                table_out = _new_like(table, stream)
+            elif stream is None:
+                table_out = table.new_empty((R, table.shape[1]))
+            else:
+                with torch.cuda.stream(stream):
+                    table_out = table.new_empty((R, table.shape[1]))
+        else:
+            refs_out, table_out = out
+            if table_out.dim() != 2:
+                raise ValueError("table must be [rows, max_pages]")
+        width = table_out.shape[1]
+        _call(index, stream, self.lib.kvk_paged_fork, self.handle, *ptrs, _ints(parents, "parents", (R,), index),
+              0 if after is None else _ints(after, "after", (R,), index), R,
+              _ints(refs_out, "refs", (self.desc.n_pages,), index), _ints(table_out, "table", (R, width), index), width)
+        return refs_out, table_out
+
+    def free(self, refs: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, *, out: torch.Tensor = None, stream=None):
+        """``refs`` (``out``, which may be it) without the pages of the table's rows."""
+        ptrs = self._counts(refs, table, lengths)
+        if out is None:
+            out = _new_like(refs, stream)
+        _call(self._index, stream, self.lib.kvk_paged_fork, self.handle, *ptrs, 0, 0, 0,
+              _ints(out, "refs", (self.desc.n_pages,), self._index), 0, 0)
+        return out
+
+    def compact(self, refs: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, *, out=None, used: torch.Tensor = None,
+                stream=None):
+        """Moves the used pages to the beginning of the pools.  Returns (refs, table,
+        where): the counts and the table afterwards and each page's new number, -1 for
+        a free one.  ``out``: the three to write, refs and table perhaps the given
+        ones.  ``used``: an int32 tensor of one element that gets the used pages'
+        number."""
+        ptrs = self._counts(refs, table, lengths)
+        if out is None:
+            out = _new_like(refs, stream), _new_like(table, stream), _new_like(refs, stream)
+        refs_out, table_out, where = out
+        index, n = self._index, self.desc.n_pages
+        _call(index, stream, self.lib.kvk_paged_compact, self.handle, *ptrs, _ints(refs_out, "refs", (n,), index),
+              _ints(table_out, "table", tuple(table.shape), index), _ints(where, "where", (n,), index),
+              0 if used is None else _ints(used, "used", (1,), index))
+        return refs_out, table_out, where
 
     def set_give_up(self, give_up: bool):
         """Whether attentions give up before their first tile, as if a bounded wait
