@@ -580,12 +580,16 @@ kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
 /* The same cache held in 8 bits: a pool's elements are e4m3 codes (a sign, 4 bits
  * of exponent of bias 7, 3 of mantissa; 0x7f and 0xff: NaN), and for every page and
  * KV head a power of two, [n_pages, n_kv_heads] of int8 for the keys and as many for
- * the values: an element is code * 2^exponent.  Pools as above; exponents 4-byte
- * aligned.  `dtype` is what queries, new keys and values and results are; exponents
- * lie in [-110, 119] (BF16) or [-15, 7] (F16; others read as the nearest of these),
- * so that every element is a number of the dtype and attention is that over the
- * dtype's own pages, with weights in f16 either way.  The handle serves every
- * kvk_paged_ call.
+ * the values: an element is code * 2^exponent.  Pools as above; exponents on as
+ * many bytes as divide n_kv_heads, 4 at most.  `dtype` is what queries, new keys and
+ * values and results are; exponents lie in [-110, 119] (BF16) or [-15, 7] (F16;
+ * others read as the nearest of these), so that every element is a number of the
+ * dtype.  Attention is as over pages of the dtype, with the products' operands in
+ * F16: weights are rounded to it once; queries are exact down to 2^-28 of a row's
+ * largest; with more than 16 rows of a KV head (max_new times its query heads)
+ * elements are exact down to 2^-21 of the largest power among the pages of 128
+ * positions (keys) or of the sequence so far (values), and off by 2^-31 of that power
+ * at most below.  The handle serves every kvk_paged_ call.
  *
  * An append sets a page and head's exponent to the least that holds the largest
  * finite magnitude among its new numbers, max |x| <= 448 * 2^exponent, and the codes

@@ -111,7 +111,10 @@ struct AttnArgs {
 cudaError_t make_pages_map(void *out, bool bf, void *pool, int D, int page, int Hkv, int n_pages, int heads);
 cudaError_t launch_attn_rows(const AttnArgs &a, int dtype, cudaStream_t st);
 cudaError_t launch_attn_tc(const AttnArgs &a, int dtype, cudaStream_t st);
-cudaError_t launch_attn_codes(const AttnArgs &a, int dtype, cudaStream_t st);
+// the same over pages in 8 bits
+cudaError_t make_codes_map(void *out, void *pool, int D, int page, int Hkv, int n_pages, int heads);
+cudaError_t launch_attn_codes_rows(const AttnArgs &a, int dtype, cudaStream_t st);
+cudaError_t launch_attn_tc_codes(const AttnArgs &a, int dtype, cudaStream_t st);
 
 // ---- operators on pages -------------------------------------------------------
 constexpr int kForkRows = 16384;   // rows that a fork may leave
@@ -157,6 +160,12 @@ constexpr int kRowsPerUnit = 16, kRowsMaxHeads = 4;
 constexpr int rows_heads(int page, int Hkv) {
   int hc = 1;
   while (hc < kRowsMaxHeads && 2 * hc * page <= 64 && Hkv % (2 * hc) == 0) hc *= 2;
+  return hc;
+}
+// the same of codes: 128 rows
+constexpr int code_heads(int page, int Hkv) {
+  int hc = 1;
+  while (hc < kRowsMaxHeads && 2 * hc * page <= 128 && Hkv % (2 * hc) == 0) hc *= 2;
   return hc;
 }
 // floats of one partial: rows of D sums, then maxima, then totals

@@ -249,6 +249,7 @@ kvk_status check_pages(const kvk_paged *p, const int32_t *refs, const int32_t *r
 // rows 54 / 40; 1 x 1024, 10 rows 17 / 18).
 constexpr int kFewRows = 16;
 cudaError_t launch_attn(const AttnArgs &a, int dtype, cudaStream_t st) {
+  if (a.pv.ke) return (int64_t)a.max_new * a.G <= kFewRows ? launch_attn_codes_rows(a, dtype, st) : launch_attn_tc_codes(a, dtype, st);
   if (a.pv.k && (int64_t)a.max_new * a.G <= kFewRows) return launch_attn_rows(a, dtype, st);
   return launch_attn_tc(a, dtype, st);
 }
@@ -393,9 +394,11 @@ static kvk_status paged_create(const kvk_paged_desc *desc, void *const *k_pages,
   kvk_status s = check_paged_desc(desc);
   if (s) return s;
   if (!k_pages || !v_pages || (coded && (!k_exps || !v_exps))) return fail(KVK_ERR_INVALID_ARG, "null page pools");
+  const int exp_align = desc->n_kv_heads % 4 == 0 ? 4 : desc->n_kv_heads % 2 == 0 ? 2 : 1;
   for (int l = 0; coded && l < desc->n_layers; ++l)
     for (const int8_t *p : {k_exps[l], v_exps[l]})
-      if (!p || !aligned(p, 4)) return fail(KVK_ERR_INVALID_ARG, "exponents of layer %d are null or not 4-byte aligned", l);
+      if (!p || !aligned(p, exp_align))
+        return fail(KVK_ERR_INVALID_ARG, "exponents of layer %d are null or not %d-byte aligned", l, exp_align);
   for (int l = 0; l < desc->n_layers; ++l)
     for (const void *p : {k_pages[l], v_pages[l]})
       if (!p || (reinterpret_cast<uintptr_t>(p) & 127u))
@@ -432,9 +435,16 @@ static kvk_status paged_create(const kvk_paged_desc *desc, void *const *k_pages,
   }
   const bool bf = desc->dtype == KVK_DTYPE_BF16;
   const int hc = rows_heads(desc->page_size, desc->n_kv_heads), heads[kMaps] = {0, hc, hc, 1, 1};
-  for (int i = 0; !coded && i < desc->n_layers * kMaps && e == cudaSuccess; ++i) {
+  const int code_hc = code_heads(desc->page_size, desc->n_kv_heads);
+  for (int i = 0; i < desc->n_layers * kMaps && e == cudaSuccess; ++i) {
     const int l = i / kMaps, m = i % kMaps;
     const bool values = m == 2 || m == 4;
+    if (coded) {
+      if (m > 0)
+        e = make_codes_map(p->maps[i].bytes, values ? p->v[l] : p->k[l], desc->head_dim, desc->page_size, desc->n_kv_heads,
+                           desc->n_pages, m <= 2 ? code_hc : 1);
+      continue;
+    }
     e = make_pages_map(p->maps[i].bytes, bf, values ? p->v[l] : p->k[l], desc->head_dim, desc->page_size, desc->n_kv_heads,
                        desc->n_pages, heads[m]);
   }
@@ -557,21 +567,18 @@ kvk_status kvk_paged_attention(kvk_paged *p, int32_t layer, const kvk_paged_batc
   a.sms = p->sms;
   a.device = p->device;
   a.give_up = p->give_up.load(std::memory_order_relaxed);
-  if (!p->coded) {
-    const PageMap *maps = &p->maps[(size_t)layer * kMaps];
-    a.mk = maps[0].bytes;
-    a.wk = maps[1].bytes;
-    a.wv = maps[2].bytes;
-    a.ok = maps[3].bytes;
-    a.ov = maps[4].bytes;
-  }
+  const PageMap *maps = &p->maps[(size_t)layer * kMaps];
+  a.mk = maps[0].bytes;
+  a.wk = maps[1].bytes;
+  a.wv = maps[2].bytes;
+  a.ok = maps[3].bytes;
+  a.ov = maps[4].bytes;
   // Two launches around the workspace's list of cut units: another thread's must
   // not come between them, its units would be joined into this call's output.
   cudaError_t e;
   {
     std::lock_guard<std::mutex> one(p->calls);
-    e = p->coded ? launch_attn_codes(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream))
-                 : launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
+    e = launch_attn(a, p->d.dtype, reinterpret_cast<cudaStream_t>(stream));
   }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "paged attention launch");
   return KVK_OK;

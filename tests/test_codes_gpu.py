@@ -83,6 +83,13 @@ class Codes:
                 r = tuple(np.zeros_like(x) for x in r)
             out.append(r[0])
             tol.append(osv.attend_bound(*r, self.d, max(l, 1), U[self.dtype], SMALL))
+            if l > 0:
+                # chunks: a value is code * 2^(e - E + 6) in f16, E the largest of the powers e of
+                # the sequence's pages; below 2^-14 that is rounded to a multiple of 2^-24, by at most
+                # 2^-25, and the weights, which sum to 1, make it at most 2^(E - 31) of the result
+                pages = self.table[b, :(l + self.page - 1) // self.page]
+                top = np.ldexp(1.0, self.exps[1][pages].astype(int).max(0) - 31)
+                tol[-1] += np.repeat(top, self.hq // self.hkv)[:, None]
             at += n
         return np.concatenate(out), np.concatenate(tol)
 
@@ -489,3 +496,27 @@ def test_weights_far_below_the_largest(gap, dtype, d, page, positions):
     for max_new in (1, b.n):
         got = b.attend(1.0, max_new=max_new)[:1]
         close(got, r[0], osv.attend_bound(*r, d, positions, U[dtype], SMALL), f"max_new {max_new}")
+
+
+@pytest.mark.parametrize("news", [[2, 1], [80, 150]])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_keys_of_zeros_and_small_queries(news, dtype):
+    """Pages of zero keys have the least power; scores of 0 and masked ones beside each other."""
+    b = Codes(news, [200, 190], 10, 2, 128, dtype, 16, seed=32)
+    for s in range(2):
+        b.k[s][: 160 + 20 * s] = 0.0
+    b.q *= 2.0 ** (-60 if dtype == BF16 else -12)
+    b.append().same()
+    for window in (0, 33):
+        b.check(window)
+
+
+@pytest.mark.parametrize("news", [[1, 1], [70, 130]])
+def test_an_attention_that_gives_up_says_so(news):
+    b = Codes(news, [200, 190], 10, 2, 128, BF16, 16, seed=33).append()
+    keep = b.attend(0.088)
+    b.cache.set_give_up(True)
+    b.attend(0.088)
+    assert b.cache.device_error() == 8
+    b.cache.set_give_up(False)
+    assert torch.equal(b.attend(0.088), keep) and b.cache.device_error() == 0

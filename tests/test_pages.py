@@ -48,7 +48,7 @@ def test_coded_create_refuses_pools_exponents_and_workspaces(lib):
     ws = _plan(lib)[3]
     ok = p(256, 256)
     for k, v, ke, ve, w, n in ((p(256, 0), ok, ok, ok, 256, ws), (ok, p(256, 272), ok, ok, 256, ws), (ok, ok, p(256, 0), ok, 256, ws),
-                               (ok, ok, ok, p(256, 258), 256, ws), (ok, ok, None, ok, 256, ws), (ok, ok, ok, None, 256, ws),
+                               (ok, ok, ok, p(256, 257), 256, ws), (ok, ok, None, ok, 256, ws), (ok, ok, ok, None, 256, ws),
                                (ok, ok, ok, ok, 128, ws), (ok, ok, ok, ok, 256, ws - 1), (None, ok, ok, ok, 256, ws)):
         assert so.kvk_paged_coded_create(ctypes.byref(_desc(lib)), k, v, ke, ve, w, n, ctypes.byref(h)) == INVALID
         assert not h.value
