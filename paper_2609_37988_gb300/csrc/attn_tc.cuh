@@ -95,8 +95,9 @@ struct Job {
 struct TilePow {
   uint32_t kf[8], vf[8];  // of every part, 2^(e - ref + 6) as the product of two halves, the second mostly 1
   int kref, vref;         // ref - 6
+  int kfar, vfar;         // whether a second half is not 1
 };
-constexpr int kRefUp = 6;
+constexpr int kRefUp = 6, kNoPow = -1000;
 
 
 // floats of a piece's query tile: D / 4 x 128 rows x 4 results, then references
@@ -109,8 +110,8 @@ template <int D, bool CODES>
 struct Smem {
   static constexpr int kTile = D / 64 * kBox;          // a query, key or value tile
   static constexpr int kRawTile = kTcT * D;            // its codes
-  static constexpr int kStages = CODES ? (D == 128 ? 4 : 6) : D == 128 ? 5 : 8;
-  static constexpr int kRaw = CODES ? (D == 128 ? 2 : 6) : 0;
+  static constexpr int kStages = CODES ? (D == 128 ? 3 : 6) : D == 128 ? 5 : 8;
+  static constexpr int kRaw = CODES ? (D == 128 ? 4 : 6) : 0;
   static constexpr int kPows = D == 128 ? 8 : 16;      // tiles whose powers are kept
   static_assert(!CODES || (kStages + kRaw) / 2 + 3 <= kPows, "powers of the tiles in either ring and at work");
   static constexpr int kQ = 0, kRing = 2 * kTile, kRawRing = kRing + kStages * kTile, kBar = kRawRing + kRaw * kRawTile;
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           return pv.n_pages;
         };
         auto power = [&](int pg, const int8_t *e) {
-          return pg < pv.n_pages ? min(max((int)e[(int64_t)pg * pv.Hkv + j.h], pv.e_lo), pv.e_hi) : -128;
+          return pg < pv.n_pages ? min(max((int)e[(int64_t)pg * pv.Hkv + j.h], pv.e_lo), pv.e_hi) : kNoPow;
         };
         auto factor = [&](int d) {
           const int x = max(d + kRefUp, -14), y = max(d + kRefUp - x, -24);
@@ -352,8 +353,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             if (!wait0(&rfree[s], ph ^ 1)) return false;
             if (kv == 0) {
               TilePow *tp = &pows[(j.tile0 + jt) % SM::kPows];
-              if (lane < cparts) tp->kf[lane] = factor(max(ek - kref, -128)), tp->vf[lane] = factor(max(ev - vref, -128));
-              if (lane == 0) tp->kref = kref - kRefUp, tp->vref = vref - kRefUp;
+              // (parts without a page are zeros whatever their factor)
+              const int dk = ek == kNoPow ? 0 : max(ek - kref, -128), dv = ev == kNoPow ? 0 : max(ev - vref, -128);
+              if (lane < cparts) tp->kf[lane] = factor(dk), tp->vf[lane] = factor(dv);
+              const bool kfar = __any_sync(kAll, dk + kRefUp < -14), vfar = __any_sync(kAll, dv + kRefUp < -14);
+              if (lane == 0) tp->kref = kref - kRefUp, tp->vref = vref - kRefUp, tp->kfar = kfar, tp->vfar = vfar;
               __syncwarp();
             }
             if (lane == 0) mbar_expect_tx(&rfull[s], SM::kRawTile);
@@ -727,8 +731,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     __syncwarp();
   } else if (CODES && warp >= 10) {
     // -- f16 tiles of codes: a warp has 64 rows of each ------------------------------
-    constexpr int LR = D / 16, RI = 32 / LR;  // lanes of a row (16 codes each), rows at a time
-    const int w = warp - 10, cc = lane % LR, r0 = 64 * w + lane / LR;
+    // A lane takes 16 codes of a row: piece cc, two pieces in f16.  D = 64: 8 rows at a
+    // time, a row's pieces on neighbouring lanes.  D = 128: 4 rows, of 8 that take two
+    // turns; rows b and b ^ 5 of either half's four pieces stand on 8 neighbouring
+    // lanes, so that neither their codes nor the f16 pieces meet on a bank.
+    constexpr bool wide = D == 128;
+    const int w = warp - 10, cc = (lane & 3) | (wide ? lane >> 1 & 4 : 0);
+    int at_raw[2], at_f16[2];  // of a row in either turn
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const int r = 64 * w + (wide ? (lane & 4 ? 5 : 0) ^ (lane & 16 ? 2 : 0) ^ y : lane >> 2);
+      at_raw[y] = r * D + ((cc ^ (wide ? r & 7 : r >> 1 & 3)) << 4);
+      at_f16[y] = (cc >> 2) * kBox + r * 128 + (((2 * (cc & 3)) ^ (r & 7)) << 4);
+    }
     int s = 0, rs = 0;
     uint32_t ph = 0, rph = 0, loads = 0;
     for (int k = 0;; ++k) {
@@ -783,50 +798,56 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
           uint8_t *dst = sm + SM::kRing + s * SM::kTile;
           const uint32_t *fac = kv ? tp->vf : tp->kf;
           bool fine = true;
-          constexpr int U = 4;
-#pragma unroll 1
-          for (int i = 0; i < 64 / RI; i += U) {
-            uint4 u[U];
+          auto go = [&](auto FAR, auto LOOK) {
+            constexpr int N = wide ? 4 : 2;  // times for 16 rows, which have one factor
 #pragma unroll
-            for (int y = 0; y < U; ++y) {
-              const int r = r0 + (i + y) * RI;
-              u[y] = *reinterpret_cast<const uint4 *>(src + r * D + ((cc ^ (D == 128 ? r & 7 : r >> 1 & 3)) << 4));
-            }
-            if (kv && partial) {
+            for (int q = 0; q < 4; q += 2) {
+              uint4 u[2 * N];
+              uint32_t f[2];
 #pragma unroll
-              for (int y = 0; y < U; ++y) {
+              for (int y = 0; y < 2 * N; ++y)
+                u[y] = *reinterpret_cast<const uint4 *>(src + at_raw[wide ? y & 1 : 0] + (N * q + y >> (wide ? 1 : 0)) * (8 * D));
+#pragma unroll
+              for (int y = 0; y < 2; ++y) f[y] = fac[(64 * w + 16 * (q + y)) >> pv.page_shift];
+#pragma unroll
+              for (int y = 0; y < 2 * N; ++y) {
                 uint32_t v[4] = {u[y].x, u[y].y, u[y].z, u[y].w};
+                if constexpr (decltype(LOOK)::value) {
 #pragma unroll
-                for (int z = 0; z < 4; ++z) {
-                  const uint32_t bad = ((v[z] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // a NaN's top bit
-                  if (bad) {
-                    fine = false;
+                  for (int z = 0; z < 4; ++z) {
+                    const uint32_t bad = ((v[z] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // a NaN's top bit
+                    fine = fine && bad == 0;
                     v[z] &= ~((bad >> 7) * 255u);
                   }
                 }
-                u[y] = make_uint4(v[0], v[1], v[2], v[3]);
+                const uint32_t f1 = __byte_perm(f[y / N], 0, 0x1010);
+                uint32_t h[8];
+#pragma unroll
+                for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(code2_f16(z & 1 ? v[z >> 1] >> 16 : v[z >> 1]), f1);
+                if constexpr (decltype(FAR)::value) {
+                  const uint32_t f2 = __byte_perm(f[y / N], 0, 0x3232);
+#pragma unroll
+                  for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(h[z], f2);
+                }
+                uint8_t *to = dst + (N * q + y >> (wide ? 1 : 0)) * (8 * 128);
+                const int at = at_f16[wide ? y & 1 : 0];
+                *reinterpret_cast<uint4 *>(to + at) = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4 *>(to + (at ^ 16)) = make_uint4(h[4], h[5], h[6], h[7]);
               }
             }
-#pragma unroll
-            for (int y = 0; y < U; ++y) {
-              const int r = r0 + (i + y) * RI;
-              const uint32_t f = fac[r >> pv.page_shift], f1 = __byte_perm(f, 0, 0x1010), f2 = __byte_perm(f, 0, 0x3232);
-              const uint32_t v[4] = {u[y].x, u[y].y, u[y].z, u[y].w};
-              uint32_t h[8];
-#pragma unroll
-              for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(code2_f16(z & 1 ? v[z >> 1] >> 16 : v[z >> 1]), f1);
-              if (f2 != 0x3c003c00u) {
-#pragma unroll
-                for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(h[z], f2);
-              }
-              const uint4 a0 = make_uint4(h[0], h[1], h[2], h[3]), a1 = make_uint4(h[4], h[5], h[6], h[7]);
-              uint8_t *row = dst + (cc >> 2) * kBox + r * 128;
-              const int c0 = ((2 * (cc & 3)) ^ (r & 7)) << 4;
-              // lanes of either half begin with another piece, on other banks
-              const bool swap = cc >> 2;
-              *reinterpret_cast<uint4 *>(row + (swap ? c0 ^ 16 : c0)) = swap ? a1 : a0;
-              *reinterpret_cast<uint4 *>(row + (swap ? c0 : c0 ^ 16)) = swap ? a0 : a1;
-            }
+          };
+          constexpr std::integral_constant<bool, false> no;
+          constexpr std::integral_constant<bool, true> yes;
+          const bool far = kv ? tp->vfar : tp->kfar;
+          if (kv && partial) {
+            if (far)
+              go(yes, yes);
+            else
+              go(no, yes);
+          } else if (far) {
+            go(yes, no);
+          } else {
+            go(no, no);
           }
           if (!fine) js.bad = 1;
           fence_proxy_async();
