@@ -3,10 +3,12 @@
 //
 // Units, runs and the joining of cut units are those of the 16-bit form
 // (rows_common.cuh).  A tile is 128 positions x KV heads of codes, 16 KB; a unit has
-// up to 4 KV heads, so that a copy is 8 or 16 KB where pages are small.  A CTA: 8
-// warps, 16 positions of one head's tile each, which lie in one page and so have one
-// power of two, and a warp that looks up pages and powers and copies the tiles by
-// TMA through a ring of 96 KB.
+// up to 4 KV heads, so that a copy is 8 or 16 KB where pages are small.  A CTA: 4
+// warps, 32 positions of one head's tile each, in two blocks of 16 that lie in one
+// page and so have one power of two, and a warp that looks up pages and powers and
+// copies the tiles by TMA through a ring of 96 KB.  (8 warps of one block each took
+// 426 instructions a block, a third of them around the products: 100 us where
+// two blocks take 93.)
 //
 // Codes are exact in f16 and go to the tensor cores as they are: S^T = K Q^T and
 // O^T += V^T P^T on mma.m16n8k16.  The keys' power multiplies the scores.  The
@@ -39,8 +41,9 @@ namespace kvk {
 namespace {
 
 constexpr int kT = 128;         // positions x KV heads of a tile
-constexpr int kWarps = 8;       // that compute; one beside them copies
+constexpr int kWarps = 4;       // that compute; one beside them copies
 constexpr int kThreads = 32 * kWarps;
+constexpr int kBlocks = 2;      // of 16 positions, a warp's of a tile
 constexpr int kMinShare = 2;    // tiles of a run at least
 constexpr float kShift = 14.f;  // weights are 2^14 as large
 
@@ -50,15 +53,25 @@ struct RowsArgs {
 };
 
 // an even number: keys and values in turn
-template <int D, int NB>
-constexpr int rows_stages() { return 768 / D * NB; }
+template <int D>
+constexpr int rows_stages() { return 768 / D; }
 
-// NB: query rows of a unit in blocks of 8.  Two of them take twice the registers and
-// one CTA an SM.
+__device__ __forceinline__ void ldm(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at));
+}
+__device__ __forceinline__ void ldm_t(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(at));
+}
+
+// NB: query rows of a unit in blocks of 8
 template <int D, int NB, bool BF16>
-__global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(const __grid_constant__ RowsArgs ra) {
+__global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const __grid_constant__ RowsArgs ra) {
   constexpr int kTile = kT * D;        // bytes of a key (or value) tile
-  constexpr int KS = D / 16, NS = rows_stages<D, NB>(), RU = 8 * NB;
+  constexpr int KS = D / 16, NS = rows_stages<D>(), RU = 8 * NB;
   const AttnArgs &a = ra.a;
   extern __shared__ uint8_t sm_raw[];
   uint8_t *sm = sm_raw + ((1024u - (smem_u32(sm_raw) & 1023u)) & 1023u);
@@ -202,9 +215,17 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
     __syncwarp();
     if (lane == 0) mbar_arrive(&s_free[at_stage]);
   };
-  // this lane's row of the warp's 16 positions, as ldmatrix wants its address
-  const int rk = sub * 16 + (lane & 15), at_k = row_at(rk), xk = lane >> 4;
-  const int my_part = (sub * 16) >> shift;
+  // this lane's row of either block, as ldmatrix wants its address: of its first 16
+  // codes, the swizzle in place (what a row starts on leaves those bits alone)
+  constexpr int PB = kBlocks;
+  const int r_lane = sub * 16 * PB + (lane & 15);
+  uint32_t at_row[PB];
+  int my_part[PB];
+#pragma unroll
+  for (int b = 0; b < PB; ++b) {
+    at_row[b] = smem_u32(sm) + row_at(r_lane + 16 * b) + (((lane >> 4) ^ swz(r_lane)) << 4);
+    my_part[b] = (sub * PB + b) * 16 >> shift;
+  }
   for (int w = 0; w < mine;) {
     // a piece: tiles [t_begin, t_end) of one unit
     const int t_begin = at.t, t_end = min(at.nt, at.t + (mine - w)), w_begin = w;
@@ -272,48 +293,53 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
     for (; at.t < t_end; ++at.t, ++w) {
       if (!wait(&s_full[stage], par)) break;
       k_stage = stage;
-      const uint8_t *ks = sm + stage * kTile + at_k;
-      const int ek = min(max((int)s_pow[stage >> 1][0][my_part][hh], pv.e_lo), pv.e_hi);
-      const int ev = min(max((int)s_pow[stage >> 1][1][my_part][hh], pv.e_lo), pv.e_hi);
-      next_stage();
-      const int t0 = at.lo + at.t * pt + sub * 16;  // the warp's positions
-      // two chains of products: one is latency
-      float s[NB][4] = {}, s1[NB][4] = {};
+      float fk[PB];
+      int ev[PB];
 #pragma unroll
-      for (int k = 0; k < KS; k += 2) {
-        uint32_t r[4];
-        ldmatrix_x4(r[0], r[1], r[2], r[3], ks + (((k + xk) ^ swz(rk)) << 4));
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const uint32_t a0 = code2_f16(r[2 * y]), a1 = code2_f16(r[2 * y + 1]);
-          const uint32_t a2 = code2_f16(r[2 * y] >> 16), a3 = code2_f16(r[2 * y + 1] >> 16);
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) mma<false>(y ? s1[nb] : s[nb], a0, a1, a2, a3, qf[k + y][nb][0], qf[k + y][nb][1]);
-        }
+      for (int b = 0; b < PB; ++b) {
+        fk[b] = pow2f(min(max((int)s_pow[stage >> 1][0][my_part[b]][hh], pv.e_lo), pv.e_hi));
+        ev[b] = min(max((int)s_pow[stage >> 1][1][my_part[b]][hh], pv.e_lo), pv.e_hi);
       }
+      const int t0 = at.lo + at.t * pt + sub * 16 * PB;  // the warp's positions
+      float s[PB][NB][4] = {};
+#pragma unroll
+      for (int k = 0; k < KS; k += 2)
+#pragma unroll
+        for (int b = 0; b < PB; ++b) {
+          uint32_t r[4];
+          ldm(r, (at_row[b] + k_stage * kTile) ^ (k << 4));
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const uint32_t a0 = code2_f16(r[2 * y]), a1 = code2_f16(r[2 * y + 1]);
+            const uint32_t a2 = code2_f16(r[2 * y] >> 16), a3 = code2_f16(r[2 * y + 1] >> 16);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma<false>(s[b][nb], a0, a1, a2, a3, qf[k + y][nb][0], qf[k + y][nb][1]);
+          }
+        }
+      next_stage();
       // the last tile's stages are kept: the warps' states meet there
       const bool last = at.t + 1 == t_end;
       if (!last) release(k_stage);
-      const bool partial = t0 + 15 > lim_min || t0 < low_max;
-      const float fk = pow2f(ek);
+      const bool partial = t0 + 16 * PB - 1 > lim_min || t0 < low_max;
       float mx[2 * NB];
       bool more = false;
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int i = 0; i < 2 * NB; ++i) {
+        mx[i] = -INFINITY;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int i = 2 * nb + e;
-          const float f = sig[i] * fk;
+        for (int b = 0; b < PB; ++b) {
+          const float f = sig[i] * fk[b];
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
-            const int t = t0 + g + 8 * y;
-            float x = (s[nb][2 * y + e] + s1[nb][2 * y + e]) * f;
+            float &x = s[b][i >> 1][2 * y + (i & 1)];
+            x *= f;
+            const int t = t0 + 16 * b + 8 * y + g;
             if (partial && (t > lim[i] || t < low[i])) x = -INFINITY;
-            s[nb][2 * y + e] = x;
+            mx[i] = fmaxf(mx[i], x);
           }
-          mx[i] = fmaxf(s[nb][e], s[nb][2 + e]);
-          more = more || mx[i] > m[i];
         }
+        more = more || mx[i] > m[i];
+      }
       if (__any_sync(kAll, more)) {
 #pragma unroll
         for (int i = 0; i < 2 * NB; ++i) {
@@ -329,70 +355,87 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
           m[i] = mn;
         }
       }
-      if (ev > E) {
-        const float f = pow2f(max(E - ev, -126));
+      int top = ev[0];
+#pragma unroll
+      for (int b = 1; b < PB; ++b) top = max(top, ev[b]);
+      if (top > E) {
+        const float f = pow2f(max(E - top, -126));
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
           for (int k = 0; k < KS; ++k) o[nb][k][0] *= f, o[nb][k][1] *= f, o[nb][k][2] *= f, o[nb][k][3] *= f;
-        E = ev;
+        E = top;
       }
-      const float fv = pow2f(max(ev - E, -126));
       // P^T as the B operand
-      uint32_t ph[NB][2];
+      uint32_t ph[PB][NB][2];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
+      for (int b = 0; b < PB; ++b) {
+        const float fv = pow2f(max(ev[b] - E, -126));
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float ref = m[2 * nb + (e & 1)];
-          s[nb][e] = fast_exp2(s[nb][e] - (ref == -INFINITY ? 0.f : ref) + kShift);
-          l[2 * nb + (e & 1)] += s[nb][e];
-          s[nb][e] *= fv;
+        for (int nb = 0; nb < NB; ++nb) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float ref = m[2 * nb + (e & 1)];
+            float &x = s[b][nb][e];
+            x = fast_exp2(x - ((ref == -INFINITY ? 0.f : ref) - kShift));
+            l[2 * nb + (e & 1)] += x;
+            x *= fv;
+          }
+#pragma unroll
+          for (int y = 0; y < 2; ++y) ph[b][nb][y] = movmatrix_t(pack_f16(s[b][nb][2 * y], s[b][nb][2 * y + 1]));
         }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) ph[nb][y] = movmatrix_t(pack_f16(s[nb][2 * y], s[nb][2 * y + 1]));
       }
       if (!wait(&s_full[stage], par)) break;
       v_stage = stage;
-      const uint8_t *vs = sm + stage * kTile + at_k;
       next_stage();
       bool plain = false;
       if (partial) {
         // weight 0 times a NaN would be NaN
         uint32_t any = 0;
 #pragma unroll
-        for (int k = 0; k < KS; k += 2) {
-          const uint4 u = *reinterpret_cast<const uint4 *>(vs + (((k + xk) ^ swz(rk)) << 4));
-          any |= (u.x & 0x7f7f7f7fu) + 0x01010101u | (u.y & 0x7f7f7f7fu) + 0x01010101u | (u.z & 0x7f7f7f7fu) + 0x01010101u |
-                 (u.w & 0x7f7f7f7fu) + 0x01010101u;
-        }
+        for (int b = 0; b < PB; ++b)
+#pragma unroll
+          for (int k = 0; k < KS; k += 2) {
+            uint32_t r[4];
+            ldm(r, (at_row[b] + v_stage * kTile) ^ (k << 4));
+#pragma unroll
+            for (int y = 0; y < 4; ++y) any |= (r[y] & 0x7f7f7f7fu) + 0x01010101u;
+          }
         plain = __any_sync(kAll, (any & 0x80808080u) != 0);
       }
       if (!plain) {
 #pragma unroll
-        for (int k = 0; k < KS; k += 2) {
-          uint32_t r[4];
-          ldmatrix_x4_t(r[0], r[1], r[2], r[3], vs + (((k + xk) ^ swz(rk)) << 4));
+        for (int k = 0; k < KS; k += 2)
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            // bytes of either channel side by side
-            const uint32_t u = __byte_perm(r[2 * y], 0, 0x3120), v = __byte_perm(r[2 * y + 1], 0, 0x3120);
-            const uint32_t a0 = code2_f16(u), a1 = code2_f16(u >> 16), a2 = code2_f16(v), a3 = code2_f16(v >> 16);
+          for (int b = 0; b < PB; ++b) {
+            uint32_t r[4];
+            ldm_t(r, (at_row[b] + v_stage * kTile) ^ (k << 4));
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma<false>(o[nb][k + y], a0, a1, a2, a3, ph[nb][0], ph[nb][1]);
+            for (int y = 0; y < 2; ++y) {
+              // bytes of either channel side by side
+              const uint32_t u = __byte_perm(r[2 * y], 0, 0x3120), v = __byte_perm(r[2 * y + 1], 0, 0x3120);
+              const uint32_t a0 = code2_f16(u), a1 = code2_f16(u >> 16), a2 = code2_f16(v), a3 = code2_f16(v >> 16);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma<false>(o[nb][k + y], a0, a1, a2, a3, ph[b][nb][0], ph[b][nb][1]);
+            }
           }
-        }
       } else {
 #pragma unroll 1
-        for (int y = 0; y < 16; ++y) {
-          const int rr = sub * 16 + y, t = t0 + y;
+        for (int y = 0; y < 16 * PB; ++y) {
+          const int rr = sub * 16 * PB + y, t = t0 + y;
           const uint8_t *row = sm + v_stage * kTile + row_at(rr);
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              const float p0 = __shfl_sync(kAll, s[nb][e], (y & 7) * 4 + c), p1 = __shfl_sync(kAll, s[nb][2 + e], (y & 7) * 4 + c);
-              const float p = y & 8 ? p1 : p0;
+              float p = 0.f;
+#pragma unroll
+              for (int b = 0; b < PB; ++b)
+#pragma unroll
+                for (int z = 0; z < 2; ++z) {
+                  const float x = __shfl_sync(kAll, s[b][nb][2 * z + e], (y & 7) * 4 + c);
+                  p = y >> 3 == 2 * b + z ? x : p;
+                }
               if (t <= lim[2 * nb + e] && t >= low[2 * nb + e]) {
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
@@ -408,8 +451,8 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
     }
 
     // The warps' states meet in the two stages just read (keys in an even one,
-    // values in the next), 8 rows at a time, relative to the head's largest power.
-    float *mg = reinterpret_cast<float *>(sm + k_stage * kTile);  // [kWarps][8][D]
+    // values in the next), relative to the head's largest power.
+    float *mg = reinterpret_cast<float *>(sm + k_stage * kTile);  // [kWarps][RU][D]
 #pragma unroll
     for (int i = 0; i < 2 * NB; ++i) {
 #pragma unroll
@@ -448,41 +491,38 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
     constexpr int V = D / 4, RW = 32 / V;  // lanes of a row, rows of a warp at a time
     const int v = lane % V;
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      if (nb > 0) bar_sync();
+    for (int i = 0; i < 2 * NB; ++i) {
+      const int r = 8 * (i >> 1) + 2 * c + (i & 1);
+      float M = m[i];
+      for (int y = 0; y < per_head; ++y) M = fmaxf(M, s_ml[hh * per_head + y][r].x);
+      // a warp that saw nothing has zeros, and 0 * f stays 0; NaN sums stay NaN
+      const float f = (m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - M)) * rel;
+      float *dst = mg + (warp * RU + r) * D;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int i = 2 * nb + e, r = 2 * c + e;
-        float M = m[i];
-        for (int y = 0; y < per_head; ++y) M = fmaxf(M, s_ml[hh * per_head + y][8 * nb + r].x);
-        // a warp that saw nothing has zeros, and 0 * f stays 0; NaN sums stay NaN
-        const float f = (m[i] == -INFINITY ? 0.f : fast_exp2(m[i] - M)) * rel;
-        float *dst = mg + (warp * 8 + r) * D;
-#pragma unroll
-        for (int k = 0; k < KS; ++k)
-          *reinterpret_cast<float2 *>(dst + ((16 * k + 2 * g + 16 * c) & (D - 1))) = make_float2(o[nb][k][e] * f, o[nb][k][2 + e] * f);
-      }
-      bar_sync();
-      // the warps of a head share its rows, 4 channels a lane
+      for (int k = 0; k < KS; ++k)
+        *reinterpret_cast<float2 *>(dst + ((16 * k + 2 * g + 16 * c) & (D - 1))) =
+            make_float2(o[i >> 1][k][i & 1] * f, o[i >> 1][k][2 + (i & 1)] * f);
+    }
+    bar_sync();
+    // the warps of a head share its rows, 4 channels a lane
 #pragma unroll 2
-      for (int i = sub * RW; i < 8; i += RW * per_head) {
-        const int r = i + lane / V, rr = 8 * nb + r;
-        const float f = __shfl_sync(kAll, inv, rr & 31);
-        const uint32_t off = __shfl_sync(kAll, row_off, rr & 31);
-        if (rr < R) {
-          const float *src = mg + ((hh * per_head) * 8 + r) * D + ((4 * v + 16 * (r >> 1)) & (D - 1));
-          float4 x = *reinterpret_cast<const float4 *>(src);
-          for (int y = 1; y < per_head; ++y) {
-            const float4 z = *reinterpret_cast<const float4 *>(src + y * 8 * D);
-            x.x += z.x, x.y += z.y, x.z += z.z, x.w += z.w;
-          }
-          if (!whole) {
-            __stcg(reinterpret_cast<float4 *>(part + rr * D + 4 * v), make_float4(x.x * unit, x.y * unit, x.z * unit, x.w * unit));
-          } else {
-            if (f < 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
-            *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + ((uint64_t)off * D + 4 * v) * 2) =
-                make_uint2(pack2<BF16>(x.x * f * unit, x.y * f * unit), pack2<BF16>(x.z * f * unit, x.w * f * unit));
-          }
+    for (int i = sub * RW; i < RU; i += RW * per_head) {
+      const int r = i + lane / V;
+      const float f = __shfl_sync(kAll, inv, r & 31);
+      const uint32_t off = __shfl_sync(kAll, row_off, r & 31);
+      if (r < R) {
+        const float *src = mg + ((hh * per_head) * RU + r) * D + ((4 * v + 16 * (r >> 1 & 3)) & (D - 1));
+        float4 x = *reinterpret_cast<const float4 *>(src);
+        for (int y = 1; y < per_head; ++y) {
+          const float4 z = *reinterpret_cast<const float4 *>(src + y * RU * D);
+          x.x += z.x, x.y += z.y, x.z += z.z, x.w += z.w;
+        }
+        if (!whole) {
+          __stcg(reinterpret_cast<float4 *>(part + r * D + 4 * v), make_float4(x.x * unit, x.y * unit, x.z * unit, x.w * unit));
+        } else {
+          if (f < 0.f) x = make_float4(0.f, 0.f, 0.f, 0.f);
+          *reinterpret_cast<uint2 *>(static_cast<uint8_t *>(a.out) + ((uint64_t)off * D + 4 * v) * 2) =
+              make_uint2(pack2<BF16>(x.x * f * unit, x.y * f * unit), pack2<BF16>(x.z * f * unit, x.w * f * unit));
         }
       }
     }
@@ -505,7 +545,7 @@ __global__ void __launch_bounds__(kThreads + 32, 3 - NB) attn_codes_rows_kernel(
 
 template <int D, int NB, bool BF16>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
-  constexpr int smem = rows_stages<D, NB>() * kT * D + 1024;
+  constexpr int smem = rows_stages<D>() * kT * D + 1024;
   RowsArgs ra;
   memcpy(&ra.mk, a.whole ? a.ok : a.wk, sizeof ra.mk);
   memcpy(&ra.mv, a.whole ? a.ov : a.wv, sizeof ra.mv);
@@ -517,7 +557,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   const int64_t cap = ((int64_t)a.pv.max_pages << a.pv.page_shift) / (kT / a.hc) + 2;
   const int64_t tiles = (int64_t)a.pv.B * (a.pv.Hkv / a.hc) * cap;
   const int64_t runs = a.whole ? tiles / cap : (tiles + kMinShare - 1) / kMinShare;
-  const int grid = (int)std::min<int64_t>(std::min((3 - NB) * a.sms, kRowsMaxCtas), runs);
+  const int grid = (int)std::min<int64_t>(std::min(2 * a.sms, kRowsMaxCtas), runs);
   e = launch_pdl(attn_codes_rows_kernel<D, NB, BF16>, dim3(grid), dim3(kThreads + 32), smem, st, ra);
   if (e != cudaSuccess || a.whole) return e;
   // a unit cut in pieces starts in a CTA of its own; eight of the joining CTAs
