@@ -128,46 +128,53 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
   auto swz = [&](int r) { return D == 128 ? r & 7 : r >> 1 & 3; };
 
   if (warp == kWarps) {
-    // -- copies: a lane per part of a tile, its page looked up two tiles ahead and
-    // its powers one; outside the pool reads as zeros.  Parts that no query sees (a
-    // window may begin inside a tile) have no page: their entries may be stale.
+    // -- copies: a lane per part of a tile, its page looked up two tiles ahead and its
+    // powers one; what is read is not touched before the next turn, as a look at it
+    // would wait for it.  Outside the pool reads as zeros.  Parts that no query sees
+    // (a window may begin inside a tile) have no page: their entries may be stale.
     struct Next {
-      int page, y, h;  // page < 0: not in the pool, to be told
+      int page, y, h;  // as found: -1 where no query sees it
+      bool seen;
     };
     auto look_up = [&](const At &x) {
       const int t = x.lo + x.t * pt + (lane << shift);
-      const bool seen = lane < parts && t < x.s.len && t + (1 << shift) > x.s.len - x.s.n - a.window + 1;
-      Next n = {pv.n_pages, t & ((1 << pv.page_shift) - 1), x.h * HC};
-      if (seen) {
-        n.page = pv.table[(int64_t)x.b * pv.max_pages + (t >> pv.page_shift)];
-        if ((unsigned)n.page >= (unsigned)pv.n_pages) n.page = -1;
+      Next n = {-1, t & ((1 << pv.page_shift) - 1), x.h * HC, lane < parts && t < x.s.len && t + (1 << shift) > x.s.len - x.s.n - a.window + 1};
+      n.page = load_if(pv.table + (int64_t)x.b * pv.max_pages + (t >> pv.page_shift), n.seen, -1);
+      return n;
+    };
+    auto checked = [&](Next n) {
+      if ((unsigned)n.page >= (unsigned)pv.n_pages) {
+        if (n.seen) set_err(pv.err, kErrPage);
+        n.page = pv.n_pages;
       }
       return n;
     };
     auto powers = [&](const Next &n, const int8_t *e) {
-      if ((unsigned)n.page >= (unsigned)pv.n_pages) return 0u;
       const int8_t *p = e + (int64_t)n.page * pv.Hkv + n.h;
-      return HC == 4 ? *reinterpret_cast<const uint32_t *>(p) : HC == 2 ? *reinterpret_cast<const uint16_t *>(p) : (uint32_t)(uint8_t)*p;
+      const bool in = n.page < pv.n_pages;
+      if (HC == 4) return (uint32_t)load_if(reinterpret_cast<const int32_t *>(p), in, 0);
+      if (HC == 2) return (uint32_t)load_if(reinterpret_cast<const uint16_t *>(p), in, 0);
+      return (uint32_t)load_if(reinterpret_cast<const uint8_t *>(p), in, 0);
     };
-    Next now = look_up(at), next = now;
-    uint32_t ek = powers(now, pv.ke), ev = powers(now, pv.ve);
     auto step = [&]() {
       if (++at.t >= at.nt) next_unit(a, units, at);
       return look_up(at);
     };
-    if (mine > 1) next = step();
+    Next now = look_up(at), found = now;
+    if (mine > 1) found = step();
+    now = checked(now);
+    uint32_t ek = powers(now, pv.ke), ev = powers(now, pv.ve);
     // (asked once: a limit from the arguments in the loop's waits cost 1.3 % in the 16-bit form)
     bool ok = !a.give_up;
     if (!ok && lane == 0) *abort_flag = 1;
     for (int w = 0; w < mine && ok; ++w) {
       uint32_t ek_next = 0, ev_next = 0;
-      Next after = next;
+      Next next = now;
       if (w + 1 < mine) {
+        next = checked(found);
         ek_next = powers(next, pv.ke), ev_next = powers(next, pv.ve);
-        if (w + 2 < mine) after = step();
+        if (w + 2 < mine) found = step();
       }
-      if (now.page < 0) set_err(pv.err, kErrPage);
-      const int page = now.page < 0 ? pv.n_pages : now.page;
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         int got = 1;
@@ -184,10 +191,10 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
         if (lane == 0) mbar_expect_tx(&s_full[stage], kTile);
         __syncwarp();
         if (lane < parts)
-          tma_load_4d(sm + stage * kTile + ((lane * HC) << shift) * D, kv ? &ra.mv : &ra.mk, 0, now.y, now.h, page, &s_full[stage]);
+          tma_load_4d(sm + stage * kTile + ((lane * HC) << shift) * D, kv ? &ra.mv : &ra.mk, 0, now.y, now.h, now.page, &s_full[stage]);
         next_stage();
       }
-      now = next, next = after, ek = ek_next, ev = ev_next;
+      now = next, ek = ek_next, ev = ev_next;
     }
     pdl_trigger();
     // the copies in flight land before the CTA ends, whoever waits for them: the

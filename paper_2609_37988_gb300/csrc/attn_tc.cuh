@@ -67,6 +67,10 @@ namespace {
 
 constexpr int kTcT = 128;                 // positions per tile, rows per query tile
 constexpr int kTcThreads = 384;
+// in 8 bits a warpgroup more that makes f16 tiles, and registers handed over
+constexpr int kExpand = 4;                // its warps, 12 on
+template <bool CODES>
+constexpr int tc_threads() { return CODES ? kTcThreads + 32 * kExpand : kTcThreads; }
 constexpr int kBox = 128 * 128;           // 64 channels x 128 rows
 constexpr int kErrTimeout = 8, kErrCount = 4, kErrPage = 32;  // KVK_DEVERR_*
 constexpr uint32_t kAll = 0xffffffffu;
@@ -115,7 +119,7 @@ struct Smem {
   static constexpr int kPows = D == 128 ? 8 : 16;      // tiles whose powers are kept
   static_assert(!CODES || (kStages + kRaw) / 2 + 3 <= kPows, "powers of the tiles in either ring and at work");
   static constexpr int kQ = 0, kRing = 2 * kTile, kRawRing = kRing + kStages * kTile, kBar = kRawRing + kRaw * kRawTile;
-  static constexpr int kBars = 3 * kStages + 17 + 2 * kRaw + 2;
+  static constexpr int kBars = 3 * kStages + 17 + 2 * kRaw + (CODES ? 2 : 0);
   static constexpr int kJob = kBar + 8 * kBars;        // two jobs
   static constexpr int kPow = kJob + 2 * (int)sizeof(Job);
   static constexpr int kSq = kPow + (CODES ? kPows * (int)sizeof(TilePow) : 0);  // a job's rows' factors
@@ -165,7 +169,7 @@ __device__ __forceinline__ int seq_tokens(const PagedView &v, int b, int &q0) {
 }
 
 template <int D, bool BF16, int SRC>
-__global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_constant__ TcArgs t) {
+__global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel(const __grid_constant__ TcArgs t) {
   constexpr bool PAGED = SRC != kPacked, CODES = SRC == kCodes;
   constexpr bool TB = BF16 && !CODES;  // type of the products' operands
   using SM = Smem<D, CODES>;
@@ -185,7 +189,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
            *sfull = jfree + 2, *pfull = sfull + 2, *odone = pfull + 4, *ofree = odone + 2, *vclean = ofree + 2,
            *drain = vclean + NS;
   // kCodes: codes landed, codes read; a job's queries in f16 (by its slot).  full is
-  // then the two warps' that make f16 tiles, free the products'.
+  // then the warps' that make f16 tiles, free the products'.
   uint64_t *rfull = drain + 1, *rfree = rfull + NR, *qready = rfree + NR;
   TilePow *pows = reinterpret_cast<TilePow *>(sm + SM::kPow);
   int8_t *sq = reinterpret_cast<int8_t *>(sm + SM::kSq);
@@ -200,11 +204,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
   if (tid == 0) {
     for (int i = 0; i < SM::kBars; ++i) {
       uint64_t *b = bar + i;
-      const int n = b >= jfree && b < jfree + 2 ? 11
+      const int n = b >= jfree && b < jfree + 2 ? (CODES ? 9 + kExpand : 11)
                     : (b >= pfull && b < pfull + 4) || (b >= ofree && b < ofree + 2) ? 4
                     : b >= vclean && b < vclean + NS ? 2
                     : b >= free_ && b < free_ + NS   ? (CODES ? 1 : 3)
-                    : CODES && ((b >= full && b < full + NS) || (b >= rfree && b < qready + 2)) ? 2
+                    : CODES && ((b >= full && b < full + NS) || (b >= rfree && b < qready + 2)) ? kExpand
                                                                                                : 1;
       mbar_init(b, n);
     }
@@ -234,6 +238,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     return false;
   };
 
+  if (warp >= 8) {
+  if constexpr (CODES) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcCodesRegs.regs[1]) : "memory");
   if (warp == 9) {
     // -- schedule and copies ---------------------------------------------------
     int s = 0;          // ring place and its round's parity
@@ -324,28 +330,37 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         return pv.n_pages;
       };
       if constexpr (CODES) {
-        // (a lane per part; pages looked up two tiles ahead, their powers one)
+        // A lane per part; pages looked up two tiles ahead, their powers one, and what is
+        // read is not touched before the next turn (a look at it would wait for it: a
+        // pair of tiles took 3000 cycles so).
         const int cshift = pv.page_shift, cparts = kTcT >> cshift;
-        auto find = [&](int jt) {
+        auto seen = [&](int jt) {
           const int pos = j.lo + jt * kTcT + (lane << cshift);
-          if (lane >= cparts || pos >= j.p0 + j.n || pos + (1 << cshift) <= j.first - a.window + 1) return pv.n_pages;
-          const int pg = pv.table[(int64_t)j.b * pv.max_pages + (pos >> cshift)];
+          return lane < cparts && pos < j.p0 + j.n && pos + (1 << cshift) > j.first - a.window + 1;
+        };
+        auto find = [&](int jt) {
+          return load_if(pv.table + (int64_t)j.b * pv.max_pages + ((j.lo + jt * kTcT + (lane << cshift)) >> cshift),
+                         jt < j.nt && seen(jt), -1);
+        };
+        auto page_at = [&](int pg, int jt) {  // what was found, n_pages where there is none
           if ((unsigned)pg < (unsigned)pv.n_pages) return pg;
-          set_err(pv.err, kErrPage);
+          if (jt < j.nt && seen(jt)) set_err(pv.err, kErrPage);
           return pv.n_pages;
         };
-        auto power = [&](int pg, const int8_t *e) {
-          return pg < pv.n_pages ? min(max((int)e[(int64_t)pg * pv.Hkv + j.h], pv.e_lo), pv.e_hi) : kNoPow;
-        };
+        auto power = [&](int pg, const int8_t *e) { return load_if(e + (int64_t)pg * pv.Hkv + j.h, pg < pv.n_pages, kNoPow); };
+        auto clamped = [&](int e) { return e == kNoPow ? e : min(max(e, pv.e_lo), pv.e_hi); };
         auto factor = [&](int d) {
           const int x = max(d + kRefUp, -14), y = max(d + kRefUp - x, -24);
           return (uint32_t)(15 + x) << 10 | (y >= -14 ? (uint32_t)(15 + y) << 10 : 1u << (24 + y)) << 16;
         };
-        int now = find(0), next = j.nt > 1 ? find(1) : pv.n_pages, vref = pv.e_lo;
-        int ek = power(now, pv.ke), ev = power(now, pv.ve);
+        int found = find(0), found_next = find(1), vref = pv.e_lo;
+        int now = page_at(found, 0);
+        int ek_read = power(now, pv.ke), ev_read = power(now, pv.ve);
         for (int jt = 0; jt < j.nt; ++jt) {
+          const int next = page_at(found_next, jt + 1);
           const int ek_next = power(next, pv.ke), ev_next = power(next, pv.ve);
-          const int after = jt + 2 < j.nt ? find(jt + 2) : pv.n_pages;
+          found_next = find(jt + 2);
+          const int ek = clamped(ek_read), ev = clamped(ev_read);
           const int kref = max(__reduce_max_sync(kAll, ek), pv.e_lo);
           vref = max(vref, __reduce_max_sync(kAll, ev));
 #pragma unroll
@@ -366,7 +381,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
               tma_load_4d(sm + SM::kRawRing + s * SM::kRawTile + (lane << cshift) * D, kv ? &t.mv : &t.mk, 0, 0, j.h, now, &rfull[s]);
             if (++s == NR) s = 0, ph ^= 1;
           }
-          now = next, next = after, ek = ek_next, ev = ev_next;
+          now = next, ek_read = ek_next, ev_read = ev_next;
         }
         return true;
       }
@@ -729,18 +744,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
     umma_commit_if(leader, drain);
     mbar_wait(drain, 0, kWaits);
     __syncwarp();
-  } else if (CODES && warp >= 10) {
-    // -- f16 tiles of codes: a warp has 64 rows of each ------------------------------
+  } else if (CODES && warp >= 12) {
+    // -- f16 tiles of codes: a warp has 32 rows of each ------------------------------
+    // (Two warps for keys and two for values took longer: a tile's way is what counts.)
     // A lane takes 16 codes of a row: piece cc, two pieces in f16.  D = 64: 8 rows at a
     // time, a row's pieces on neighbouring lanes.  D = 128: 4 rows, of 8 that take two
     // turns; rows b and b ^ 5 of either half's four pieces stand on 8 neighbouring
     // lanes, so that neither their codes nor the f16 pieces meet on a bank.
     constexpr bool wide = D == 128;
-    const int w = warp - 10, cc = (lane & 3) | (wide ? lane >> 1 & 4 : 0);
+    const int w = warp - 12, cc = (lane & 3) | (wide ? lane >> 1 & 4 : 0);
     int at_raw[2], at_f16[2];  // of a row in either turn
 #pragma unroll
     for (int y = 0; y < 2; ++y) {
-      const int r = 64 * w + (wide ? (lane & 4 ? 5 : 0) ^ (lane & 16 ? 2 : 0) ^ y : lane >> 2);
+      const int r = 32 * w + (wide ? (lane & 4 ? 5 : 0) ^ (lane & 16 ? 2 : 0) ^ y : lane >> 2);
       at_raw[y] = r * D + ((cc ^ (wide ? r & 7 : r >> 1 & 3)) << 4);
       at_f16[y] = (cc >> 2) * kBox + r * 128 + (((2 * (cc & 3)) ^ (r & 7)) << 4);
     }
@@ -753,13 +769,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       const int nt = js.b < 0 ? -1 : js.nt, lo = js.lo, first = js.first, low = js.low, tile0 = js.tile0, two = js.two;
       bool ok = true;
       if (BF16 && nt > 0) {
-        // the job's queries: two rows of either tile a lane
+        // the job's queries: a row of either tile a lane
         if (!wait(qfull, loads)) break;
         loads ^= 1;
 #pragma unroll 1
-        for (int x = 0; x < (two ? 4 : 2); ++x) {
-          const int r = (x & 1) * 64 + 32 * w + lane;
-          uint8_t *row = sm + SM::kQ + (x >> 1) * SM::kTile + r * 128;
+        for (int x = 0; x < 1 + two; ++x) {
+          const int r = 32 * w + lane;
+          uint8_t *row = sm + SM::kQ + x * SM::kTile + r * 128;
           auto piece = [&](int y) { return reinterpret_cast<uint4 *>(row + (y >> 3) * kBox + (((y & 7) ^ (r & 7)) << 4)); };
           uint32_t top = 0;  // magnitudes of either half
 #pragma unroll
@@ -781,7 +797,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
             }
             *p = make_uint4(u[0], u[1], u[2], u[3]);
           }
-          sq[(slot * 2 + (x >> 1)) * kTcT + r] = (int8_t)-e;
+          sq[(slot * 2 + x) * kTcT + r] = (int8_t)-e;
         }
         fence_proxy_async();
         __syncwarp();
@@ -793,62 +809,56 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
         const bool partial = t0 + kTcT - 1 > first || t0 < low;
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv) {
-          if (!(ok = wait(&rfull[rs], rph) && wait(&free_[s], ph ^ 1))) break;
+          if (!(ok = wait(&rfull[rs], rph))) break;
           const uint8_t *src = sm + SM::kRawRing + rs * SM::kRawTile;
           uint8_t *dst = sm + SM::kRing + s * SM::kTile;
           const uint32_t *fac = kv ? tp->vf : tp->kf;
+          const bool far = kv ? tp->vfar : tp->kfar;
           bool fine = true;
-          auto go = [&](auto FAR, auto LOOK) {
-            constexpr int N = wide ? 4 : 2;  // times for 16 rows, which have one factor
+          constexpr int N = wide ? 4 : 2;  // times for 16 rows, which have one factor
+          uint4 u[2 * N];
+          uint32_t f[2];
 #pragma unroll
-            for (int q = 0; q < 4; q += 2) {
-              uint4 u[2 * N];
-              uint32_t f[2];
+          for (int y = 0; y < 2 * N; ++y)
+            u[y] = *reinterpret_cast<const uint4 *>(src + at_raw[wide ? y & 1 : 0] + (y >> (wide ? 1 : 0)) * (8 * D));
 #pragma unroll
-              for (int y = 0; y < 2 * N; ++y)
-                u[y] = *reinterpret_cast<const uint4 *>(src + at_raw[wide ? y & 1 : 0] + (N * q + y >> (wide ? 1 : 0)) * (8 * D));
+          for (int y = 0; y < 2; ++y) f[y] = fac[(32 * w + 16 * y) >> pv.page_shift];
+          auto make = [&](auto FAR, auto LOOK) {
 #pragma unroll
-              for (int y = 0; y < 2; ++y) f[y] = fac[(64 * w + 16 * (q + y)) >> pv.page_shift];
+            for (int y = 0; y < 2 * N; ++y) {
+              uint32_t v[4] = {u[y].x, u[y].y, u[y].z, u[y].w};
+              if constexpr (decltype(LOOK)::value) {
 #pragma unroll
-              for (int y = 0; y < 2 * N; ++y) {
-                uint32_t v[4] = {u[y].x, u[y].y, u[y].z, u[y].w};
-                if constexpr (decltype(LOOK)::value) {
-#pragma unroll
-                  for (int z = 0; z < 4; ++z) {
-                    const uint32_t bad = ((v[z] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // a NaN's top bit
-                    fine = fine && bad == 0;
-                    v[z] &= ~((bad >> 7) * 255u);
-                  }
+                for (int z = 0; z < 4; ++z) {
+                  const uint32_t bad = ((v[z] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;  // a NaN's top bit
+                  fine = fine && bad == 0;
+                  v[z] &= ~((bad >> 7) * 255u);
                 }
-                const uint32_t f1 = __byte_perm(f[y / N], 0, 0x1010);
-                uint32_t h[8];
-#pragma unroll
-                for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(code2_f16(z & 1 ? v[z >> 1] >> 16 : v[z >> 1]), f1);
-                if constexpr (decltype(FAR)::value) {
-                  const uint32_t f2 = __byte_perm(f[y / N], 0, 0x3232);
-#pragma unroll
-                  for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(h[z], f2);
-                }
-                uint8_t *to = dst + (N * q + y >> (wide ? 1 : 0)) * (8 * 128);
-                const int at = at_f16[wide ? y & 1 : 0];
-                *reinterpret_cast<uint4 *>(to + at) = make_uint4(h[0], h[1], h[2], h[3]);
-                *reinterpret_cast<uint4 *>(to + (at ^ 16)) = make_uint4(h[4], h[5], h[6], h[7]);
               }
+              const uint32_t f1 = __byte_perm(f[y / N], 0, 0x1010);
+              uint32_t h[8];
+#pragma unroll
+              for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(code2_f16(z & 1 ? v[z >> 1] >> 16 : v[z >> 1]), f1);
+              if constexpr (decltype(FAR)::value) {
+                const uint32_t f2 = __byte_perm(f[y / N], 0, 0x3232);
+#pragma unroll
+                for (int z = 0; z < 8; ++z) h[z] = hmul2_u32(h[z], f2);
+              }
+              uint8_t *to = dst + (y >> (wide ? 1 : 0)) * (8 * 128);
+              const int at = at_f16[wide ? y & 1 : 0];
+              *reinterpret_cast<uint4 *>(to + at) = make_uint4(h[0], h[1], h[2], h[3]);
+              *reinterpret_cast<uint4 *>(to + (at ^ 16)) = make_uint4(h[4], h[5], h[6], h[7]);
             }
           };
+          if (!(ok = wait(&free_[s], ph ^ 1))) break;
           constexpr std::integral_constant<bool, false> no;
           constexpr std::integral_constant<bool, true> yes;
-          const bool far = kv ? tp->vfar : tp->kfar;
-          if (kv && partial) {
-            if (far)
-              go(yes, yes);
-            else
-              go(no, yes);
-          } else if (far) {
-            go(yes, no);
-          } else {
-            go(no, no);
-          }
+          if (kv && partial)
+            make(yes, yes);
+          else if (far)
+            make(yes, no);
+          else
+            make(no, no);
           if (!fine) js.bad = 1;
           fence_proxy_async();
           __syncwarp();
@@ -865,7 +875,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       if (nt < 0 || !ok) break;
     }
     __syncwarp();
-  } else if (warp >= 10) {
+  } else if (!CODES && warp >= 10) {
     // -- values of partly seen tiles ----------------------------------------------
     int s = 0;
     uint32_t ph = 0;
@@ -920,8 +930,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attn_tc_kernel(const __grid_con
       if (lane == 0) mbar_arrive(&jfree[slot]);
       if (nt < 0 || !ok) break;
     }
+  }
   } else {
     // -- softmax and results: a thread per row of query tile i -----------------------
+    if constexpr (CODES) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcCodesRegs.regs[0]) : "memory");
     const int i = warp >> 2;
     const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t ts = tS + 128 * i + lane_off, to = tO + D * i + lane_off;
@@ -1271,6 +1283,9 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   constexpr bool PAGED = SRC != kPacked;
   constexpr int smem = Smem<D, SRC == kCodes>::kBytes;
   cudaError_t e = allow_smem<&attn_tc_kernel<D, BF16, SRC>>(smem, a.device);
+  if constexpr (SRC == kCodes) {
+    if (e == cudaSuccess) e = check_reg_split<&attn_tc_kernel<D, BF16, SRC>>(kTcCodesRegs);
+  }
   if (e != cudaSuccess) return e;
   TcArgs t;
   t.a = a;
@@ -1304,9 +1319,9 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   const double rows = (double)std::min<int64_t>(2 * t.P, share) * a.G / (2 * kTcT);
   t.a.runs = PAGED && waves < 4 && idle > 5 + 0.12 * std::min(full, (double)a.sms) * rows;
   if (!t.a.runs)
-    return launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(kTcThreads), smem, st, t);
+    return launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(tc_threads<SRC == kCodes>()), smem, st, t);
   const int grid = std::min(a.sms, kTcMaxCtas);
-  e = launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3(grid), dim3(kTcThreads), smem, st, t);
+  e = launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3(grid), dim3(tc_threads<SRC == kCodes>()), smem, st, t);
   if (e != cudaSuccess) return e;
   // a CTA's run cuts off the start of one job at most
   const int64_t cut = std::min<int64_t>(jobs, grid);

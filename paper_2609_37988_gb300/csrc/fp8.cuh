@@ -4,6 +4,22 @@
 
 namespace kvk {
 
+// What stands at p, or `other` where `in` is not set, by one predicated load: a value
+// chosen behind the load would be a look at it, which waits for it.
+#define KVK_LOAD_IF(name, T, op)                                                                              \
+  __device__ __forceinline__ int name(const T *p, bool in, int other) {                                      \
+    int r;                                                                                                    \
+    asm volatile("{\n .reg .pred q;\n setp.ne.u32 q, %2, 0;\n mov.b32 %0, %3;\n @q ld.global." op " %0, [%1];\n}\n" \
+                 : "=&r"(r)                                                                                   \
+                 : "l"(p), "r"(in ? 1u : 0u), "r"(other));                                                    \
+    return r;                                                                                                 \
+  }
+KVK_LOAD_IF(load_if, int32_t, "s32")
+KVK_LOAD_IF(load_if, uint16_t, "u16")
+KVK_LOAD_IF(load_if, uint8_t, "u8")
+KVK_LOAD_IF(load_if, int8_t, "s8")
+#undef KVK_LOAD_IF
+
 // 2^e, -126 <= e <= 127
 __device__ __forceinline__ float pow2f(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 

@@ -27,4 +27,7 @@ constexpr RegSplit kEvictRegs{{512, 256, 128}, {88, 56, 40}};
 // decode over quantised latents: softmax; products; expansion (512 x 128 launched)
 constexpr RegSplit kMlaQRegs{{128, 128, 256}, {256, 96, 80}};
 
+// chunks over pages in 8 bits: softmax; schedule, products and expansion (512 x 128 launched)
+constexpr RegSplit kTcCodesRegs{{256, 256, 0}, {168, 88, 0}};
+
 }  // namespace kvk

@@ -1,6 +1,8 @@
 """Refusals of the paged cache in 8 bits and of the operators on pages that need no
 GPU, through the C ABI and the binding."""
 import ctypes
+import os
+import subprocess
 
 import pytest
 import torch
@@ -60,6 +62,17 @@ def test_null_handles(lib):
     assert so.kvk_paged_copy(None, 256, 256, 1, None) == INVALID
     assert so.kvk_paged_fork(None, 256, 256, 256, 1, 1, 256, 256, 1, 256, 512, 1, None) == INVALID
     assert so.kvk_paged_compact(None, 256, 256, 256, 1, 1, 256, 256, 256, None, None) == INVALID
+
+
+def test_chunks_hand_registers_over_as_they_were_launched(tmp_path):
+    """512 x 128 = 256 x 168 + 256 x 88, allocated in units of 8 a thread."""
+    csrc = os.path.join(os.path.dirname(kbuild.__file__), "csrc")
+    src, exe = tmp_path / "split.cpp", tmp_path / "split"
+    src.write_text('#include "regsplit.h"\n#include <cstdio>\n'
+                   'int main() { for (int r = 1; r < 256; ++r) if (kvk::kTcCodesRegs.fits(r)) std::printf("%d ", r); }\n')
+    subprocess.run(["g++", "-std=c++17", "-I", csrc, str(src), "-o", str(exe)], check=True)
+    got = subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()
+    assert [int(x) for x in got] == list(range(121, 129))
 
 
 def test_binding_checks_pools():
