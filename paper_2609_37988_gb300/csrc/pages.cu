@@ -52,6 +52,67 @@ __device__ __forceinline__ int held(const PagesArgs &a, int b) {
   return (int)min((int64_t)max(a.lens[b], 0), (int64_t)a.max_pages << a.page_shift);
 }
 
+constexpr int kPiece = 8192;  // bytes that a CTA copies at a time, 32 a thread
+
+// Pieces [first, end) of page s, of the pools of all layers one behind another, to
+// page d; with piece 0 of a pool its powers.
+template <bool CODED>
+__device__ void copy_page(const CopyArgs &a, int s, int d, int first, int end) {
+  const int tid = threadIdx.x, pieces = (int)((a.bytes + kPiece - 1) / kPiece);
+  if (s == d) return;
+  constexpr int U = 4;
+  for (int w0 = first; w0 < end; w0 += U) {
+    uint4 u[U], v[U];
+    uint8_t *to[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int w = w0 + i, pool = w / pieces, piece = w - pool * pieces, l = pool >> 1;
+      const int64_t off = (int64_t)piece * kPiece + 32 * tid;
+      to[i] = nullptr;
+      if (w >= end || off >= a.bytes) continue;
+      uint8_t *x = pool & 1 ? a.v[l] : a.k[l];
+      const uint4 *from = reinterpret_cast<const uint4 *>(x + s * a.bytes + off);
+      u[i] = from[0], v[i] = from[1];
+      to[i] = x + d * a.bytes + off;
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+      if (to[i]) st_sector(to[i], u[i], v[i]);
+    if (CODED) {
+#pragma unroll 1
+      for (int w = w0; w < min(w0 + U, end); ++w) {
+        const int pool = w / pieces;
+        if (w != pool * pieces) continue;
+        int8_t *e = pool & 1 ? a.ve[pool >> 1] : a.ke[pool >> 1];
+        for (int h = tid; h < a.Hkv; h += kThreads) e[(int64_t)d * a.Hkv + h] = e[(int64_t)s * a.Hkv + h];
+      }
+    }
+  }
+}
+
+// A CTA's part of a list of pages to copy: entry by entry, so many pieces at a time.
+template <bool CODED>
+__device__ void copy_list(const CopyArgs &a, int n, int share) {
+  const int pieces = (int)((a.bytes + kPiece - 1) / kPiece) * 2 * a.layers, shares = (pieces + share - 1) / share;
+  for (int64_t w = blockIdx.x; w < (int64_t)shares * n; w += gridDim.x) {
+    const int i = (int)(w / shares), part = (int)(w - (int64_t)i * shares);
+    const int s = a.src[i], d = a.dst[i];
+    if (s == -1 || d == -1) continue;
+    if ((unsigned)s >= (unsigned)a.n_pages || (unsigned)d >= (unsigned)a.n_pages) {
+      if (threadIdx.x == 0) set_err(a.err, kErrPage);
+      continue;
+    }
+    copy_page<CODED>(a, s, d, part * share, min((part + 1) * share, pieces));
+  }
+}
+
+template <bool CODED>
+__global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a, int share) {
+  pdl_wait();
+  copy_list<CODED>(a, a.n_dev ? *a.n_dev : a.n, share);
+  pdl_trigger();
+}
+
 // This thread's pages of chunk c and how many of them are used; the chunk's holders
 // are kept as they are before the call (refs_out may be refs).
 __device__ int count_chunk(const PagesArgs &a, int c, int32_t *keep) {
@@ -103,15 +164,16 @@ __global__ void __launch_bounds__(kThreads) fork_count_kernel(const PagesArgs a,
       // A page that is not full will be written to: it stays with the first row that
       // has it so if nobody else holds it and no row has it full.
       bool shared = false;
+      const int page = a.table[(int64_t)r.parent * a.max_pages + r.old - 1];
+#pragma unroll 4
       for (int j = lane; j < a.R; j += 32) {
+        if (a.parents[j] != r.parent || j == i) continue;
         int p, o, w;
         bool op;
-        if (j == i) continue;
         fork_row(a, j, p, o, w, op);
-        if (p == r.parent) shared = shared || o > r.old || (o == r.old && (!op || j < i));
+        shared = shared || o > r.old || (o == r.old && (!op || j < i));
       }
       shared = __any_sync(kAll, shared);
-      const int page = a.table[(int64_t)r.parent * a.max_pages + r.old - 1];
       if ((unsigned)page < (unsigned)a.n_pages && (shared || a.refs[page] != 1)) r.copy = page;
     }
     if (lane == 0) {
@@ -125,12 +187,53 @@ __global__ void __launch_bounds__(kThreads) fork_count_kernel(const PagesArgs a,
   pdl_trigger();
 }
 
-// A CTA per row: the given one lets go of its pages, the new one takes its own.
-__global__ void __launch_bounds__(kThreads) fork_rows_kernel(const PagesArgs a) {
+// Free pages number base .. base + need - 1 to `give(k, page)`; how many there were.
+// Every thread of the CTA calls it.
+template <typename F>
+__device__ int take_free(const PagesArgs &a, int base, int need, F give) {
   __shared__ int s_chunk, s_before;
-  const int tid = threadIdx.x, lane = tid & 31, r = blockIdx.x;
+  const int tid = threadIdx.x;
+  const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
+  // the chunk with free page number `base`
+  if (tid == 0) s_chunk = chunks, s_before = base;
+  for (int c0 = 0, before = 0, total; c0 < chunks && before <= base; c0 += kThreads, before += total) {
+    const int x = c0 + tid < chunks ? a.chunk[c0 + tid] : 0, at = before + scan_cta(x, total);
+    if (at <= base && base < at + x) s_chunk = c0 + tid, s_before = at;
+  }
+  __syncthreads();
+  int before = s_before;
+  for (int c = s_chunk; c < chunks && before < base + need; ++c) {
+    bool is_free[kPer];
+    int n = 0, total;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = c * kPageChunk + kPer * tid + i;
+      is_free[i] = p < a.n_pages && a.before[p] <= 0;
+      n += is_free[i];
+    }
+    int k = before + scan_cta(n, total) - base;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      if (!is_free[i]) continue;
+      if (k >= 0 && k < need) give(k, c * kPageChunk + kPer * tid + i);
+      ++k;
+    }
+    before += total;
+  }
+  return min(max(before - base, 0), need);
+}
+
+// A CTA per given row, which lets go of its pages, and one per new row, which takes its
+// own.  Those beside a new row's (gridDim.y) copy a share of its copied page, as it does.
+template <bool CODED>
+__global__ void __launch_bounds__(kThreads) fork_rows_kernel(const PagesArgs a, const __grid_constant__ CopyArgs copy, int share) {
+  __shared__ int s_to;
+  const int tid = threadIdx.x, r = (int)blockIdx.x - a.B;
+  const bool main = blockIdx.y == 0;
   pdl_wait();
-  if (r < a.B) {
+  if (tid == 0) s_to = -1;
+  if (main && r < 0) {
+    const int r = blockIdx.x;
     const int n = pages_of(a, held(a, r));
     if (tid == 0 && (int64_t)a.lens[r] > (int64_t)a.max_pages << a.page_shift) set_err(a.err, kErrCount);
     for (int j = tid; j < n; j += kThreads) {
@@ -144,83 +247,55 @@ __global__ void __launch_bounds__(kThreads) fork_rows_kernel(const PagesArgs a) 
       }
     }
   }
-  if (r < a.R) {
+  if (r >= 0) {
     const ForkRow row = a.rows[r];
-    const int copied = row.copy >= 0, fresh_from = row.old - copied, need = row.want - fresh_from;
+    const int copied = row.copy >= 0, fresh_from = row.old - copied, need = main ? row.want - fresh_from : copied;
     int32_t *out = a.table_out + (int64_t)r * a.width;
-    for (int j = tid; j < a.width; j += kThreads) {
-      if (j < fresh_from) {
-        const int page = a.table[(int64_t)row.parent * a.max_pages + j];
-        if ((unsigned)page < (unsigned)a.n_pages) atomicAdd(&a.refs_out[page], 1);
-        out[j] = page;
-      } else if (j >= row.want) {
-        out[j] = -1;
-      }
-    }
-    if (tid == 0) {
-      a.src[r] = row.copy;
-      a.dst[r] = -1;
-    }
+    // free pages that the rows before take
+    int mine = 0;
     if (need > 0) {  // (the same for the CTA)
-      // free pages that the rows before take
-      int mine = 0, base;
+#pragma unroll 4
       for (int j = tid; j < r; j += kThreads) {
         const ForkRow x = a.rows[j];
         mine += x.want - x.old + (x.copy >= 0);
       }
-      scan_cta(mine, base);
-      // the chunk with free page number `base`
-      const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
-      if (tid < 32) {
-        int before = 0, c0 = 0;
-        for (; c0 < chunks; c0 += 32) {
-          const int x = c0 + lane < chunks ? a.chunk[c0 + lane] : 0;
-          int sum = x;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const int y = __shfl_up_sync(kAll, sum, o);
-            if (lane >= o) sum += y;
-          }
-          const uint32_t past = __ballot_sync(kAll, before + sum > base);
-          if (past) {
-            const int f = __ffs(past) - 1;
-            before += __shfl_sync(kAll, sum - x, f);
-            c0 += f;
-            break;
-          }
-          before += __shfl_sync(kAll, sum, 31);
+    }
+    if (main) {
+      for (int j = tid; j < a.width; j += kThreads) {
+        if (j < fresh_from) {
+          const int page = a.table[(int64_t)row.parent * a.max_pages + j];
+          if ((unsigned)page < (unsigned)a.n_pages) atomicAdd(&a.refs_out[page], 1);
+          out[j] = page;
+        } else if (j >= row.want) {
+          out[j] = -1;
         }
-        if (lane == 0) s_chunk = c0, s_before = before;
+      }
+    }
+    if (need > 0) {
+      int base;
+      scan_cta(mine, base);
+      const int got = take_free(a, base, need, [&](int k, int p) {
+        if (main) {
+          out[fresh_from + k] = p;
+          a.refs_out[p] = 1;
+        }
+        if (copied && k == 0) s_to = p;
+      });
+      if (main) {  // those that no page is left for
+        for (int j = fresh_from + got + tid; j < row.want; j += kThreads) out[j] = -1;
+        if (got < need && tid == 0) set_err(a.err, kErrCapacity);
       }
       __syncthreads();
-      int c = s_chunk, before = s_before;
-      for (; c < chunks && before < base + need; ++c) {
-        bool is_free[kPer];
-        int n = 0, total;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int p = c * kPageChunk + kPer * tid + i;
-          is_free[i] = p < a.n_pages && a.before[p] <= 0;
-          n += is_free[i];
-        }
-        int k = before + scan_cta(n, total) - base;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          if (!is_free[i]) continue;
-          if (k >= 0 && k < need) {
-            const int p = c * kPageChunk + kPer * tid + i;
-            out[fresh_from + k] = p;
-            a.refs_out[p] = 1;
-            if (copied && k == 0) a.dst[r] = p;
-          }
-          ++k;
-        }
-        before += total;
-      }
-      // those that no page is left for
-      const int got = min(max(before - base, 0), need);
-      for (int j = fresh_from + got + tid; j < row.want; j += kThreads) out[j] = -1;
-      if (got < need && tid == 0) set_err(a.err, kErrCapacity);
+    }
+    const int to = s_to;
+    if (main && tid == 0) {  // for the layers of other launches
+      a.src[r] = row.copy;
+      a.dst[r] = to;
+    }
+    if (copied && to >= 0) {
+      const int pieces = (int)((copy.bytes + kPiece - 1) / kPiece) * 2 * copy.layers;
+      const int first = blockIdx.y * share;
+      if (first < pieces) copy_page<CODED>(copy, row.copy, to, first, min(first + share, pieces));
     }
   }
   pdl_trigger();
@@ -235,22 +310,34 @@ __global__ void __launch_bounds__(kThreads) compact_count_kernel(const PagesArgs
 }
 
 // Which page goes where: used page number k at or behind the used count to free
-// page number k before it.
+// page number k before it.  COUNTED: by the chunks' counts; otherwise every CTA
+// counts all pages, 4 a load, the holders being refs itself.
+template <bool COUNTED>
 __global__ void __launch_bounds__(kThreads) compact_moves_kernel(const PagesArgs a) {
   const int tid = threadIdx.x, c = blockIdx.x, chunks = gridDim.x;
   int mine = 0, all = 0, before, used, low_before, x;
   pdl_wait();
-  for (int i = tid; i < chunks; i += kThreads) {
-    const int n = a.chunk[i];
-    all += n;
-    if (i < c) mine += n;
+  if (COUNTED) {
+    for (int i = tid; i < chunks; i += kThreads) {
+      const int n = a.chunk[i];
+      all += n;
+      if (i < c) mine += n;
+    }
+  } else {
+#pragma unroll 8
+    for (int p = tid; p < a.n_pages; p += kThreads) {
+      const int n = a.before[p] > 0;
+      all += n;
+      if (p < c * kPageChunk) mine += n;
+    }
   }
   scan_cta(mine, before);
   scan_cta(all, used);
   // used pages before number `used`
-  const int edge = used / kPageChunk;
+  const int edge = COUNTED ? used / kPageChunk : 0;
   int low = 0;
   for (int i = tid; i < edge; i += kThreads) low += a.chunk[i];
+#pragma unroll 8
   for (int p = edge * kPageChunk + tid; p < used; p += kThreads) low += a.before[p] > 0;
   scan_cta(low, low_before);
   bool in[kPer];
@@ -288,8 +375,9 @@ __global__ void __launch_bounds__(kThreads) compact_moves_kernel(const PagesArgs
   pdl_trigger();
 }
 
-// The moved pages' numbers and holders, the table.
-__global__ void __launch_bounds__(kThreads) compact_apply_kernel(const PagesArgs a) {
+// The moved pages' numbers and holders, the table, the pages.
+template <bool CODED>
+__global__ void __launch_bounds__(kThreads) compact_apply_kernel(const PagesArgs a, const __grid_constant__ CopyArgs copy, int share) {
   pdl_wait();
   const int n = *a.n_moved;
   const int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x, step = (int64_t)gridDim.x * kThreads;
@@ -323,69 +411,66 @@ __global__ void __launch_bounds__(kThreads) compact_apply_kernel(const PagesArgs
     }
     a.table_out[e] = to;
   }
-  pdl_trigger();
-}
-
-constexpr int kPiece = 8192;  // bytes
-
-// Pieces of pages: a CTA copies 32 bytes a thread at a time.
-template <bool CODED>
-__global__ void __launch_bounds__(kThreads) copy_pages_kernel(const __grid_constant__ CopyArgs a) {
-  const int tid = threadIdx.x;
-  pdl_wait();
-  const int n = a.n_dev ? *a.n_dev : a.n;
-  const int pieces = (int)((a.bytes + kPiece - 1) / kPiece), pools = 2 * a.layers;
-  const int64_t per = (int64_t)pools * pieces, total = per * n;
-  for (int64_t w = blockIdx.x; w < total; w += gridDim.x) {
-    const int i = (int)(w / per), rest = (int)(w - i * per), pool = rest / pieces, piece = rest - pool * pieces;
-    const int s = a.src[i], d = a.dst[i];
-    if (s == -1 || d == -1) continue;
-    if ((unsigned)s >= (unsigned)a.n_pages || (unsigned)d >= (unsigned)a.n_pages) {
-      if (tid == 0) set_err(a.err, kErrPage);
-      continue;
-    }
-    if (s == d) continue;
-    const int l = pool >> 1;
-    uint8_t *x = pool & 1 ? a.v[l] : a.k[l];
-    const int64_t off = (int64_t)piece * kPiece + 32 * tid;
-    if (off < a.bytes) {
-      const uint4 *from = reinterpret_cast<const uint4 *>(x + s * a.bytes + off);
-      const uint4 u = from[0], v = from[1];
-      st_sector(x + d * a.bytes + off, u, v);
-    }
-    if (CODED && piece == 0) {
-      int8_t *e = pool & 1 ? a.ve[l] : a.ke[l];
-      for (int h = tid; h < a.Hkv; h += kThreads) e[(int64_t)d * a.Hkv + h] = e[(int64_t)s * a.Hkv + h];
-    }
-  }
+  copy_list<CODED>(copy, n, share);
   pdl_trigger();
 }
 
 }  // namespace
 
+namespace {
+int64_t pieces_of(const CopyArgs &c) { return (c.bytes + kPiece - 1) / kPiece * 2 * c.layers; }
+// Pieces that a CTA takes of a page at once: 64 KB, fewer where that would leave SMs
+// without work.
+int share_of(const CopyArgs &c, int64_t pages, int sms) {
+  int share = 8;
+  while (share > 1 && pages * ((pieces_of(c) + share - 1) / share) < 4 * sms) share /= 2;
+  return share;
+}
+}  // namespace
+
 cudaError_t launch_copy_pages(const CopyArgs &a, bool coded, int sms, cudaStream_t st) {
-  const int64_t pieces = (a.bytes + kPiece - 1) / kPiece * 2 * a.layers * a.n;
-  if (pieces == 0) return cudaSuccess;
-  const dim3 grid((unsigned)std::min<int64_t>(pieces, (int64_t)8 * sms));
-  return launch_pdl(coded ? copy_pages_kernel<true> : copy_pages_kernel<false>, grid, dim3(kThreads), 0, st, a);
+  const int share = share_of(a, a.n, sms);
+  const int64_t items = (pieces_of(a) + share - 1) / share * a.n;
+  if (items == 0) return cudaSuccess;
+  const dim3 grid((unsigned)std::min<int64_t>(items, (int64_t)8 * sms));
+  return launch_pdl(coded ? copy_pages_kernel<true> : copy_pages_kernel<false>, grid, dim3(kThreads), 0, st, a, share);
 }
 
-cudaError_t launch_fork(const PagesArgs &a, cudaStream_t st) {
-  const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
+cudaError_t launch_fork(const PagesArgs &a, const CopyArgs &copy, bool coded, int sms, cudaStream_t st) {
+  const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk, rows = a.B + a.R;
   cudaError_t e = launch_pdl(fork_count_kernel, dim3(chunks + (a.R + kThreads / 32 - 1) / (kThreads / 32)), dim3(kThreads), 0, st, a,
                              chunks);
-  if (e != cudaSuccess || std::max(a.B, a.R) == 0) return e;
-  return launch_pdl(fork_rows_kernel, dim3(std::max(a.B, a.R)), dim3(kThreads), 0, st, a);
+  if (e != cudaSuccess || rows == 0) return e;
+  // CTAs beside a row's own: 64 KB of its copied page each
+  const int share = share_of(copy, std::max(a.R, 1), sms);
+  const int64_t beside = a.R ? std::min<int64_t>((pieces_of(copy) + share - 1) / share, 65535) : 1;
+  const int each = (int)((pieces_of(copy) + beside - 1) / beside);
+  return launch_pdl(coded ? fork_rows_kernel<true> : fork_rows_kernel<false>, dim3(rows, (unsigned)beside), dim3(kThreads), 0, st, a,
+                    copy, each);
 }
 
-cudaError_t launch_compact(const PagesArgs &a, cudaStream_t st) {
+// Pools up to this size are counted by every CTA for itself, which saves a launch
+// (2047 pages: XX us for YY); not where the counts change in place meanwhile.
+constexpr int kCountAll = 32768;
+
+cudaError_t launch_compact(const PagesArgs &in, const CopyArgs &copy, bool coded, int sms, cudaStream_t st) {
+  PagesArgs a = in;
   const int chunks = (a.n_pages + kPageChunk - 1) / kPageChunk;
-  cudaError_t e = launch_pdl(compact_count_kernel, dim3(chunks), dim3(kThreads), 0, st, a);
-  if (e == cudaSuccess) e = launch_pdl(compact_moves_kernel, dim3(chunks), dim3(kThreads), 0, st, a);
+  const bool apart = a.refs_out + a.n_pages <= a.refs || a.refs + a.n_pages <= a.refs_out;
+  cudaError_t e = cudaSuccess;
+  if (apart && a.n_pages <= kCountAll) {
+    a.before = const_cast<int32_t *>(a.refs);  // (only read from here on)
+    e = launch_pdl(compact_moves_kernel<false>, dim3(chunks), dim3(kThreads), 0, st, a);
+  } else {
+    e = launch_pdl(compact_count_kernel, dim3(chunks), dim3(kThreads), 0, st, a);
+    if (e == cudaSuccess) e = launch_pdl(compact_moves_kernel<true>, dim3(chunks), dim3(kThreads), 0, st, a);
+  }
   if (e != cudaSuccess) return e;
-  const int64_t work = std::max<int64_t>((int64_t)a.B * a.width, a.n_pages / 2);
-  return launch_pdl(compact_apply_kernel, dim3((unsigned)std::min<int64_t>((work + kThreads - 1) / kThreads, 1024)), dim3(kThreads), 0,
-                    st, a);
+  const int share = share_of(copy, a.n_pages / 4, sms);
+  const int64_t work = std::max(((int64_t)a.B * a.width + kThreads - 1) / kThreads,
+                                (int64_t)(a.n_pages / 2) * ((pieces_of(copy) + share - 1) / share));
+  return launch_pdl(coded ? compact_apply_kernel<true> : compact_apply_kernel<false>,
+                    dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(work, (int64_t)8 * sms))), dim3(kThreads), 0, st, a, copy, share);
 }
 
 }  // namespace kvk

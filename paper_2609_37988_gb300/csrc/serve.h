@@ -149,8 +149,9 @@ struct CopyArgs {
   int64_t bytes;              // of a page of a pool
   int32_t *err;
 };
-cudaError_t launch_fork(const PagesArgs &a, cudaStream_t st);
-cudaError_t launch_compact(const PagesArgs &a, cudaStream_t st);
+// (with the pages of copy's layers; their lists stay in the workspace for others)
+cudaError_t launch_fork(const PagesArgs &a, const CopyArgs &copy, bool coded, int sms, cudaStream_t st);
+cudaError_t launch_compact(const PagesArgs &a, const CopyArgs &copy, bool coded, int sms, cudaStream_t st);
 // up to kCopyLayers layers; coded: their powers too
 cudaError_t launch_copy_pages(const CopyArgs &a, bool coded, int sms, cudaStream_t st);
 

@@ -204,27 +204,30 @@ PagesArgs pages_args(const kvk_paged *p) {
   return a;
 }
 
-// Pages of all layers, `n` entries at most (n_dev: as many as it says).
-cudaError_t copy_layers(const kvk_paged *p, const int32_t *src, const int32_t *dst, int n, const int32_t *n_dev, cudaStream_t st) {
-  cudaError_t e = cudaSuccess;
-  for (int l0 = 0; l0 < p->d.n_layers && e == cudaSuccess; l0 += kCopyLayers) {
-    CopyArgs c = {};
-    c.layers = p->d.n_layers - l0 < kCopyLayers ? p->d.n_layers - l0 : kCopyLayers;
-    for (int l = 0; l < c.layers; ++l) {
-      c.k[l] = p->k[l0 + l];
-      c.v[l] = p->v[l0 + l];
-      if (p->coded) c.ke[l] = p->ke[l0 + l], c.ve[l] = p->ve[l0 + l];
-    }
-    c.src = src;
-    c.dst = dst;
-    c.n = n;
-    c.n_dev = n_dev;
-    c.n_pages = p->d.n_pages;
-    c.Hkv = p->d.n_kv_heads;
-    c.bytes = (int64_t)p->d.n_kv_heads * p->d.page_size * p->d.head_dim * (p->coded ? 1 : 2);
-    c.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim, p->d.n_pages).err);
-    e = launch_copy_pages(c, p->coded, p->sms, st);
+// Layers l0 on, as many as one launch takes.
+CopyArgs copy_args(const kvk_paged *p, int l0, const int32_t *src, const int32_t *dst, int n, const int32_t *n_dev) {
+  CopyArgs c = {};
+  c.layers = p->d.n_layers - l0 < kCopyLayers ? p->d.n_layers - l0 : kCopyLayers;
+  for (int l = 0; l < c.layers; ++l) {
+    c.k[l] = p->k[l0 + l];
+    c.v[l] = p->v[l0 + l];
+    if (p->coded) c.ke[l] = p->ke[l0 + l], c.ve[l] = p->ve[l0 + l];
   }
+  c.src = src;
+  c.dst = dst;
+  c.n = n;
+  c.n_dev = n_dev;
+  c.n_pages = p->d.n_pages;
+  c.Hkv = p->d.n_kv_heads;
+  c.bytes = (int64_t)p->d.n_kv_heads * p->d.page_size * p->d.head_dim * (p->coded ? 1 : 2);
+  c.err = reinterpret_cast<int32_t *>(p->ws + paged_ws(p->d.head_dim, p->d.n_pages).err);
+  return c;
+}
+// Pages of the layers from l0 on, `n` entries at most (n_dev: as many as it says).
+cudaError_t copy_layers(const kvk_paged *p, int l0, const int32_t *src, const int32_t *dst, int n, const int32_t *n_dev, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  for (; l0 < p->d.n_layers && e == cudaSuccess; l0 += kCopyLayers)
+    e = launch_copy_pages(copy_args(p, l0, src, dst, n, n_dev), p->coded, p->sms, st);
   return e;
 }
 
@@ -591,7 +594,7 @@ kvk_status kvk_paged_copy(kvk_paged *p, const int32_t *src, const int32_t *dst, 
   if (n < 0) return fail(KVK_ERR_INVALID_ARG, "n must not be negative");
   if (n == 0) return KVK_OK;
   if (!src || !dst || !aligned(src, 4) || !aligned(dst, 4)) return fail(KVK_ERR_INVALID_ARG, "null or misaligned pages");
-  const cudaError_t e = copy_layers(p, src, dst, n, nullptr, reinterpret_cast<cudaStream_t>(stream));
+  const cudaError_t e = copy_layers(p, 0, src, dst, n, nullptr, reinterpret_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page copy launch");
   return KVK_OK;
 }
@@ -626,8 +629,9 @@ kvk_status kvk_paged_fork(kvk_paged *p, const int32_t *refs, const int32_t *tabl
   cudaError_t e;
   {
     std::lock_guard<std::mutex> one(p->calls);
-    e = launch_fork(a, reinterpret_cast<cudaStream_t>(stream));
-    if (e == cudaSuccess && rows) e = copy_layers(p, a.src, a.dst, rows, nullptr, reinterpret_cast<cudaStream_t>(stream));
+    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    e = launch_fork(a, copy_args(p, 0, a.src, a.dst, rows, nullptr), p->coded, p->sms, st);
+    if (e == cudaSuccess && rows) e = copy_layers(p, kCopyLayers, a.src, a.dst, rows, nullptr, st);
   }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page fork launch");
   return KVK_OK;
@@ -644,6 +648,9 @@ kvk_status kvk_paged_compact(kvk_paged *p, const int32_t *refs, const int32_t *t
   const int64_t in = (int64_t)batch * max_pages;
   if (in && table_out != table && table_out < table + in && table < table_out + in)
     return fail(KVK_ERR_INVALID_ARG, "table_out may be the table, and may not overlap it otherwise");
+  const int n = p->d.n_pages;
+  if ((where < refs + n && refs < where + n) || (where < refs_out + n && refs_out < where + n))
+    return fail(KVK_ERR_INVALID_ARG, "where may not overlap the holders");
   PagesArgs a = pages_args(p);
   a.refs = refs;
   a.refs_out = refs_out;
@@ -657,8 +664,10 @@ kvk_status kvk_paged_compact(kvk_paged *p, const int32_t *refs, const int32_t *t
   cudaError_t e;
   {
     std::lock_guard<std::mutex> one(p->calls);
-    e = launch_compact(a, reinterpret_cast<cudaStream_t>(stream));
-    if (e == cudaSuccess) e = copy_layers(p, a.src, a.dst, p->d.n_pages / 2, a.n_moved, reinterpret_cast<cudaStream_t>(stream));
+    const cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
+    const int most = p->d.n_pages / 2;
+    e = launch_compact(a, copy_args(p, 0, a.src, a.dst, most, a.n_moved), p->coded, p->sms, st);
+    if (e == cudaSuccess) e = copy_layers(p, kCopyLayers, a.src, a.dst, most, a.n_moved, st);
   }
   if (e != cudaSuccess) return kvk_internal_cuda_error(e, "page compaction launch");
   return KVK_OK;
