@@ -594,7 +594,8 @@ kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
  * An append sets a page and head's exponent to the least that holds the largest
  * finite magnitude among its new numbers, max |x| <= 448 * 2^exponent, and the codes
  * to the nearest of x * 2^-exponent (ties to even; at most 448 in magnitude, which
- * cuts BF16 off at 2.98e38 and F16 at 57344).  Where positions of the page were held
+ * cuts BF16 off at 2.98e38 and F16 at 57344; a key that the append turns is rounded to
+ * the dtype first, as kvk_rotary_apply's is).  Where positions of the page were held
  * before the call's first, the exponent does not fall; where it rises, their codes
  * are rounded again, to the nearest of code * 2^(old - new).  Numbers that are not
  * finite are held as NaN.  No two sequences of an append may write to one page. */
@@ -665,7 +666,7 @@ kvk_status kvk_paged_copy(kvk_paged *cache, const int32_t *src, const int32_t *d
  * and none has it full; else the row gets a copy, on a free page of its own.  So
  * beams fork and are reordered, sequences grow, are taken back to fewer positions,
  * end (in no parents) and begin.
- * refs_out [n_pages] (it may be refs): the counts, less the given rows' pages, more
+ * refs_out [n_pages] (it may be refs, and may not overlap it otherwise): the counts, less the given rows' pages, more
  * the new rows'.  What this frees is handed out by the next call.  Entries behind a
  * row's pages are -1, as are those that no free page was left for, which sets
  * KVK_DEVERR_CAPACITY.  A parent that is no row (taken for -1), a negative length or
@@ -679,7 +680,9 @@ kvk_status kvk_paged_fork(kvk_paged *cache, const int32_t *refs, const int32_t *
  * page from number U on goes to the k-th free one before it.  where [n_pages]: each
  * page's new number, -1 for one that was free; table_out [batch, max_pages] (it may be
  * table): the rows' new numbers, -1 behind their pages; refs_out (it may be refs): the
- * counts; used (one int32, or NULL): U.  What stands behind U is free. */
+ * counts; used (one int32, or NULL): U.  What stands behind U is free.  Tables that
+ * are not given are renumbered by the caller, with where.  where overlaps neither
+ * refs nor refs_out, the others may not overlap but as said. */
 kvk_status kvk_paged_compact(kvk_paged *cache, const int32_t *refs, const int32_t *table, const int32_t *lengths,
                              int32_t batch, int32_t max_pages, int32_t *refs_out, int32_t *table_out, int32_t *where,
                              int32_t *used, kvk_stream stream);

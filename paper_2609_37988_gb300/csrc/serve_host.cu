@@ -244,6 +244,9 @@ kvk_status check_pages(const kvk_paged *p, const int32_t *refs, const int32_t *r
     return fail(KVK_ERR_INVALID_ARG, "null holders, lengths or table");
   if (!aligned(refs, 4) || !aligned(refs_out, 4) || !aligned(table, 4) || !aligned(lengths, 4))
     return fail(KVK_ERR_INVALID_ARG, "misaligned holders, lengths or table");
+  const int n = p->d.n_pages;
+  if (refs_out != refs && refs_out < refs + n && refs < refs_out + n)
+    return fail(KVK_ERR_INVALID_ARG, "refs_out may be refs, and may not overlap it otherwise");
   return KVK_OK;
 }
 

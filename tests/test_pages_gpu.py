@@ -208,6 +208,48 @@ def test_compact_of_a_large_pool_and_errors():
         assert small.cache.device_error() == code
 
 
+def test_fork_and_compact_of_more_layers_than_one_launch_takes():
+    page, g = 16, np.random.default_rng(9)
+    lens = [20, 40, 5]
+    refs, table = table_of(g, 40, page, lens, 4)
+    pool = Pool(40, page, 8, layers=130, hkv=1)
+    refs2, out, copies, _ = paged.fork(refs, table, lens, [0, 0, 1], [21, 22, 41], 4, page)
+    got_refs, got = pool.cache.fork(ints(refs.tolist()), ints(table.tolist()), ints(lens), ints([0, 0, 1]), ints([21, 22, 41]))
+    np.testing.assert_array_equal(got.cpu().numpy(), out)
+    pool.moved(copies)
+    refs3, out3, where, moves = paged.compact(refs2, out, [21, 22, 41], page)
+    r, t, w = pool.cache.compact(got_refs, got, ints([21, 22, 41]))
+    for x, y in ((r, refs3), (t, out3), (w, where)):
+        np.testing.assert_array_equal(x.cpu().numpy(), y)
+    pool.moved(moves)
+
+
+@pytest.mark.parametrize("call", ["fork", "compact", "copy"])
+def test_on_another_stream(call):
+    """Outputs and copies are there once that stream has run."""
+    page, g = 16, np.random.default_rng(10)
+    lens = [200, 47]
+    refs, table = table_of(g, 60, page, lens, 14)
+    pool = Pool(60, page, 16)
+    args = ints(refs.tolist()), ints(table.tolist()), ints(lens)
+    parents, src, dst = ints([1, 1, 0]), ints([3]), ints([59])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    if call == "fork":
+        got = pool.cache.fork(*args, parents, stream=side)
+        want = paged.fork(refs, table, lens, [1, 1, 0], None, 14, page)
+    elif call == "compact":
+        got = pool.cache.compact(*args, stream=side)
+        want = paged.compact(refs, table, lens, page)
+    else:
+        pool.cache.copy(src, dst, stream=side)
+        got, want = (), ([(3, 59)],)
+    side.synchronize()
+    for x, y in zip(got, want):
+        np.testing.assert_array_equal(x.cpu().numpy(), y)
+    pool.moved([m for m in want if isinstance(m, list)][0])
+
+
 def test_captured_forks_follow_their_inputs():
     """Fork, compaction and copy in one graph, replayed with other tables."""
     page, width, n_pages = 16, 6, 80
