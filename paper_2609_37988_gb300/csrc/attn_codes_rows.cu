@@ -6,7 +6,8 @@
 // up to 4 KV heads, so that a copy is 8 or 16 KB where pages are small.  A CTA: 4
 // warps, 32 positions of one head's tile each, in two blocks of 16 that lie in one
 // page and so have one power of two, and a warp that looks up pages and powers and
-// copies the tiles by TMA through a ring of 96 KB.  (8 warps of one block each took
+// copies the tiles by TMA through a ring of 64 KB (96 KB leave the L1 too little for
+// what 16 rows spill: three tokens of 32 sequences 122 us, 114 with 64).  (8 warps of one block each took
 // 426 instructions a block, a third of them around the products: 100 us where
 // two blocks take 93.)
 //
@@ -54,7 +55,7 @@ struct RowsArgs {
 
 // an even number: keys and values in turn
 template <int D>
-constexpr int rows_stages() { return 768 / D; }
+constexpr int rows_stages() { return 512 / D; }
 
 __device__ __forceinline__ void ldm(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];\n"
@@ -238,10 +239,9 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
     const int t_begin = at.t, t_end = min(at.nt, at.t + (mine - w)), w_begin = w;
     const int R = at.s.n * a.G;
     const int p_base = at.s.len - at.s.n;
-    // Q^T as the B operand (row 8 nb + g), and the positions that rows
-    // 8 nb + 2 c + e see, the scores' factor
-    uint32_t qf[KS][NB][2];
-    int lim[2 * NB], low[2 * NB];
+    // Q^T as the B operand (row 8 nb + g); of rows 8 nb + 2 c + e their tokens, a byte
+    // each (255: none), and the scores' factor
+    uint32_t qf[KS][NB][2], tok = 0;
     float sig[2 * NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
@@ -280,11 +280,15 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int rr = 8 * nb + 2 * c + e;
-        lim[2 * nb + e] = rr < R ? p_base + rr / a.G : -1;
-        low[2 * nb + e] = lim[2 * nb + e] - a.window + 1;
+        tok |= (rr < R ? (uint32_t)(rr / a.G) : 255u) << (8 * (2 * nb + e));
         sig[2 * nb + e] = a.sig_log2 * __shfl_sync(kAll, back, 4 * (2 * c + e));
       }
     }
+    // whether row i sees position t
+    auto sees = [&](int i, int t) {
+      const int j = tok >> (8 * i) & 255;
+      return j != 255 && t <= p_base + j && t > p_base + j - a.window;
+    };
     const int lim_min = p_base, low_max = at.s.len - a.window;  // of the first and the last token
     float o[NB][KS][4];
 #pragma unroll
@@ -340,13 +344,26 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
           for (int y = 0; y < 2; ++y) {
             float &x = s[b][i >> 1][2 * y + (i & 1)];
             x *= f;
-            const int t = t0 + 16 * b + 8 * y + g;
-            if (partial && (t > lim[i] || t < low[i])) x = -INFINITY;
             mx[i] = fmaxf(mx[i], x);
           }
         }
-        more = more || mx[i] > m[i];
       }
+      if (partial) {
+#pragma unroll
+        for (int i = 0; i < 2 * NB; ++i) {
+          mx[i] = -INFINITY;
+#pragma unroll
+          for (int b = 0; b < PB; ++b)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+              float &x = s[b][i >> 1][2 * y + (i & 1)];
+              if (!sees(i, t0 + 16 * b + 8 * y + g)) x = -INFINITY;
+              mx[i] = fmaxf(mx[i], x);
+            }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * NB; ++i) more = more || mx[i] > m[i];
       if (__any_sync(kAll, more)) {
 #pragma unroll
         for (int i = 0; i < 2 * NB; ++i) {
@@ -435,15 +452,18 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
           for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float p = 0.f;
+              // the weight, from the lane that has it in the operand
+              uint32_t w2 = 0;
 #pragma unroll
               for (int b = 0; b < PB; ++b)
 #pragma unroll
                 for (int z = 0; z < 2; ++z) {
-                  const float x = __shfl_sync(kAll, s[b][nb][2 * z + e], (y & 7) * 4 + c);
-                  p = y >> 3 == 2 * b + z ? x : p;
+                  const uint32_t x = __shfl_sync(kAll, ph[b][nb][z], 4 * (2 * c + e) + (y >> 1 & 3));
+                  w2 = y >> 3 == 2 * b + z ? x : w2;
                 }
-              if (t <= lim[2 * nb + e] && t >= low[2 * nb + e]) {
+              const float2 pair = unpack2<false>(w2);
+              const float p = y & 1 ? pair.y : pair.x;
+              if (sees(2 * nb + e, t)) {
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                   const float2 x = unpack2<false>(code2_f16(*reinterpret_cast<const uint16_t *>(row + ((k ^ swz(rr)) << 4) + 2 * g)));
