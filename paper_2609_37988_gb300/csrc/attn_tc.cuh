@@ -290,9 +290,9 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
       return j;
     };
     // hands a job out and copies its tiles
-    auto emit = [&](Job j) {
+    auto emit = [&](const Job &j) {
+      const int tile0 = tiles;
       if constexpr (CODES) {
-        j.tile0 = tiles;
         if (j.b >= 0) tiles += j.nt;
       }
       const int slot = k & 1;
@@ -300,6 +300,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
       ++k;
       if (lane == 0) {
         jobs[slot] = j;
+        if constexpr (CODES) jobs[slot].tile0 = tile0;
         mbar_arrive(&jfull[slot]);
       }
       __syncwarp();
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait0(&rfree[s], ph ^ 1)) return false;
             if (kv == 0) {
-              TilePow *tp = &pows[(j.tile0 + jt) % SM::kPows];
+              TilePow *tp = &pows[(tile0 + jt) % SM::kPows];
               // (parts without a page are zeros whatever their factor)
               const int dk = ek == kNoPow ? 0 : max(ek - kref, -128), dv = ev == kNoPow ? 0 : max(ev - vref, -128);
               if (lane < cparts) tp->kf[lane] = factor(dk), tp->vf[lane] = factor(dv);

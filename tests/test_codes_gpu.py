@@ -520,3 +520,11 @@ def test_an_attention_that_gives_up_says_so(news):
     assert b.cache.device_error() == 8
     b.cache.set_give_up(False)
     assert torch.equal(b.attend(0.088), keep) and b.cache.device_error() == 0
+
+
+@pytest.mark.parametrize("new", [1, 3, 20])
+def test_contexts_of_seventy_thousand_positions(new):
+    """A table wider than 65536 positions, pieces in every CTA; a window at its end."""
+    b = Codes([new], [70001], 4, 1, 64, F16, 16, seed=34).append()
+    for window in (0, 66000):
+        b.check(window)
