@@ -305,6 +305,40 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
       }
       __syncwarp();
       if (j.b < 0 || j.nt == 0) return true;
+      // A lane per part; pages looked up two tiles ahead, their powers one, and what is
+      // read is not touched before the next turn (a look at it would wait for it: a
+      // pair of tiles took 3000 cycles so).
+      const int cshift = pv.page_shift, cparts = kTcT >> cshift;
+      auto seen = [&](int jt) {
+        const int pos = j.lo + jt * kTcT + (lane << cshift);
+        return lane < cparts && pos < j.p0 + j.n && pos + (1 << cshift) > j.first - a.window + 1;
+      };
+      auto find = [&](int jt) {
+        return load_if(pv.table + (int64_t)j.b * pv.max_pages + ((j.lo + jt * kTcT + (lane << cshift)) >> cshift),
+                       jt < j.nt && seen(jt), -1);
+      };
+      auto page_at = [&](int pg, int jt) {  // what was found, n_pages where there is none
+        if ((unsigned)pg < (unsigned)pv.n_pages) return pg;
+        if (jt < j.nt && seen(jt)) set_err(pv.err, kErrPage);
+        return pv.n_pages;
+      };
+      auto power = [&](int pg, const int8_t *e) { return load_if(e + (int64_t)pg * pv.Hkv + j.h, pg < pv.n_pages, kNoPow); };
+      auto clamped = [&](int e) { return e == kNoPow ? e : min(max(e, pv.e_lo), pv.e_hi); };
+      auto factor = [&](int d) {
+        const int x = max(d + kRefUp, -14), y = max(d + kRefUp - x, -24);
+        return (uint32_t)(15 + x) << 10 | (y >= -14 ? (uint32_t)(15 + y) << 10 : 1u << (24 + y)) << 16;
+      };
+      // tile 0's pages and powers: before the wait for the queries' place, behind the
+      // copy of the first queries
+      int found = -1, found_next = -1, now = 0, ek_read = kNoPow, ev_read = kNoPow;
+      auto resolve = [&]() {
+        now = page_at(found, 0);
+        ek_read = power(now, pv.ke), ev_read = power(now, pv.ve);
+      };
+      if constexpr (CODES) {
+        found = find(0), found_next = find(1);
+        if (loads > 0) resolve();
+      }
       if (loads > 0 && !wait0(qfree, (loads - 1) & 1)) return false;
       ++loads;
       if (lane == 0) mbar_expect_tx(qfull, (1 + j.two) * NB * G * P * 128);
@@ -331,32 +365,8 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         return pv.n_pages;
       };
       if constexpr (CODES) {
-        // A lane per part; pages looked up two tiles ahead, their powers one, and what is
-        // read is not touched before the next turn (a look at it would wait for it: a
-        // pair of tiles took 3000 cycles so).
-        const int cshift = pv.page_shift, cparts = kTcT >> cshift;
-        auto seen = [&](int jt) {
-          const int pos = j.lo + jt * kTcT + (lane << cshift);
-          return lane < cparts && pos < j.p0 + j.n && pos + (1 << cshift) > j.first - a.window + 1;
-        };
-        auto find = [&](int jt) {
-          return load_if(pv.table + (int64_t)j.b * pv.max_pages + ((j.lo + jt * kTcT + (lane << cshift)) >> cshift),
-                         jt < j.nt && seen(jt), -1);
-        };
-        auto page_at = [&](int pg, int jt) {  // what was found, n_pages where there is none
-          if ((unsigned)pg < (unsigned)pv.n_pages) return pg;
-          if (jt < j.nt && seen(jt)) set_err(pv.err, kErrPage);
-          return pv.n_pages;
-        };
-        auto power = [&](int pg, const int8_t *e) { return load_if(e + (int64_t)pg * pv.Hkv + j.h, pg < pv.n_pages, kNoPow); };
-        auto clamped = [&](int e) { return e == kNoPow ? e : min(max(e, pv.e_lo), pv.e_hi); };
-        auto factor = [&](int d) {
-          const int x = max(d + kRefUp, -14), y = max(d + kRefUp - x, -24);
-          return (uint32_t)(15 + x) << 10 | (y >= -14 ? (uint32_t)(15 + y) << 10 : 1u << (24 + y)) << 16;
-        };
-        int found = find(0), found_next = find(1), vref = pv.e_lo;
-        int now = page_at(found, 0);
-        int ek_read = power(now, pv.ke), ev_read = power(now, pv.ve);
+        if (loads == 1) resolve();
+        int vref = pv.e_lo;
         for (int jt = 0; jt < j.nt; ++jt) {
           const int next = page_at(found_next, jt + 1);
           const int ek_next = power(next, pv.ke), ev_next = power(next, pv.ve);
