@@ -35,6 +35,11 @@ __device__ __forceinline__ uint32_t code2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ uint32_t code2_of_f16(uint32_t h) {
+  uint16_t r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(h));
+  return r;
+}
 // two codes as f16 (exact)
 __device__ __forceinline__ uint32_t code2_f16(uint32_t c) {
   uint32_t r;
@@ -43,9 +48,21 @@ __device__ __forceinline__ uint32_t code2_f16(uint32_t c) {
 }
 __device__ __forceinline__ float finite_or_nan(float x) { return fabsf(x) <= 3.4028234e38f ? x : __int_as_float(0x7fc00000); }
 
-// the codes of two pairs of the dtype, times `up`
+// the codes of two pairs of the dtype, times the power of two `up`; finite numbers, and
+// any (those that are not finite to NaN)
+// (f16: the product is exact, or below 2^-14 and so the code 0 however it is rounded)
 template <bool BF16>
 __device__ __forceinline__ uint32_t code4(uint32_t a, uint32_t b, float up) {
+  if constexpr (BF16) {
+    const float2 x = unpack2<BF16>(a), y = unpack2<BF16>(b);
+    return code2(x.x * up, x.y * up) | code2(y.x * up, y.y * up) << 16;
+  } else {
+    const uint32_t f = pack_f16(up, up);
+    return code2_of_f16(hmul2_u32(a, f)) | code2_of_f16(hmul2_u32(b, f)) << 16;
+  }
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t code4_any(uint32_t a, uint32_t b, float up) {
   const float2 x = unpack2<BF16>(a), y = unpack2<BF16>(b);
   return code2(finite_or_nan(x.x) * up, finite_or_nan(x.y) * up) | code2(finite_or_nan(y.x) * up, finite_or_nan(y.y) * up) << 16;
 }

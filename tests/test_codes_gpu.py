@@ -205,6 +205,27 @@ def test_append_turns_keys_as_the_rotary_does(dtype, page, hq, hkv, d, mode):
     assert one.cache.device_error() == 0
 
 
+@pytest.mark.parametrize("page", [64, 128])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_one_long_sequence_among_single_tokens(page, d):
+    """Groups for few tokens go over a page's rows more than once; numbers that are not
+    finite in one turn of several."""
+    from paper_2609_37988_gb300.serving import Rotary
+    lens = [1] * 40 + [300] + [5] * 20
+    b = Codes([0] * len(lens), lens, 2, 2, d, BF16, page, seed=35)
+    b.k[40][100, 1, 3] = float("inf")
+    b.v[40][7, 0, 0] = float("nan")
+    b.v[40][290] *= 100
+    b.append().same()
+    rot, pos = Rotary(head_dim=d), torch.cat([torch.arange(l) for l in lens]).to(torch.int32).cuda()
+    one, two = (Codes([0] * len(lens), lens, 2, 2, d, BF16, page, seed=36) for _ in range(2))
+    k, v = torch.cat(one.k).cuda(), torch.cat(one.v).cuda()
+    one.cache.append(0, k, v, offsets(lens), ints(lens), one.table_d, rotary=rot)
+    two.cache.append(0, rot.apply(None, k, pos)[1], v, offsets(lens), ints(lens), two.table_d)
+    assert torch.equal(one.cache.k_pages[0].view(torch.uint8), two.cache.k_pages[0].view(torch.uint8))
+    assert torch.equal(one.cache.k_exps[0], two.cache.k_exps[0])
+
+
 @pytest.mark.parametrize("count", [33, 200])
 def test_append_of_many_sequences(count):
     rng = np.random.default_rng(9)
