@@ -237,7 +237,8 @@ kvk_status check_pages(const kvk_paged *p, const int32_t *refs, const int32_t *r
   if (!p) return fail(KVK_ERR_INVALID_ARG, "null paged cache");
   const kvk_status s = check_device(p);
   if (s) return s;
-  if (batch < 0 || max_pages < 0) return fail(KVK_ERR_INVALID_ARG, "batch and max_pages must not be negative");
+  if (batch < 0 || batch > (1 << 24) || max_pages < 0)
+    return fail(KVK_ERR_INVALID_ARG, "batch must be in [0, 2^24], max_pages not negative");
   if ((int64_t)max_pages * p->d.page_size > (1 << 26))
     return fail(KVK_ERR_INVALID_ARG, "max_pages %d: more than 2^26 positions", max_pages);
   if (!refs || !refs_out || (batch && (!lengths || (!table && max_pages))))

@@ -100,7 +100,7 @@ def test_refusals_with_a_cache(lib):
         fork = lambda *a: so.kvk_paged_fork(h, *a, None)  # noqa: E731
         good = [r, t, l, 1, 2, l, l, 1, r, two, 2]
         assert fork(*good[:8], r + 4, *good[9:]) == INVALID  # beside itself
-        for at, bad in ((0, None), (1, None), (2, None), (3, -1), (4, -1), (4, 2 ** 23), (5, None), (6, l + 1), (7, -1), (7, 16385),
+        for at, bad in ((0, None), (1, None), (2, None), (3, -1), (3, 2 ** 25), (4, -1), (4, 2 ** 23), (5, None), (6, l + 1), (7, -1), (7, 16385),
                         (8, None), (8, r + 2), (9, None), (9, t), (9, t + 4), (10, -1), (10, 2 ** 23)):
             assert fork(*good[:at], bad, *good[at + 1:]) == INVALID, at
         compact = lambda *a: so.kvk_paged_compact(h, *a, None)  # noqa: E731
