@@ -38,6 +38,12 @@
 // exact where e >= ref - 21 and off by 2^(ref - 31) at most below.  The keys' ref
 // multiplies the scores; a row's result is relative to the values' and is rescaled in
 // place when it rises.
+// Chunks of one query tile (SRC kCodesFew) would leave a softmax warpgroup idle: both
+// take it, one the even tiles of positions, the other the odd ones, and the first joins
+// their results in TMEM; the second query tile's place is one more of the ring's.  (4
+// tokens of 32 sequences over 8192 positions 186 -> 169 us, 161 with warps that have no
+// row of anybody's left out; shared memory bounds it, which a tile passes through as
+// codes, as f16 and, with the queries, on its way to the products.)
 // Queries in bf16 become f16, a row times the power of two that brings its largest
 // to [2^13, 2^14): exact but for numbers below 2^-28 of that.  A NaN among values
 // of a partly seen tile enters as zero there and then.
@@ -79,7 +85,7 @@ constexpr int kErrTimeout = 8, kErrCount = 4, kErrPage = 32;  // KVK_DEVERR_*
 constexpr uint32_t kAll = 0xffffffffu;
 constexpr uint32_t kWaits = 1u << 20;     // polls of up to 2 us each
 
-enum { kPacked, kPaged, kCodes };          // where keys and values are
+enum { kPacked, kPaged, kCodes, kCodesFew };  // where keys and values are
 
 struct TcArgs {
   CUtensorMap mq, mk, mv;
@@ -113,15 +119,17 @@ constexpr int tc_part(int D) { return kTcT * (D + 2); }
 constexpr int kTcMinShare = 4;  // tiles of a run at least
 constexpr int kTcOrdered = 128;  // sequences whose jobs are put in order
 
-template <int D, bool CODES>
+template <int D, int SRC>
 struct Smem {
+  static constexpr bool CODES = SRC >= kCodes;
+  static constexpr int kQTiles = SRC == kCodesFew ? 1 : 2;
   static constexpr int kTile = D / 64 * kBox;          // a query, key or value tile
   static constexpr int kRawTile = kTcT * D;            // its codes
-  static constexpr int kStages = CODES ? (D == 128 ? 3 : 6) : D == 128 ? 5 : 8;
+  static constexpr int kStages = CODES ? (D == 128 ? 3 : 6) + 2 - kQTiles : D == 128 ? 5 : 8;
   static constexpr int kRaw = CODES ? (D == 128 ? 4 : 6) : 0;
   static constexpr int kPows = D == 128 ? 8 : 16;      // tiles whose powers are kept
   static_assert(!CODES || (kStages + kRaw) / 2 + 3 <= kPows, "powers of the tiles in either ring and at work");
-  static constexpr int kQ = 0, kRing = 2 * kTile, kRawRing = kRing + kStages * kTile, kBar = kRawRing + kRaw * kRawTile;
+  static constexpr int kQ = 0, kRing = kQTiles * kTile, kRawRing = kRing + kStages * kTile, kBar = kRawRing + kRaw * kRawTile;
   static constexpr int kBars = 3 * kStages + 17 + 2 * kRaw + (CODES ? 2 : 0);
   static constexpr int kJob = kBar + 8 * kBars;        // two jobs
   static constexpr int kPow = kJob + 2 * (int)sizeof(Job);
@@ -130,9 +138,10 @@ struct Smem {
   static constexpr int kTotal = kWords + 16;
   static constexpr int kBytes = kTotal + 1024;         // + alignment of the base
 };
-static_assert(Smem<128, false>::kBytes <= 232448 && Smem<64, false>::kBytes <= 232448, "shared memory");
-static_assert(Smem<128, true>::kBytes <= 232448 && Smem<64, true>::kBytes <= 232448, "shared memory");
-static_assert(Smem<64, false>::kBytes > 116 * 1024 && Smem<64, true>::kBytes > 116 * 1024,
+static_assert(Smem<128, kPaged>::kBytes <= 232448 && Smem<64, kPaged>::kBytes <= 232448, "shared memory");
+static_assert(Smem<128, kCodes>::kBytes <= 232448 && Smem<64, kCodes>::kBytes <= 232448, "shared memory");
+static_assert(Smem<128, kCodesFew>::kBytes <= 232448 && Smem<64, kCodesFew>::kBytes <= 232448, "shared memory");
+static_assert(Smem<64, kPaged>::kBytes > 116 * 1024 && Smem<64, kCodes>::kBytes > 116 * 1024 && Smem<64, kCodesFew>::kBytes > 116 * 1024,
               "one CTA (holding all TMEM columns) per SM");
 
 // 32 columns of this warp's lanes, not waited for
@@ -172,10 +181,11 @@ __device__ __forceinline__ int seq_tokens(const PagedView &v, int b, int &q0) {
 }
 
 template <int D, bool BF16, int SRC>
-__global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel(const __grid_constant__ TcArgs t) {
-  constexpr bool PAGED = SRC != kPacked, CODES = SRC == kCodes;
+__global__ void __launch_bounds__(tc_threads<(SRC >= kCodes)>(), 1) attn_tc_kernel(const __grid_constant__ TcArgs t) {
+  constexpr bool PAGED = SRC != kPacked, CODES = SRC >= kCodes;
+  constexpr bool FEW = SRC == kCodesFew;  // one query tile: its even tiles of positions, and its odd ones
   constexpr bool TB = BF16 && !CODES;  // type of the products' operands
-  using SM = Smem<D, CODES>;
+  using SM = Smem<D, SRC>;
   constexpr int NS = SM::kStages, NR = SM::kRaw;
   extern __shared__ uint8_t tc_raw[];
   uint8_t *sm = tc_raw + ((1024u - (smem_u32(tc_raw) & 1023u)) & 1023u);
@@ -190,7 +200,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
   // read.
   uint64_t *full = bar, *free_ = bar + NS, *qfull = bar + 2 * NS, *qfree = qfull + 1, *jfull = qfree + 1, *jfree = jfull + 2,
            *sfull = jfree + 2, *pfull = sfull + 2, *odone = pfull + 4, *ofree = odone + 2, *vclean = ofree + 2,
-           *drain = vclean + NS;
+           *drain = vclean + NS, *xfull = vclean;  // kCodesFew: the odd tiles' sums stand ready
   // kCodes: codes landed, codes read; a job's queries in f16 (by its slot).  full is
   // then the warps' that make f16 tiles, free the products'.
   uint64_t *rfull = drain + 1, *rfree = rfull + NR, *qready = rfree + NR;
@@ -202,14 +212,14 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
   const AttnArgs &a = t.a;
   const PagedView &pv = a.pv;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int P = t.P, G = a.G;
+  const int P = t.P, G = a.G, PB = SM::kQTiles * P;  // PB: tokens of a job
 
   if (tid == 0) {
     for (int i = 0; i < SM::kBars; ++i) {
       uint64_t *b = bar + i;
       const int n = b >= jfree && b < jfree + 2 ? (CODES ? 9 + kExpand : 11)
                     : (b >= pfull && b < pfull + 4) || (b >= ofree && b < ofree + 2) ? 4
-                    : b >= vclean && b < vclean + NS ? 2
+                    : b >= vclean && b < vclean + NS ? (FEW ? 4 : 2)
                     : b >= free_ && b < free_ + NS   ? (CODES ? 1 : 3)
                     : CODES && ((b >= full && b < full + NS) || (b >= rfree && b < qready + 2)) ? kExpand
                                                                                                : 1;
@@ -257,7 +267,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
       return __shfl_sync(kAll, ok, 0) != 0;
     };
     constexpr int NB = D / 64;
-    // describes block `blk` of sequence b (2 P tokens), KV head h
+    // describes block `blk` of sequence b (PB tokens), KV head h
     auto describe = [&](int b, int h, int blk, int q0, int n) {
       Job j = {};
       j.b = b;
@@ -275,8 +285,8 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         }
       }
       j.p0 = len - n;
-      j.tok0 = blk * 2 * P;
-      j.two = j.tok0 + P < n;
+      j.tok0 = blk * PB;
+      j.two = !FEW && j.tok0 + P < n;
       j.lo = max(0, j.p0 + j.tok0 - a.window + 1) / kTcT * kTcT;
       int last = 0;
       for (int i = 0; i < 1 + j.two; ++i) {
@@ -430,7 +440,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
     };
     auto read_blocks = [&](int b) {
       int q0;
-      return b < pv.B ? (seq_tokens(pv, b, q0) + 2 * P - 1) / (2 * P) : 0;
+      return b < pv.B ? (seq_tokens(pv, b, q0) + PB - 1) / PB : 0;
     };
     Job end = {};
     end.b = -1;
@@ -443,8 +453,8 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         const int n = seq_tokens(pv, b, q0);
         if (n == 0) return 0;
         const int p0 = (int)min((int64_t)max(pv.lens[b], 0), (int64_t)pv.max_pages << pv.page_shift) - n;
-        for (int tok = 0; tok < n; tok += 2 * P) {
-          const int last = p0 + min(n, tok + 2 * P) - 1, lo = max(0, p0 + tok - a.window + 1) / kTcT;
+        for (int tok = 0; tok < n; tok += PB) {
+          const int last = p0 + min(n, tok + PB) - 1, lo = max(0, p0 + tok - a.window + 1) / kTcT;
           sum += last < 0 ? 1 : last / kTcT - lo + 1;
         }
         return sum;
@@ -484,7 +494,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         h = ok ? (int)div_pos(off, per) : 0;
         t = (int)(off - (int64_t)h * per);
         Job j = describe(b, h, 0, q0, n);
-        while (ok && t >= max(1, j.nt) && (blk + 1) * 2 * P < n) {
+        while (ok && t >= max(1, j.nt) && (blk + 1) * PB < n) {
           t -= max(1, j.nt);
           j = describe(b, h, ++blk, q0, n);
         }
@@ -513,7 +523,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
           left -= t1 - t;
           if (left == 0) break;
           t = 0;
-          if (++blk >= (n + 2 * P - 1) / (2 * P)) {
+          if (++blk >= (n + PB - 1) / PB) {
             blk = 0;
             if (++h >= pv.Hkv) {
               h = 0;
@@ -538,7 +548,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         if (PAGED && n > 0) {
           int q0;
           const int held = (int)min((int64_t)max(pv.lens[b], 0), (int64_t)pv.max_pages << pv.page_shift);
-          from[i] = max(held - seq_tokens(pv, b, q0), 0) / (2 * P);
+          from[i] = max(held - seq_tokens(pv, b, q0), 0) / PB;
         }
         to[i] = from[i] + n;
         total += n;
@@ -608,7 +618,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         const int from_end = r - (before + __shfl_sync(kAll, sum - x, f));
         int q0;
         const int n = seq_tokens(pv, b0 + f, q0);
-        ok = emit(describe(b0 + f, (int)(idx - (int64_t)r * pv.Hkv), (n + 2 * P - 1) / (2 * P) - 1 - from_end, q0, n));
+        ok = emit(describe(b0 + f, (int)(idx - (int64_t)r * pv.Hkv), (n + PB - 1) / PB - 1 - from_end, q0, n));
       }
     }
     if (!__any_sync(kAll, *abort_flag)) emit(end);
@@ -643,7 +653,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
     uint32_t tiles[2] = {0, 0}, done[2] = {0, 0};  // of either query tile: parity of its tiles, jobs with any
     auto scores = [&](auto I, int at) {
       constexpr int i = decltype(I)::value;
-      const uint32_t q = q_at + i * (SM::kTile >> 4), kk = umma_desc_lo(ring + at * SM::kTile, 16);
+      const uint32_t q = q_at + (FEW ? 0 : i * (SM::kTile >> 4)), kk = umma_desc_lo(ring + at * SM::kTile, 16);
 #pragma unroll
       for (int b = 0; b < D / 64; ++b)
 #pragma unroll
@@ -685,6 +695,38 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
       } else {
         if (!wait(qfull, loads)) break;
         loads ^= 1;
+      }
+      if constexpr (FEW) {
+        // A tile's scores go before the last one's values, whose softmax runs meanwhile.
+        auto step = [&]() {
+          if (++s == NS) s = 0, ph ^= 1;
+        };
+        auto keys = [&](int jt) {
+          // the odd tiles' scores stand where their last sums were left to be read
+          if (jt == 1 && done[1]++ > 0 && !wait(&ofree[1], done[1] & 1)) return false;
+          if (!wait(&full[s], ph)) return false;
+          tc_fence_after();
+          if (jt & 1)
+            scores(i1, s);
+          else
+            scores(i0, s);
+          umma_commit_if(leader, &free_[s]);
+          if (jt + 1 == nt) umma_commit_if(leader, qfree);
+          step();
+          return true;
+        };
+        ok = keys(0);
+        for (int jt = 0; ok && jt < nt; ++jt) {
+          const int at = s;
+          const uint32_t at_ph = ph;
+          step();
+          if (jt + 1 < nt && !(ok = keys(jt + 1))) break;
+          if (jt == 0 && done[0]++ > 0 && !(ok = wait(&ofree[0], done[0] & 1))) break;
+          if (!(ok = wait(&full[at], at_ph))) break;
+          if (!(ok = jt & 1 ? values(i1, at, jt > 1) : values(i0, at, jt > 1))) break;
+          umma_commit_if(leader, &free_[at]);
+        }
+        continue;
       }
       // K of tile 0
       if (!wait(&full[s], ph)) break;
@@ -956,7 +998,8 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
     // f16 weights are 2^8 larger, and the reference moves sooner: at most 2^14
     constexpr float kShift = TB ? 0.f : 8.f, kLag = TB ? 8.f : 6.f;
     int tiles = 0;  // of this query tile so far
-    uint32_t q_loads[2] = {0, 0};
+    uint32_t q_loads[2] = {0, 0}, joins = 0;
+    const int qt = FEW ? 0 : i;
     auto arrive = [&](uint64_t *b) {
       __syncwarp();
       if (lane == 0) mbar_arrive(b);
@@ -972,19 +1015,30 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         if (jb >= 0 && j.nt > 0) {
           if (!wait(&qready[slot], q_loads[slot])) break;
           q_loads[slot] ^= 1;
-          sg_row = a.sig_log2 * pow2f(sq[(slot * 2 + i) * kTcT + row]);
+          sg_row = a.sig_log2 * pow2f(sq[(slot * 2 + qt) * kTcT + row]);
         }
       }
-      if (jb >= 0 && (i == 0 || j.two)) {
-        const int tok = j.tok0 + i * P + my_tok;
+      if (jb >= 0 && (i == 0 || (FEW ? j.nt > 1 : j.two))) {
+        const int tok = j.tok0 + qt * P + my_tok;
         const bool real = my_tok < P && tok < j.n;
         const int pos = j.p0 + tok;
         // rows that are nobody's are never masked: their own affair
         const int lim = real ? pos : 1 << 30, low = real ? pos - a.window + 1 : -(1 << 30);
-        const int js = j.js[i], je = j.je[i], lo = j.lo;
+        const int js = j.js[qt], je = j.je[qt], lo = j.lo;  // kCodesFew: all of the job's
+        const int j0 = FEW ? i : js;  // the first of this warpgroup's
         float m = -INFINITY, l = 0.f;
         int unit = 0;  // kCodes: the result is relative to 2^unit
-        for (int jt = js; jt < je; ++jt) {
+        const bool idle = FEW && !__any_sync(kAll, real);
+        if (FEW && idle) {
+          // a warp whose rows are all nobody's: their products may hold anything
+          for (int jt = j0; jt < je; jt += 2) {
+            if (!(ok = wait(&sfull[i], tiles & 1))) break;
+            arrive(&pfull[2 * i]);
+            arrive(&pfull[2 * i + 1]);
+            ++tiles;
+          }
+        }
+        for (int jt = idle ? je : j0; jt < je; jt += FEW ? 2 : 1) {
           if (!(ok = wait(&sfull[i], tiles & 1))) break;
           tc_fence_after();
           float fo = 1.f;  // the values' power has risen
@@ -993,7 +1047,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
             // (not 0, which times a masked score would be NaN: pages of zeros)
             sg = fmaxf(sg_row * pow2f(tp->kref), 1.1754944e-38f);
             const int vref = tp->vref;
-            if (jt > js && vref > unit) fo = pow2f(max(unit - vref, -126));
+            if (jt > j0 && vref > unit) fo = pow2f(max(unit - vref, -126));
             unit = vref;
           }
           float x[128];
@@ -1025,7 +1079,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
             m = mn;
             l *= f;
             if constexpr (CODES) f *= fo;
-            if (jt > js) {  // the products before this tile's have to be in
+            if (jt > j0) {  // the products before this tile's have to be in
               if (!(ok = wait(&odone[i], (tiles - 1) & 1))) break;
               tc_fence_after();
 #pragma unroll 1
@@ -1072,6 +1126,37 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
           ++tiles;
         }
         if (!ok) break;
+        float f0 = 1.f, f1 = 0.f;  // kCodesFew: of the even tiles' results and the odd ones'
+        if constexpr (FEW) {
+          if (j.nt > 1) {
+            if (i == 1) {
+              // reference, sum and power for the other warpgroup, in the scores' place
+              if (!wait(&odone[1], (tiles - 1) & 1)) break;
+              tc_fence_after();
+              const uint32_t w[8] = {__float_as_uint(m), __float_as_uint(l), (uint32_t)unit};
+              tmem_st8_nw(ts, w);
+              tmem_wait_st();
+              tc_fence_before();
+              arrive(xfull);
+              arrive(&jfree[slot]);
+              continue;
+            }
+            if (!wait(xfull, joins)) break;
+            joins ^= 1;
+            tc_fence_after();
+            float z[16];
+            tmem_ld16(ts + 128, z);
+            const float top = fmaxf(m, z[0]);
+            const int unit1 = __float_as_int(z[2]), high = max(unit, unit1);
+            f0 = m == -INFINITY ? 0.f : fast_exp2(m - top);
+            f1 = z[0] == -INFINITY ? 0.f : fast_exp2(z[0] - top);
+            l = l * f0 + z[1] * f1;
+            f0 *= pow2f(max(unit - high, -126));
+            f1 *= pow2f(max(unit1 - high, -126));
+            m = top;
+            unit = high;
+          }
+        }
         const float inv = real && pos >= 0 ? 1.f / l : 0.f;
         uint32_t nan[D / 32] = {};  // channels of which the row sees a value that is not finite
         if (je > js) {
@@ -1145,6 +1230,14 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
 #pragma unroll
             for (int y = 0; y < 32; ++y) o[y] = 0.f;
           }
+          if constexpr (FEW) {
+            if (j.nt > 1) {
+              float z[32];
+              tmem_ld32(to + D + 32 * c, z);
+#pragma unroll
+              for (int y = 0; y < 32; ++y) o[y] = o[y] * f0 + z[y] * f1;
+            }
+          }
           if constexpr (CODES) {
             const float f = slot_out >= 0 ? fu : inv;
 #pragma unroll
@@ -1181,6 +1274,7 @@ __global__ void __launch_bounds__(tc_threads<SRC == kCodes>(), 1) attn_tc_kernel
         if (je > js) {
           tc_fence_before();
           arrive(&ofree[i]);
+          if (FEW && j.nt > 1) arrive(&ofree[1]);
         }
       }
       arrive(&jfree[slot]);
@@ -1215,7 +1309,7 @@ __global__ void __launch_bounds__(HALVES *kTcT) attn_tc_join_kernel(const AttnAr
     const TcSplit u = a.tc_list->unit[item / (2 * C)];
     const int i = item / C & 1, c = item % C;
     const int tok = u.tok0 + i * P + tok_row;
-    const bool real = tok_row < P && tok < u.n;
+    const bool real = tok_row < P && tok < u.n && !(a.few && i);
     float M = -INFINITY, L = 0.f, x[CH];
 #pragma unroll
     for (int y = 0; y < CH; ++y) x[y] = 0.f;
@@ -1295,20 +1389,22 @@ cudaError_t rows_map(CUtensorMap *m, bool bf, void *p, int D, int64_t n1, int64_
 template <int D, bool BF16, int SRC>
 cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   constexpr bool PAGED = SRC != kPacked;
-  constexpr int smem = Smem<D, SRC == kCodes>::kBytes;
+  constexpr int smem = Smem<D, SRC>::kBytes;
   cudaError_t e = allow_smem<&attn_tc_kernel<D, BF16, SRC>>(smem, a.device);
-  if constexpr (SRC == kCodes) {
+  if constexpr (SRC >= kCodes) {
     if (e == cudaSuccess) e = check_reg_split<&attn_tc_kernel<D, BF16, SRC>>(kTcCodesRegs);
   }
   if (e != cudaSuccess) return e;
   TcArgs t;
   t.a = a;
   t.P = kTcT / a.G;
+  const int PB = Smem<D, SRC>::kQTiles * t.P;  // tokens of a job
+  t.a.few = SRC == kCodesFew;
   t.a.out_sector = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   const int N = a.pv.n_tokens;
   e = rows_map(&t.mq, BF16, a.q.p, D, a.Hq, a.q.hs, N, a.q.ts, a.G, t.P);
   if (PAGED) {
-    memcpy(&t.mk, SRC == kCodes ? a.ok : a.mk, sizeof t.mk);
+    memcpy(&t.mk, SRC >= kCodes ? a.ok : a.mk, sizeof t.mk);
     memcpy(&t.mv, a.ov, sizeof t.mv);
   } else {
     if (e == cudaSuccess) e = rows_map(&t.mk, BF16, a.k.p, D, N, a.k.ts, a.pv.Hkv, a.k.hs, kTcT, 1);
@@ -1316,7 +1412,7 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   }
   if (e != cudaSuccess) return e;
   // at most so many jobs: every sequence's last one may be a partial one
-  const int64_t jobs = (int64_t)a.pv.Hkv * (N / (2 * t.P) + std::min(a.pv.B, N));
+  const int64_t jobs = (int64_t)a.pv.Hkv * (N / PB + std::min(a.pv.B, N));
   // Runs where whole jobs would leave SMs idle for longer than the pieces take on
   // their way through memory: the part of the last round of jobs that is not
   // filled, against 5 tiles for a second kernel and up to 18 for the pieces of as
@@ -1326,16 +1422,16 @@ cudaError_t launch_t(const AttnArgs &a, cudaStream_t st) {
   // 35 / 48, over 4000 73 / 66; 512 over 8192 86 / 70; 600 over 600 15 / 28; 4 x 33
   // over 2000 27 / 18; 32 x 4 over 1900 54 / 55, over 8192 182 / 174.  Up to four
   // rounds: of 2048 tokens over 32768, 1 (2.2 rounds) 971 / 916, 4 (8.6) 3473 / 3894.
-  const int64_t seqs = std::min(a.pv.B, N), share = (N + seqs - 1) / seqs, blocks = (share + 2 * t.P - 1) / (2 * t.P);
-  const int64_t seen = std::min((int64_t)a.pv.max_pages << a.pv.page_shift, (int64_t)a.window + 2 * t.P + kTcT);
+  const int64_t seqs = std::min(a.pv.B, N), share = (N + seqs - 1) / seqs, blocks = (share + PB - 1) / PB;
+  const int64_t seen = std::min((int64_t)a.pv.max_pages << a.pv.page_shift, (int64_t)a.window + PB + kTcT);
   const double full = (double)a.pv.Hkv * seqs * blocks, waves = full / a.sms;
   const double idle = (std::ceil(waves) - waves) * (double)((seen + kTcT - 1) / kTcT);
-  const double rows = (double)std::min<int64_t>(2 * t.P, share) * a.G / (2 * kTcT);
+  const double rows = (double)std::min<int64_t>(PB, share) * a.G / (2 * kTcT);
   t.a.runs = PAGED && waves < 4 && idle > 5 + 0.12 * std::min(full, (double)a.sms) * rows;
   if (!t.a.runs)
-    return launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(tc_threads<SRC == kCodes>()), smem, st, t);
+    return launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3((int)std::min<int64_t>(a.sms, jobs)), dim3(tc_threads<(SRC >= kCodes)>()), smem, st, t);
   const int grid = std::min(a.sms, kTcMaxCtas);
-  e = launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3(grid), dim3(tc_threads<SRC == kCodes>()), smem, st, t);
+  e = launch_pdl(attn_tc_kernel<D, BF16, SRC>, dim3(grid), dim3(tc_threads<(SRC >= kCodes)>()), smem, st, t);
   if (e != cudaSuccess) return e;
   // a CTA's run cuts off the start of one job at most
   const int64_t cut = std::min<int64_t>(jobs, grid);

@@ -105,6 +105,7 @@ struct AttnArgs {
   RowsList *list;
   TcList *tc_list;
   int runs;               // tensor-core form: equal runs of tiles
+  int few;                // over codes: jobs of one query tile
   int sms, device;
   int give_up;            // a CTA's copying warp gives up before its first tile
 };

@@ -549,3 +549,64 @@ def test_contexts_of_seventy_thousand_positions(new):
     b = Codes([new], [70001], 4, 1, 64, F16, 16, seed=34).append()
     for window in (0, 66000):
         b.check(window)
+
+
+# -- chunks of one query tile: the two softmax groups share its tiles of positions ------
+ONE_TILE = [([17, 18, 5], [17, 1290, 128]), ([18], [2049]), ([4, 9, 18], [256, 384, 129]), ([18, 0, 12], [9, 0, 1500]), ([6] * 9, [640] * 9)]
+
+
+@pytest.mark.parametrize("news,lens", ONE_TILE)
+@pytest.mark.parametrize("hq,hkv,d,dtype,page", [(40, 8, 128, BF16, 16), (28, 4, 128, F16, 64), (8, 2, 64, BF16, 128), (1, 1, 64, F16, 16)])
+def test_chunks_of_one_query_tile(news, lens, hq, hkv, d, dtype, page):
+    b = Codes(news, lens, hq, hkv, d, dtype, page, seed=35).append()
+    for window in (0, 1, 40, 129, 300):
+        b.check(window)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_one_query_tile_over_pages_of_very_different_powers(dtype):
+    test_pages_of_very_different_powers([9, 14], dtype)
+    test_keys_of_zeros_and_small_queries([9, 14], dtype)
+
+
+def test_one_query_tile_over_far_powers():
+    test_far_powers_of_bf16([20, 30])
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("rising", [True, False])
+def test_one_query_tile_with_weights_and_values_in_every_other_tile(page, rising):
+    """Scores and values of the even tiles of positions far from those of the odd ones."""
+    b = Codes([20], [700], 4, 1, 128, BF16, page, seed=36)
+    tile = torch.arange(700) // 128
+    b.k[0] *= torch.exp2(((tile % 2 == 0) == rising).float() * 3)[:, None, None].to(BF16)
+    b.v[0] *= torch.exp2((tile % 2 == (1 if rising else 0)).float() * 40)[:, None, None].to(BF16)
+    b.append().same()
+    for window in (0, 128, 300):
+        b.check(window)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_one_query_tile_with_values_that_are_not_finite(bad):
+    test_values_that_are_not_finite_reach_only_rows_that_see_them([20, 12], bad)
+    test_queries_that_are_not_finite_spoil_their_rows_alone([40])
+
+
+@pytest.mark.parametrize("news,lens", [([18, 1, 7], [3000, 1000, 700]), ([7] * 20, [500] * 20)])
+def test_one_query_tile_repeated_strided_and_captured(news, lens):
+    test_strided_queries_and_repeated_calls_agree_to_the_bit(news, lens)
+    test_captured_and_replayed_as_lengths_grow(news, lens)
+
+
+def test_more_tokens_than_said_of_one_query_tile():
+    """Refused by the device's own check; what is read and written stays in bounds and
+    later calls are as before."""
+    b = Codes([60, 9], [300, 90], 10, 2, 128, BF16, 16, seed=37).append()
+    keep = b.attend(0.088)
+    b.attend(0.088, max_new=9)
+    assert b.cache.device_error() == 4
+    assert torch.equal(b.attend(0.088), keep) and b.cache.device_error() == 0
+
+
+def test_one_query_tile_that_gives_up_says_so():
+    test_an_attention_that_gives_up_says_so([20, 7])
