@@ -586,7 +586,10 @@ kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
  * others read as the nearest of these), so that every element is a number of the
  * dtype.  Attention is as over pages of the dtype, with the products' operands in
  * F16: weights are rounded to it once; queries are exact down to 2^-28 of a row's
- * largest; with more than 16 rows of a KV head (max_new times its query heads)
+ * largest.  With at most 16 rows of a KV head (max_new times its query heads) a weight
+ * is off by 2^-39 of its row's largest, times the largest power among the pages that
+ * any of the sequence's rows sees over its own page's, at most below F16's normal
+ * numbers.  With more rows it is off by 2^-33 of its row's largest at most there, and
  * elements are exact down to 2^-21 of the largest power among the pages of 128
  * positions (keys) or of the sequence so far (values), and off by 2^-31 of that power
  * at most below.  The handle serves every kvk_paged_ call.

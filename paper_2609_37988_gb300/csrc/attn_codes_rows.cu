@@ -14,9 +14,9 @@
 // Codes are exact in f16 and go to the tensor cores as they are: S^T = K Q^T and
 // O^T += V^T P^T on mma.m16n8k16.  The keys' power multiplies the scores.  The
 // values' power enters the weights: a warp's sums O are kept relative to 2^E, E the
-// largest power so far, the weights p 2^(e - E) are rounded to f16 (half a step:
-// 2^-12 of a weight; kept 2^14 times as large, what the type's subnormals cut off is
-// 2^-39 of the row's largest).  Queries are f16 too: bf16 ones, a row times the power
+// largest power so far among the pages that the unit's rows see, the weights p 2^(e - E)
+// are rounded to f16 (half a step: 2^-11 of a weight; kept 2^14 times as large, what the
+// type's subnormals cut off is 2^-39 of the row's largest, times 2^(E - e)).  Queries are f16 too: bf16 ones, a row times the power
 // of two that brings its largest to [2^13, 2^14), which is exact but for numbers
 // below 2^-28 of that.
 //
@@ -153,12 +153,13 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
       }
       return n;
     };
+    // (no page: the least power, so that its zeros do not move the sums' 2^E)
     auto powers = [&](const Next &n, const int8_t *e) {
       const int8_t *p = e + (int64_t)n.page * pv.Hkv + n.h;
       const bool in = n.page < pv.n_pages;
-      if (HC == 4) return (uint32_t)load_if(reinterpret_cast<const int32_t *>(p), in, 0);
-      if (HC == 2) return (uint32_t)load_if(reinterpret_cast<const uint16_t *>(p), in, 0);
-      return (uint32_t)load_if(reinterpret_cast<const uint8_t *>(p), in, 0);
+      if (HC == 4) return (uint32_t)load_if(reinterpret_cast<const int32_t *>(p), in, (int)0x80808080u);
+      if (HC == 2) return (uint32_t)load_if(reinterpret_cast<const uint16_t *>(p), in, 0x8080);
+      return (uint32_t)load_if(reinterpret_cast<const uint8_t *>(p), in, 0x80);
     };
     auto step = [&]() {
       if (++at.t >= at.nt) next_unit(a, units, at);

@@ -610,3 +610,42 @@ def test_more_tokens_than_said_of_one_query_tile():
 
 def test_one_query_tile_that_gives_up_says_so():
     test_an_attention_that_gives_up_says_so([20, 7])
+
+
+# -- few tokens: what enters the weights ---------------------------------------------------
+def few_bound(b, r, s):
+    """oracle.serving.attend_bound for up to 16 rows of a KV head: weights are rounded to f16
+    (half a step of 2^-11), kept 2^14 times as large as a row's largest and times 2^(e - E) of
+    their page's power against the largest of the pages that are seen; what f16 cuts off, half
+    of 2^-24, is 2^-39 * 2^(E - e) of the row's largest.  No term of f16 tiles of values."""
+    l = max(b.lens[s], 1)
+    pages = b.table[s, :(l + b.page - 1) // b.page]
+    e = b.exps[1][pages].astype(int)
+    smallest = 2.0 ** (e.max() - e.min() - 39)
+    return osv.attend_bound(*r, b.d, l, 2.0 ** -11, smallest) + U[b.dtype] * np.abs(r[0]) * (1 + U[b.dtype])
+
+
+# odd and even numbers of pages, ends in either half of a warp's 32 positions
+SHORT = [1, 16, 17, 33, 48, 80, 100, 144, 300, 305, 400]
+LONG = [529, 545, 1100, 1300, 2060]
+
+
+@pytest.mark.parametrize("lens", [SHORT, LONG])
+@pytest.mark.parametrize("page", [16, 32, 64, 128])
+@pytest.mark.parametrize("hq,hkv,d,new,dtype", [(8, 2, 64, 1, BF16), (8, 2, 64, 4, BF16), (40, 8, 128, 1, BF16), (40, 8, 128, 3, BF16),
+                                                (7, 1, 128, 2, BF16), (28, 4, 128, 1, F16)])
+def test_few_tokens_over_small_values(lens, page, hq, hkv, d, new, dtype):
+    """Positions that no row sees, behind a context or before its window, bring no power
+    into the weights of those that are seen, however small their values are."""
+    b = Codes([min(new, l) for l in lens], lens, hq, hkv, d, dtype, page, seed=38)
+    for s, x in enumerate(b.v):
+        x *= 2.0 ** ((-90, -30, -60, -20) if dtype == BF16 else (-8, -4, -6, -2))[s % 4]
+    b.append().same()
+    scale = 1.0 / math.sqrt(d)
+    for window in (0, 5, 33, 200):
+        got, at = f64(b.attend(scale, window)), 0
+        for s, n in enumerate(b.news):
+            r = osv.attend(f64(b.q[at:at + n]), b.held(0, s), b.held(1, s), scale, window)
+            close(got[at:at + n], r[0], few_bound(b, r, s), f"window {window}, {b.lens[s]} positions")
+            at += n
+    assert b.cache.device_error() == 0
