@@ -343,7 +343,8 @@ __global__ void __launch_bounds__(kThreads + 32, 2) attn_codes_rows_kernel(const
         mx[i] = -INFINITY;
 #pragma unroll
         for (int b = 0; b < PB; ++b) {
-          const float f = sig[i] * fk[b];
+          // (finite: powers past binary32 times a score of 0 are 0)
+          const float f = fminf(sig[i] * fk[b], 3.4028234e38f);
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             float &x = s[b][i >> 1][2 * y + (i & 1)];

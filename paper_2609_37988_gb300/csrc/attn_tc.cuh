@@ -1044,8 +1044,9 @@ __global__ void __launch_bounds__(tc_threads<(SRC >= kCodes)>(), 1) attn_tc_kern
           float fo = 1.f;  // the values' power has risen
           if constexpr (CODES) {
             const TilePow *tp = &pows[(j.tile0 + jt) % SM::kPows];
-            // (not 0, which times a masked score would be NaN: pages of zeros)
-            sg = fmaxf(sg_row * pow2f(tp->kref), 1.1754944e-38f);
+            // (not 0, which times a masked score would be NaN: pages of zeros; nor
+            // infinite, which times a score of 0 would be)
+            sg = fminf(fmaxf(sg_row * pow2f(tp->kref), 1.1754944e-38f), 3.4028234e38f);
             const int vref = tp->vref;
             if (jt > j0 && vref > unit) fo = pow2f(max(unit - vref, -126));
             unit = vref;

@@ -649,3 +649,19 @@ def test_few_tokens_over_small_values(lens, page, hq, hkv, d, new, dtype):
             close(got[at:at + n], r[0], few_bound(b, r, s), f"window {window}, {b.lens[s]} positions")
             at += n
     assert b.cache.device_error() == 0
+
+
+@pytest.mark.parametrize("new", [1, 3, 20, 60])
+@pytest.mark.parametrize("qe,ke", [(100, 100), (120, 60), (60, 120), (126, 126), (-120, 118)])
+def test_scores_of_zero_between_numbers_at_the_ends_of_bf16(new, qe, ke):
+    """Queries and keys whose powers multiply past binary32, in different channels: all
+    scores are 0, and every position that is seen has the same weight."""
+    b = Codes([new, 1], [100, 77], 8, 2, 64, BF16, 16, seed=39)
+    b.q.zero_()
+    b.q[..., 0] = 2.0 ** qe
+    for x in b.k:
+        x.zero_()
+        x[..., 1] = 2.0 ** ke
+    b.append().same()
+    for window in (0, 33):
+        b.check(window)
