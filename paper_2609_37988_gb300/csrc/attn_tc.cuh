@@ -1218,7 +1218,8 @@ __global__ void __launch_bounds__(tc_threads<(SRC >= kCodes)>(), 1) attn_tc_kern
         const int down = CODES && unit > 0 ? 40 : 0;
         const float fu = CODES ? pow2f(slot_out >= 0 ? unit - down : unit) : 1.f;
         if (slot_out >= 0) {  // the piece's reference and sum
-          part[kTcT * D - 3 * row] = m == -INFINITY ? m : m - kShift + (float)down;
+          // (no 0 added in 16 bits: it cost the f16 forms 12-32 bytes of spills)
+          part[kTcT * D - 3 * row] = m == -INFINITY ? m : CODES ? m - kShift + (float)down : m - kShift;
           part[kTcT * (D + 1) - 3 * row] = CODES ? l * pow2f(-down) : l;
         }
         uint8_t *dst = static_cast<uint8_t *>(a.out) + 2 * ((int64_t)(j.q0 + tok) * a.Hq + j.h * G + (row - my_tok * G)) * D;
