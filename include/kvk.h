@@ -674,8 +674,8 @@ kvk_status kvk_paged_copy(kvk_paged *cache, const int32_t *src, const int32_t *d
  * the next call.  Entries behind a row's pages are -1, as are those that no free page
  * was left for, which sets KVK_DEVERR_CAPACITY.  A parent that is no row (taken for -1), a negative length or
  * one past max_pages_out (cut) sets KVK_DEVERR_COUNT.  table_out may not overlap
- * table.  batch: at most 2^24, rows: at most 16384; with 0 rows all pages of the given
- * ones are let go of. */
+ * table.  batch: at most 2^24, rows: at most 16384, table_out at most 2^30 entries; with
+ * 0 rows all pages of the given ones are let go of. */
 kvk_status kvk_paged_fork(kvk_paged *cache, const int32_t *refs, const int32_t *table, const int32_t *lengths,
                           int32_t batch, int32_t max_pages, const int32_t *parents, const int32_t *after, int32_t rows,
                           int32_t *refs_out, int32_t *table_out, int32_t max_pages_out, kvk_stream stream);

@@ -611,6 +611,9 @@ kvk_status kvk_paged_fork(kvk_paged *p, const int32_t *refs, const int32_t *tabl
   if (rows < 0 || rows > kForkRows) return fail(KVK_ERR_INVALID_ARG, "rows must be in [0, %d]", kForkRows);
   if (max_pages_out < 0 || (int64_t)max_pages_out * p->d.page_size > (1 << 26))
     return fail(KVK_ERR_INVALID_ARG, "max_pages_out out of range");
+  // (what all rows ask for is counted in 32 bits)
+  if ((int64_t)rows * max_pages_out > (1 << 30))
+    return fail(KVK_ERR_INVALID_ARG, "a table of %d x %d pages: more than 2^30 entries", rows, max_pages_out);
   if (rows && (!parents || (!table_out && max_pages_out))) return fail(KVK_ERR_INVALID_ARG, "null parents or table");
   if (!aligned(parents, 4) || !aligned(after, 4) || !aligned(table_out, 4))
     return fail(KVK_ERR_INVALID_ARG, "misaligned parents, lengths or table");

@@ -130,3 +130,18 @@ def test_refusals_with_a_cache(lib):
         with pytest.raises(TypeError):
             c.append(0, x.half(), x.half(), cu, lens, table)
         assert c.device_error() == 0
+
+
+@pytest.mark.gpu
+def test_a_fork_of_more_entries_than_are_counted_is_refused(lib):
+    """1025 rows of 2^22 pages: those that the rows before the last ask for are 2^32, 0 in 32 bits."""
+    from paper_2609_37988_gb300.serving import PagedCache
+    ints = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = PagedCache(n_q_heads=2, n_layers=1, n_kv_heads=1, head_dim=64, n_pages=4)
+    refs, parents = ints([0] * 4), ints([-1] * 1025)
+    r, p, out = refs.data_ptr(), parents.data_ptr(), ints([0] * 8).data_ptr()
+    fork = lambda rows, width: lib.load().kvk_paged_fork(c.handle, r, None, None, 0, 0, p, None, rows, r, out, width, None)  # noqa: E731
+    assert fork(1025, 2 ** 22) == INVALID and fork(257, 2 ** 22) == INVALID and fork(1025, 2 ** 21) == INVALID
+    assert fork(1, 8) == 0 and fork(1025, 0) == 0
+    torch.cuda.synchronize()
+    assert c.device_error() == 0 and not refs.any()
