@@ -252,8 +252,10 @@ kvk_status check_pages(const kvk_paged *p, const int32_t *refs, const int32_t *r
 }
 
 // Rows of a KV head up to which the form for few tokens is the faster one (us,
-// few / tensor cores, 14B-shaped layer: 4 x 8192 positions, 10 rows 39 / 40, 20
-// rows 54 / 40; 1 x 1024, 10 rows 17 / 18).
+// few / tensor cores, 14B-shaped layer, 16 bits: 4 x 8192 positions, 10 rows 39 / 40, 20
+// rows 54 / 40; 1 x 1024, 10 rows 17 / 18).  In 8 bits, where that form ends at 16
+// rows: 4 x 8192, 15 rows 34 / 42; 32 x 8192 116 / 167; 1 x 1024 17 / 26; 28 / 4 heads,
+// 14 rows, 32 x 8192 69 / 92; 8 / 2 heads of 64, 16 rows, 32 x 8192 36 / 46.
 constexpr int kFewRows = 16;
 cudaError_t launch_attn(const AttnArgs &a, int dtype, cudaStream_t st) {
   if (a.pv.ke) return (int64_t)a.max_new * a.G <= kFewRows ? launch_attn_codes_rows(a, dtype, st) : launch_attn_tc_codes(a, dtype, st);

@@ -386,3 +386,19 @@ def test_beams_of_codes_over_a_compaction():
     assert not torch.equal(table, table2)
     b = cache.attend(0, q, cu, lens, table2, 0.088, max_new=1)
     assert torch.equal(a, b) and cache.device_error() == 0
+
+
+def test_fork_of_as_many_rows_as_there_may_be():
+    page, R, B, width, n_pages = 16, 16384, 700, 5, 40000
+    g = np.random.default_rng(78)
+    lens = [int(g.integers(0, 4)) * page + (int(g.integers(1, page)) if b % 20 == 0 else 0) for b in range(B)]
+    refs, table = table_of(g, n_pages, page, lens, width, shared=300)
+    parents = [int(x) for x in g.integers(-1, B, R)]
+    after = [(lens[p] if p >= 0 else 0) + int(g.integers(0, 2)) * page for p in parents]
+    pool = Pool(n_pages, page, 8, layers=1, hkv=1)
+    refs2, out, copies, short = paged.fork(refs, table, lens, parents, after, width, page)
+    assert short == 0 and len(copies) > 500
+    got_refs, got = pool.cache.fork(*[ints(x) for x in (refs.tolist(), table.tolist(), lens, parents, after)])
+    np.testing.assert_array_equal(got.cpu().numpy(), out)
+    np.testing.assert_array_equal(got_refs.cpu().numpy(), refs2)
+    pool.moved(copies)
