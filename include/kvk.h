@@ -591,8 +591,8 @@ kvk_status kvk_paged_reset(kvk_paged *cache, kvk_stream stream);
  * any of the sequence's rows sees over its own page's, at most below F16's normal
  * numbers.  With more rows it is off by 2^-33 of its row's largest at most there, and
  * elements are exact down to 2^-21 of the largest power among the pages of 128
- * positions (keys) or of the sequence so far (values), and off by 2^-31 of that power
- * at most below.  The handle serves every kvk_paged_ call.
+ * positions (keys) or, so far, among all that any of the sequence's rows sees (values),
+ * and off by 2^-31 of that power at most below.  The handle serves every kvk_paged_ call.
  *
  * An append sets a page and head's exponent to the least that holds the largest
  * finite magnitude among its new numbers, max |x| <= 448 * 2^exponent, and the codes
